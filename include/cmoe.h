@@ -318,6 +318,113 @@ int cmoe_hier_forward_plan(const cmoe_hier* h, int dense, int64_t T, int32_t pla
 #define CMOE_SCORER_SPLIT   3    /* partial sums, then selection */
 int cmoe_scorer_plan(const cmoe_layer* layer, int64_t T, int32_t plan[2]);
 
+/* ---- operators around the feed-forward layer: dropout, norm, low-rank adapters ------------- *
+ * Batches are [rows, cols] in their dtype, contiguous; addresses need only the alignment of an element (16 bytes is faster).
+ * All only enqueue work.  An output may be the very buffer of an input of its own size (for the adapters: y of base, dx of
+ * dx_base alone); other overlaps are refused.  Statistics and sums are fp32.
+ *
+ * Dropout masks are not stored: element (r, c) of a batch is a function of (seed, offset, r * ceil(cols / 8) + c / 8), by
+ * Philox-4x32-10, in 16 random bits; p counts in steps of 1 / 65536, and what is kept is scaled by the inverse of the rate at which
+ * it is.  A dropped element is 0, whatever it was.  A program gives every batch an offset of its own.  p = 0: no dropout. */
+
+/* y = drop(x) + residual (may be NULL).  The gradient of x is cmoe_dropout of y's, with the same seed and offset. */
+int cmoe_dropout(const void* x, void* y, const void* residual, int64_t rows, int32_t cols, int32_t dtype, double p, uint64_t seed,
+                 uint64_t offset, void* hip_stream);
+
+#define CMOE_NORM_LAYER 0     /* (s - mean) / sqrt(var + eps) */
+#define CMOE_NORM_RMS   1     /* s / sqrt(mean(s^2) + eps)    */
+
+/* s = drop(x) + residual, rounded to dtype if sum_out is given; y = norm(s) * weight + bias.  cols <= 32768. */
+typedef struct {
+  const void* x;
+  const void* residual;      /* [rows, cols] or NULL */
+  void* sum_out;             /* [rows, cols]: s, or NULL */
+  void* y;
+  const void* weight;        /* [cols] or NULL (1) */
+  const void* bias;          /* [cols] or NULL (0) */
+  float* mean;               /* [rows] or NULL (the rms form writes zeros) */
+  float* rstd;               /* [rows] or NULL */
+  int64_t rows;
+  double p;                  /* dropout of x */
+  uint64_t seed, offset;
+  int32_t struct_bytes;      /* sizeof(cmoe_norm_forward_args) */
+  int32_t dtype, form, cols;
+  float eps;
+  int32_t reserved;
+} cmoe_norm_forward_args;
+int cmoe_norm_forward(const cmoe_norm_forward_args* args, void* hip_stream);
+
+/* Gradients, from s (x itself where nothing was added or dropped) and the statistics of the forward pass:
+ * dresidual = (gradient of s through the norm) + dsum, dx = drop's backward of it, dweight = sum of dy * norm(s), dbias = sum of dy. */
+typedef struct {
+  const void* dy;
+  const void* s;
+  const void* dsum;          /* [rows, cols]: the gradient that reaches s past the norm, or NULL */
+  const void* weight;
+  const float* mean;         /* layer form */
+  const float* rstd;
+  void* dx;
+  void* dresidual;           /* [rows, cols] or NULL */
+  float* dweight;            /* [cols] fp32 or NULL */
+  float* dbias;              /* [cols] fp32 or NULL; needs dweight */
+  void* workspace;           /* 16-byte aligned, needed with dweight */
+  uint64_t workspace_bytes;
+  int64_t rows;
+  double p;
+  uint64_t seed, offset;
+  int32_t struct_bytes;      /* sizeof(cmoe_norm_backward_args) */
+  int32_t dtype, form, cols;
+} cmoe_norm_backward_args;
+size_t cmoe_norm_backward_workspace_bytes(int64_t rows, int32_t cols);
+int cmoe_norm_backward(const cmoe_norm_backward_args* args, void* hip_stream);
+
+/* Low-rank adapters of many requests beside a shared projection: y[t] = base[t] + scale[k] * B_k (A_k drop(x[t])), k = ids[t].
+ * A token whose id is not in [0, n_adapters) has no adapter (y = base).  rank <= 64. */
+typedef struct {
+  const void* x;             /* [tokens, d_in] */
+  const void* a;             /* [n_adapters, rank, d_in] */
+  const void* b;             /* [n_adapters, d_out, rank] */
+  const float* scale;        /* [n_adapters] fp32 */
+  const int32_t* ids;        /* [tokens], or NULL: adapter 0 for every token */
+  const void* base;          /* [tokens, d_out], or NULL: 0 */
+  void* y;
+  float* u;                  /* [tokens, rank] fp32: A_k drop(x[t]) (0 without an adapter), for the backward pass, or NULL */
+  void* workspace;           /* 16-byte aligned */
+  uint64_t workspace_bytes;
+  int64_t tokens;
+  double p;                  /* dropout of x */
+  uint64_t seed, offset;
+  int32_t struct_bytes;      /* sizeof(cmoe_adapters_forward_args) */
+  int32_t dtype, d_in, d_out, rank, n_adapters;
+} cmoe_adapters_forward_args;
+size_t cmoe_adapters_forward_workspace_bytes(int64_t tokens, int32_t d_in, int32_t d_out, int32_t rank, int32_t n_adapters, int32_t dtype);
+int cmoe_adapters_forward(const cmoe_adapters_forward_args* args, void* hip_stream);
+
+/* dx = dx_base + drop's backward of scale[k] * A_k^T (B_k^T dy[t]); da, db: the gradients of every adapter of the bank (0 where no
+ * token has it), da[k] = scale[k] * sum over its tokens of (B_k^T dy) drop(x)^T, db[k] = scale[k] * sum of dy u^T. */
+typedef struct {
+  const void* dy;            /* [tokens, d_out] */
+  const void* x;
+  const float* u;            /* of the forward pass; needed for db */
+  const void* a;
+  const void* b;
+  const float* scale;
+  const int32_t* ids;
+  const void* dx_base;       /* [tokens, d_in], or NULL: 0 */
+  void* dx;                  /* [tokens, d_in] or NULL */
+  float* da;                 /* [n_adapters, rank, d_in] fp32 or NULL */
+  float* db;                 /* [n_adapters, d_out, rank] fp32 or NULL */
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t tokens;
+  double p;
+  uint64_t seed, offset;
+  int32_t struct_bytes;      /* sizeof(cmoe_adapters_backward_args) */
+  int32_t dtype, d_in, d_out, rank, n_adapters;
+} cmoe_adapters_backward_args;
+size_t cmoe_adapters_backward_workspace_bytes(int64_t tokens, int32_t d_in, int32_t d_out, int32_t rank, int32_t n_adapters, int32_t dtype);
+int cmoe_adapters_backward(const cmoe_adapters_backward_args* args, void* hip_stream);
+
 const char* cmoe_last_error(void);   /* thread-local, never NULL */
 const char* cmoe_version(void);
 

@@ -11,7 +11,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, Optional, Sequence
+import struct
+from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -42,6 +43,8 @@ EXPORTS = [
     "cmoe_build_gpu", "cmoe_profile_activations", "cmoe_set_baseline", "cmoe_hier_build", "cmoe_hier_expert",
     "cmoe_set_tuning", "cmoe_set_neuron_sparsity", "cmoe_forward_static", "cmoe_static_scratch_bytes", "cmoe_forward_static_max_tokens",
     "cmoe_forward_plan", "cmoe_hier_forward_plan", "cmoe_scorer_plan",
+    "cmoe_dropout", "cmoe_norm_forward", "cmoe_norm_backward", "cmoe_norm_backward_workspace_bytes",
+    "cmoe_adapters_forward", "cmoe_adapters_forward_workspace_bytes", "cmoe_adapters_backward", "cmoe_adapters_backward_workspace_bytes",
 ]
 
 
@@ -108,6 +111,14 @@ def load():
     lib.cmoe_forward_plan.argtypes = [vp, C.c_int, i64, i32p]
     lib.cmoe_hier_forward_plan.argtypes = [vp, C.c_int, i64, i32p]
     lib.cmoe_scorer_plan.argtypes = [vp, i64, i32p]
+    lib.cmoe_dropout.argtypes = [vp, vp, vp, i64, C.c_int32, C.c_int32, C.c_double, C.c_uint64, C.c_uint64, vp]
+    for name in ("cmoe_norm_forward", "cmoe_norm_backward", "cmoe_adapters_forward", "cmoe_adapters_backward"):
+        getattr(lib, name).argtypes = [C.c_char_p, vp]                   # the packed bytes of an argument struct
+    lib.cmoe_norm_backward_workspace_bytes.argtypes = [i64, C.c_int32]
+    lib.cmoe_norm_backward_workspace_bytes.restype = sz
+    for name in ("cmoe_adapters_forward_workspace_bytes", "cmoe_adapters_backward_workspace_bytes"):
+        getattr(lib, name).argtypes = [i64] + [C.c_int32] * 5
+        getattr(lib, name).restype = sz
     lib.cmoe_last_error.restype = C.c_char_p
     lib.cmoe_version.restype = C.c_char_p
     _lib = lib
@@ -376,6 +387,170 @@ def cmoe_hier_destroy(h: int) -> None:
 
 def cmoe_version() -> str:
     return load().cmoe_version().decode()
+
+
+# ---- operators around the feed-forward layer -------------------------------------------------------
+
+_NORM_FORWARD = struct.Struct("=8QqdQQ4ifi")         # cmoe_norm_forward_args
+_NORM_BACKWARD = struct.Struct("=12QqdQQ4i")         # cmoe_norm_backward_args
+_ADAPTERS_FORWARD = struct.Struct("=10QqdQQ6i")      # cmoe_adapters_forward_args
+_ADAPTERS_BACKWARD = struct.Struct("=13QqdQQ6i")     # cmoe_adapters_backward_args
+_FORMS = {"layer": 0, "rms": 1}
+
+
+class Dropout(NamedTuple):
+    """Rate and counters of one batch's dropout.  The mask is a function of (seed, offset) and of an element's place, never
+    stored; the same values given to the backward pass drop the same elements.  Every batch takes an offset of its own."""
+    p: float
+    seed: int
+    offset: int = 0
+
+
+_KEEP_ALL = Dropout(0.0, 0, 0)
+
+
+def _drop(dropout: Optional[Dropout]) -> Dropout:
+    if dropout is None:
+        return _KEEP_ALL
+    if not 0.0 <= dropout.p <= 1.0 or not 0 <= dropout.seed < 1 << 64 or not 0 <= dropout.offset < 1 << 64:
+        raise CmoeError("dropout: p must be in [0, 1], seed and offset in [0, 2^64)")
+    return dropout
+
+
+def _dtype_of(name: str, t):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return t.dtype, CMOE_BF16
+    if t.dtype is torch.float32:
+        return t.dtype, CMOE_F32
+    raise CmoeError("%s must be bfloat16 or float32, not %s" % (name, t.dtype))
+
+
+def _operand(name: str, t, dtype, shape) -> int:
+    """Address of a contiguous tensor of that type and shape on the current device; 0 if it is None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise CmoeError("%s must be a contiguous %s tensor of shape %s, not %s %s%s" % (
+            name, dtype, tuple(shape), t.dtype, tuple(t.shape), "" if t.is_contiguous() else " with strides"))
+    if not t.is_cuda or t.get_device() != _current_device():
+        raise CmoeError("%s must be on the current HIP device" % name)
+    return t.data_ptr()
+
+
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+def _current_stream() -> int:
+    return _stream_ptr(_torch())
+
+
+def _workspace(nbytes: int):
+    """Device bytes of the caching allocator, ordered like the current stream: a later call may be given the same ones."""
+    import torch
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+
+
+def dropout(x, y, dropout: Dropout, residual=None) -> None:
+    """y = drop(x) + residual on [rows, cols] tensors (y may be x or residual).  Its own backward pass: drop the gradient."""
+    dtype, code = _dtype_of("x", x)
+    if x.dim() != 2:
+        raise CmoeError("x must be [rows, cols]")
+    shape, d = x.shape, _drop(dropout)
+    args = _operand("x", x, dtype, shape), _operand("y", y, dtype, shape), _operand("residual", residual, dtype, shape)
+    _check(load().cmoe_dropout(*args, shape[0], shape[1], code, d.p, d.seed, d.offset, _current_stream()), "cmoe_dropout")
+
+
+def norm_forward(x, y, weight=None, bias=None, *, form: str = "layer", eps: float = 1e-5, residual=None, dropout: Optional[Dropout] = None,
+                 sum_out=None, mean=None, rstd=None) -> None:
+    """s = drop(x) + residual, rounded to the tensors' type where sum_out takes it; y = norm(s) * weight + bias.
+
+    form: "layer" or "rms".  x, y, residual, sum_out: [rows, cols] of one type; weight, bias: [cols]; mean, rstd: [rows] fp32,
+    for the backward pass.  y and sum_out may be x or residual themselves."""
+    dtype, code = _dtype_of("x", x)
+    if x.dim() != 2 or form not in _FORMS:
+        raise CmoeError("x must be [rows, cols] and form one of %s" % ", ".join(_FORMS))
+    shape, d = x.shape, _drop(dropout)
+    rows, cols = shape
+    import torch
+    args = _NORM_FORWARD.pack(
+        _operand("x", x, dtype, shape), _operand("residual", residual, dtype, shape), _operand("sum_out", sum_out, dtype, shape),
+        _operand("y", y, dtype, shape), _operand("weight", weight, dtype, (cols,)), _operand("bias", bias, dtype, (cols,)),
+        _operand("mean", mean, torch.float32, (rows,)), _operand("rstd", rstd, torch.float32, (rows,)),
+        rows, d.p, d.seed, d.offset, _NORM_FORWARD.size, code, _FORMS[form], cols, eps, 0)
+    _check(load().cmoe_norm_forward(args, _current_stream()), "cmoe_norm_forward")
+
+
+def norm_backward(dy, s, dx, mean, rstd, weight=None, *, form: str = "layer", dsum=None, dropout: Optional[Dropout] = None, dresidual=None,
+                  dweight=None, dbias=None) -> None:
+    """Gradients of norm_forward from what it normalised (sum_out; x where nothing was added or dropped) and its statistics.
+
+    dsum: the gradient that reaches s past the norm; dresidual: the whole gradient of s; dx: that of x, through the dropout;
+    dweight, dbias: [cols] fp32."""
+    dtype, code = _dtype_of("dy", dy)
+    if dy.dim() != 2 or form not in _FORMS:
+        raise CmoeError("dy must be [rows, cols] and form one of %s" % ", ".join(_FORMS))
+    shape, d = dy.shape, _drop(dropout)
+    rows, cols = shape
+    import torch
+    f32 = torch.float32
+    operands = (
+        _operand("dy", dy, dtype, shape), _operand("s", s, dtype, shape), _operand("dsum", dsum, dtype, shape),
+        _operand("weight", weight, dtype, (cols,)), _operand("mean", mean, f32, (rows,)), _operand("rstd", rstd, f32, (rows,)),
+        _operand("dx", dx, dtype, shape), _operand("dresidual", dresidual, dtype, shape), _operand("dweight", dweight, f32, (cols,)),
+        _operand("dbias", dbias, f32, (cols,)))
+    nbytes = load().cmoe_norm_backward_workspace_bytes(rows, cols) if dweight is not None else 0
+    ws = _workspace(nbytes) if nbytes else None
+    args = _NORM_BACKWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, rows, d.p, d.seed, d.offset, _NORM_BACKWARD.size, code,
+                               _FORMS[form], cols)
+    _check(load().cmoe_norm_backward(args, _current_stream()), "cmoe_norm_backward")
+
+
+def _adapter_shapes(x_name: str, x, a, b):
+    dtype, code = _dtype_of(x_name, x)
+    if x.dim() != 2 or a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
+        raise CmoeError("adapters: %s must be [tokens, width], a [n, rank, d_in] and b [n, d_out, rank]" % x_name)
+    n, rank, d_in = a.shape
+    return dtype, code, x.shape[0], d_in, b.shape[1], rank, n
+
+
+def adapters_forward(x, y, a, b, scale, *, ids=None, base=None, dropout: Optional[Dropout] = None, u=None) -> None:
+    """y[t] = base[t] + scale[k] * b[k] @ (a[k] @ drop(x[t])) with k = ids[t] (no adapter where it is not in [0, n)).
+
+    x: [tokens, d_in]; y, base: [tokens, d_out] (y may be base itself; without a base it is 0); a: [n, rank, d_in]; b: [n, d_out, rank];
+    scale: [n] fp32; ids: [tokens] int32 in any order, None: adapter 0 for every token; u: [tokens, rank] fp32 for the backward pass."""
+    dtype, code, t, d_in, d_out, rank, n = _adapter_shapes("x", x, a, b)
+    import torch
+    d = _drop(dropout)
+    operands = (
+        _operand("x", x, dtype, (t, d_in)), _operand("a", a, dtype, (n, rank, d_in)), _operand("b", b, dtype, (n, d_out, rank)),
+        _operand("scale", scale, torch.float32, (n,)), _operand("ids", ids, torch.int32, (t,)), _operand("base", base, dtype, (t, d_out)),
+        _operand("y", y, dtype, (t, d_out)), _operand("u", u, torch.float32, (t, rank)))
+    nbytes = load().cmoe_adapters_forward_workspace_bytes(t, d_in, d_out, rank, n, code)
+    ws = _workspace(nbytes) if nbytes else None
+    args = _ADAPTERS_FORWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, d.p, d.seed, d.offset, _ADAPTERS_FORWARD.size, code, d_in,
+                                  d_out, rank, n)
+    _check(load().cmoe_adapters_forward(args, _current_stream()), "cmoe_adapters_forward")
+
+
+def adapters_backward(dy, x, u, a, b, scale, *, ids=None, dx=None, dx_base=None, dropout: Optional[Dropout] = None, da=None, db=None) -> None:
+    """Gradients of adapters_forward: dx = dx_base + what reaches x through the adapters; da, db: fp32, of a's and b's shapes, 0 for an
+    adapter that no token has.  x is read for da, u for db.  dx may be dx_base itself."""
+    dtype, code, t, d_in, d_out, rank, n = _adapter_shapes("dy", dy, a, b)
+    import torch
+    f32, d = torch.float32, _drop(dropout)
+    operands = (
+        _operand("dy", dy, dtype, (t, d_out)), _operand("x", x, dtype, (t, d_in)), _operand("u", u, f32, (t, rank)),
+        _operand("a", a, dtype, (n, rank, d_in)), _operand("b", b, dtype, (n, d_out, rank)), _operand("scale", scale, f32, (n,)),
+        _operand("ids", ids, torch.int32, (t,)), _operand("dx_base", dx_base, dtype, (t, d_in)), _operand("dx", dx, dtype, (t, d_in)),
+        _operand("da", da, f32, (n, rank, d_in)), _operand("db", db, f32, (n, d_out, rank)))
+    nbytes = load().cmoe_adapters_backward_workspace_bytes(t, d_in, d_out, rank, n, code)
+    ws = _workspace(nbytes) if nbytes else None
+    args = _ADAPTERS_BACKWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, d.p, d.seed, d.offset, _ADAPTERS_BACKWARD.size, code,
+                                   d_in, d_out, rank, n)
+    _check(load().cmoe_adapters_backward(args, _current_stream()), "cmoe_adapters_backward")
 
 
 # ---- conveniences for tests and the bench ----------------------------------------------------------

@@ -1,0 +1,59 @@
+// Dropout of a batch, with an addition to what it goes into: y = drop(x) + residual.  Forward, and backward on the gradient.
+#include <hip/hip_runtime.h>
+
+#include "../../include/cmoe.h"
+#include "cmoe_internal.h"
+#include "dropout_device.h"
+#include "operator_args.h"
+
+namespace cmoe {
+
+// A thread per chunk of eight elements.  The row of a workgroup's first chunk is a division of uniform 64-bit values, a
+// thread's own row one of 32-bit values.
+template <typename T>
+__global__ __launch_bounds__(256) void dropout_kernel(const T* x, const T* residual, T* y, int64_t rows, int cols, Drop drop) {
+  const uint32_t per_row = (cols + 7) >> 3;
+  const uint64_t first = (uint64_t)blockIdx.x * 256;
+  const uint64_t row0 = first / per_row;
+  const uint32_t c0 = (uint32_t)(first - row0 * per_row) + threadIdx.x;
+  const uint64_t row = row0 + c0 / per_row;
+  if (row >= (uint64_t)rows) return;
+  const int c = (int)(c0 % per_row);
+  const int n = cols - c * 8;
+  const uint64_t at = row * cols + (uint64_t)c * 8;
+  float v[8], r[8];
+  load8(x + at, n, v);
+  if (residual) load8(residual + at, n, r);
+  drop8(v, drop, first + threadIdx.x);
+  if (residual) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += r[e];
+  }
+  store8(y + at, n, v);
+}
+
+}  // namespace cmoe
+
+extern "C" int cmoe_dropout(const void* x, void* y, const void* residual, int64_t rows, int32_t cols, int32_t dtype, double p, uint64_t seed,
+                            uint64_t offset, void* hip_stream) {
+  using namespace cmoe;
+  const char* what = "cmoe_dropout";
+  if (dtype != CMOE_F32 && dtype != CMOE_BF16) return fail(CMOE_EINVAL, "%s: dtype must be CMOE_F32 or CMOE_BF16", what);
+  if (rows < 0 || cols < 1 || cols > (1 << 30)) return fail(CMOE_EINVAL, "%s: need rows >= 0 and 1 <= cols <= 2^30", what);
+  const uint64_t per_row = ((uint64_t)cols + 7) / 8;
+  if ((uint64_t)rows > (uint64_t)0xffffff00 / per_row)      // a launch has fewer than 2^32 threads
+    return fail(CMOE_EINVAL, "%s: the batch is too large", what);
+  Drop drop;
+  if (int rc = make_drop(what, p, seed, offset, &drop)) return rc;
+  if (rows == 0) return CMOE_OK;
+  if (!x || !y) return fail(CMOE_EINVAL, "%s: x or y is null", what);
+  const size_t es = elem_size(dtype);
+  const uint64_t bytes = (uint64_t)rows * cols * es;
+  if (int rc = check_operands(what, {{"x", x, bytes, es}, {"residual", residual, bytes, es}}, {{"y", y, bytes, es}}, true)) return rc;
+  const dim3 grid((unsigned)(((uint64_t)rows * per_row + 255) / 256));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (dtype == CMOE_BF16) hipLaunchKernelGGL(dropout_kernel<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)x, (const bf16_t*)residual, (bf16_t*)y, rows, cols, drop);
+  else hipLaunchKernelGGL(dropout_kernel<float>, grid, dim3(256), 0, s, (const float*)x, (const float*)residual, (float*)y, rows, cols, drop);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? CMOE_OK : fail(CMOE_EHIP, "%s: %s", what, hipGetErrorString(e));
+}
