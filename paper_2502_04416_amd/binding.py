@@ -426,25 +426,26 @@ def _dtype_of(name: str, t):
     raise CmoeError("%s must be bfloat16 or float32, not %s" % (name, t.dtype))
 
 
-def _operand(name: str, t, dtype, shape) -> int:
-    """Address of a contiguous tensor of that type and shape on the current device; 0 if it is None."""
+def _operand(name: str, t, dtype, shape, device: int = -2) -> int:
+    """Address of a contiguous tensor of that type and shape on the device; 0 if it is None."""
     if t is None:
         return 0
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise CmoeError("%s must be a contiguous %s tensor of shape %s, not %s %s%s" % (
             name, dtype, tuple(shape), t.dtype, tuple(t.shape), "" if t.is_contiguous() else " with strides"))
-    if not t.is_cuda or t.get_device() != _current_device():
+    if t.get_device() != device:
         raise CmoeError("%s must be on the current HIP device" % name)
     return t.data_ptr()
 
 
-def _current_device() -> int:
+def _place(name: str, t) -> tuple:
+    """(device, its current stream) of a tensor on the current device.  The raw handle: a small call's time is mostly the host's,
+    and torch's stream objects take 2.7 us of it, this 0.3."""
     import torch
-    return torch.cuda.current_device()
-
-
-def _current_stream() -> int:
-    return _stream_ptr(_torch())
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        raise CmoeError("%s must be on the current HIP device" % name)
+    return device, torch._C._cuda_getCurrentRawStream(device)
 
 
 def _workspace(nbytes: int):
@@ -459,8 +460,9 @@ def dropout(x, y, dropout: Dropout, residual=None) -> None:
     if x.dim() != 2:
         raise CmoeError("x must be [rows, cols]")
     shape, d = x.shape, _drop(dropout)
-    args = _operand("x", x, dtype, shape), _operand("y", y, dtype, shape), _operand("residual", residual, dtype, shape)
-    _check(load().cmoe_dropout(*args, shape[0], shape[1], code, d.p, d.seed, d.offset, _current_stream()), "cmoe_dropout")
+    dev, stream = _place("x", x)
+    args = _operand("x", x, dtype, shape, dev), _operand("y", y, dtype, shape, dev), _operand("residual", residual, dtype, shape, dev)
+    _check(load().cmoe_dropout(*args, shape[0], shape[1], code, d.p, d.seed, d.offset, stream), "cmoe_dropout")
 
 
 def norm_forward(x, y, weight=None, bias=None, *, form: str = "layer", eps: float = 1e-5, residual=None, dropout: Optional[Dropout] = None,
@@ -474,13 +476,14 @@ def norm_forward(x, y, weight=None, bias=None, *, form: str = "layer", eps: floa
         raise CmoeError("x must be [rows, cols] and form one of %s" % ", ".join(_FORMS))
     shape, d = x.shape, _drop(dropout)
     rows, cols = shape
+    dev, stream = _place("x", x)
     import torch
     args = _NORM_FORWARD.pack(
-        _operand("x", x, dtype, shape), _operand("residual", residual, dtype, shape), _operand("sum_out", sum_out, dtype, shape),
-        _operand("y", y, dtype, shape), _operand("weight", weight, dtype, (cols,)), _operand("bias", bias, dtype, (cols,)),
-        _operand("mean", mean, torch.float32, (rows,)), _operand("rstd", rstd, torch.float32, (rows,)),
+        _operand("x", x, dtype, shape, dev), _operand("residual", residual, dtype, shape, dev), _operand("sum_out", sum_out, dtype, shape, dev),
+        _operand("y", y, dtype, shape, dev), _operand("weight", weight, dtype, (cols,), dev), _operand("bias", bias, dtype, (cols,), dev),
+        _operand("mean", mean, torch.float32, (rows,), dev), _operand("rstd", rstd, torch.float32, (rows,), dev),
         rows, d.p, d.seed, d.offset, _NORM_FORWARD.size, code, _FORMS[form], cols, eps, 0)
-    _check(load().cmoe_norm_forward(args, _current_stream()), "cmoe_norm_forward")
+    _check(load().cmoe_norm_forward(args, stream), "cmoe_norm_forward")
 
 
 def norm_backward(dy, s, dx, mean, rstd, weight=None, *, form: str = "layer", dsum=None, dropout: Optional[Dropout] = None, dresidual=None,
@@ -494,18 +497,19 @@ def norm_backward(dy, s, dx, mean, rstd, weight=None, *, form: str = "layer", ds
         raise CmoeError("dy must be [rows, cols] and form one of %s" % ", ".join(_FORMS))
     shape, d = dy.shape, _drop(dropout)
     rows, cols = shape
+    dev, stream = _place("dy", dy)
     import torch
     f32 = torch.float32
     operands = (
-        _operand("dy", dy, dtype, shape), _operand("s", s, dtype, shape), _operand("dsum", dsum, dtype, shape),
-        _operand("weight", weight, dtype, (cols,)), _operand("mean", mean, f32, (rows,)), _operand("rstd", rstd, f32, (rows,)),
-        _operand("dx", dx, dtype, shape), _operand("dresidual", dresidual, dtype, shape), _operand("dweight", dweight, f32, (cols,)),
-        _operand("dbias", dbias, f32, (cols,)))
+        _operand("dy", dy, dtype, shape, dev), _operand("s", s, dtype, shape, dev), _operand("dsum", dsum, dtype, shape, dev),
+        _operand("weight", weight, dtype, (cols,), dev), _operand("mean", mean, f32, (rows,), dev), _operand("rstd", rstd, f32, (rows,), dev),
+        _operand("dx", dx, dtype, shape, dev), _operand("dresidual", dresidual, dtype, shape, dev), _operand("dweight", dweight, f32, (cols,), dev),
+        _operand("dbias", dbias, f32, (cols,), dev))
     nbytes = load().cmoe_norm_backward_workspace_bytes(rows, cols) if dweight is not None else 0
     ws = _workspace(nbytes) if nbytes else None
     args = _NORM_BACKWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, rows, d.p, d.seed, d.offset, _NORM_BACKWARD.size, code,
                                _FORMS[form], cols)
-    _check(load().cmoe_norm_backward(args, _current_stream()), "cmoe_norm_backward")
+    _check(load().cmoe_norm_backward(args, stream), "cmoe_norm_backward")
 
 
 def _adapter_shapes(x_name: str, x, a, b):
@@ -522,35 +526,37 @@ def adapters_forward(x, y, a, b, scale, *, ids=None, base=None, dropout: Optiona
     x: [tokens, d_in]; y, base: [tokens, d_out] (y may be base itself; without a base it is 0); a: [n, rank, d_in]; b: [n, d_out, rank];
     scale: [n] fp32; ids: [tokens] int32 in any order, None: adapter 0 for every token; u: [tokens, rank] fp32 for the backward pass."""
     dtype, code, t, d_in, d_out, rank, n = _adapter_shapes("x", x, a, b)
+    dev, stream = _place("x", x)
     import torch
     d = _drop(dropout)
     operands = (
-        _operand("x", x, dtype, (t, d_in)), _operand("a", a, dtype, (n, rank, d_in)), _operand("b", b, dtype, (n, d_out, rank)),
-        _operand("scale", scale, torch.float32, (n,)), _operand("ids", ids, torch.int32, (t,)), _operand("base", base, dtype, (t, d_out)),
-        _operand("y", y, dtype, (t, d_out)), _operand("u", u, torch.float32, (t, rank)))
+        _operand("x", x, dtype, (t, d_in), dev), _operand("a", a, dtype, (n, rank, d_in), dev), _operand("b", b, dtype, (n, d_out, rank), dev),
+        _operand("scale", scale, torch.float32, (n,), dev), _operand("ids", ids, torch.int32, (t,), dev), _operand("base", base, dtype, (t, d_out), dev),
+        _operand("y", y, dtype, (t, d_out), dev), _operand("u", u, torch.float32, (t, rank), dev))
     nbytes = load().cmoe_adapters_forward_workspace_bytes(t, d_in, d_out, rank, n, code)
     ws = _workspace(nbytes) if nbytes else None
     args = _ADAPTERS_FORWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, d.p, d.seed, d.offset, _ADAPTERS_FORWARD.size, code, d_in,
                                   d_out, rank, n)
-    _check(load().cmoe_adapters_forward(args, _current_stream()), "cmoe_adapters_forward")
+    _check(load().cmoe_adapters_forward(args, stream), "cmoe_adapters_forward")
 
 
 def adapters_backward(dy, x, u, a, b, scale, *, ids=None, dx=None, dx_base=None, dropout: Optional[Dropout] = None, da=None, db=None) -> None:
     """Gradients of adapters_forward: dx = dx_base + what reaches x through the adapters; da, db: fp32, of a's and b's shapes, 0 for an
     adapter that no token has.  x is read for da, u for db.  dx may be dx_base itself."""
     dtype, code, t, d_in, d_out, rank, n = _adapter_shapes("dy", dy, a, b)
+    dev, stream = _place("dy", dy)
     import torch
     f32, d = torch.float32, _drop(dropout)
     operands = (
-        _operand("dy", dy, dtype, (t, d_out)), _operand("x", x, dtype, (t, d_in)), _operand("u", u, f32, (t, rank)),
-        _operand("a", a, dtype, (n, rank, d_in)), _operand("b", b, dtype, (n, d_out, rank)), _operand("scale", scale, f32, (n,)),
-        _operand("ids", ids, torch.int32, (t,)), _operand("dx_base", dx_base, dtype, (t, d_in)), _operand("dx", dx, dtype, (t, d_in)),
-        _operand("da", da, f32, (n, rank, d_in)), _operand("db", db, f32, (n, d_out, rank)))
+        _operand("dy", dy, dtype, (t, d_out), dev), _operand("x", x, dtype, (t, d_in), dev), _operand("u", u, f32, (t, rank), dev),
+        _operand("a", a, dtype, (n, rank, d_in), dev), _operand("b", b, dtype, (n, d_out, rank), dev), _operand("scale", scale, f32, (n,), dev),
+        _operand("ids", ids, torch.int32, (t,), dev), _operand("dx_base", dx_base, dtype, (t, d_in), dev), _operand("dx", dx, dtype, (t, d_in), dev),
+        _operand("da", da, f32, (n, rank, d_in), dev), _operand("db", db, f32, (n, d_out, rank), dev))
     nbytes = load().cmoe_adapters_backward_workspace_bytes(t, d_in, d_out, rank, n, code)
     ws = _workspace(nbytes) if nbytes else None
     args = _ADAPTERS_BACKWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, d.p, d.seed, d.offset, _ADAPTERS_BACKWARD.size, code,
                                    d_in, d_out, rank, n)
-    _check(load().cmoe_adapters_backward(args, _current_stream()), "cmoe_adapters_backward")
+    _check(load().cmoe_adapters_backward(args, stream), "cmoe_adapters_backward")
 
 
 # ---- conveniences for tests and the bench ----------------------------------------------------------
