@@ -326,6 +326,23 @@ def test_adapters_without_ids_and_in_place(B, t):
     assert torch.equal(dx, dx2) and torch.equal(grads[0], grads[1]) and torch.equal(grads[2], grads[3])
 
 
+@pytest.mark.parametrize("t", [24, 640])
+def test_an_adapter_that_has_diverged_stays_with_its_tokens(B, t):
+    """Tokens of three adapters in turn, one of which holds NaN and infinities."""
+    m = Arena(t)
+    x, a, b, scale = m.normal(t, 96), m.normal(3, 8, 96), m.normal(3, 72, 8), m.normal(3)
+    a[1, 2, 5], b[1] = float("inf"), float("nan")
+    ids = torch.arange(t, dtype=torch.int32, device="cuda") % 3
+    base, dy = m.normal(t, 72), m.normal(t, 72)
+    y, u, dx, da, db = m.out(t, 72), m.out(t, 8), m.out(t, 96), m.out(3, 8, 96), m.out(3, 72, 8)
+    B.adapters_forward(x, y, a, b, scale, ids=ids, base=base, u=u)
+    B.adapters_backward(dy, x, u, a, b, scale, ids=ids, dx=dx, da=da, db=db)
+    for name, got in (("y", y), ("u", u), ("dx", dx)):
+        assert bool(torch.isfinite(got[ids != 1]).all()) and not bool(torch.isfinite(got[ids == 1]).all()), name
+    for name, got in (("da", da), ("db", db)):
+        assert bool(torch.isfinite(got[[0, 2]]).all()) and not bool(torch.isfinite(got[1]).all()), name
+
+
 def test_adapters_without_tokens(B):
     z = dict(device="cuda")
     a, b, scale = torch.ones(2, 4, 16, **z), torch.ones(2, 24, 4, **z), torch.ones(2, **z)
