@@ -11,132 +11,13 @@
 
 #include "../../include/cmoe.h"
 #include "cmoe_internal.h"
-#include "dropout_device.h"
+#include "adapters_device.h"
 #include "operator_args.h"
 
 namespace cmoe {
 
 constexpr int MAX_RANK = 64;
-constexpr int MAX_ADAPTERS = 12287;      // a wave's counts of them fit LDS
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-// ---- operands of the matrix instructions ---------------------------------------------------------------------------
-// Eight consecutive values along the contracted axis of one row: lane l holds row l & 15, values (l >> 4) * 8 on.  A product of
-// two operands leaves column l & 15 (of the second) and rows (l >> 4) * 4 + i (of the first) in lane l.
-template <typename T> struct Frag;
-template <> struct Frag<bf16_t> { uint32_t w[4]; };
-template <> struct Frag<float> { float w[8]; };
-
-__device__ __forceinline__ void mma(f32x4& acc, const Frag<bf16_t>& rows, const Frag<bf16_t>& cols) {
-  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rows), __builtin_bit_cast(bf16x8, cols), acc, 0, 0, 0);
-}
-// (eight steps of four: both operands number the contracted axis alike, so its order is free)
-__device__ __forceinline__ void mma(f32x4& acc, const Frag<float>& rows, const Frag<float>& cols) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(rows.w[j], cols.w[j], acc, 0, 0, 0);
-}
-
-__device__ __forceinline__ Frag<bf16_t> load_frag(const bf16_t* p) {
-  return __builtin_bit_cast(Frag<bf16_t>, *reinterpret_cast<const Bytes16<bf16_t>*>(p));
-}
-__device__ __forceinline__ Frag<float> load_frag(const float* p) {
-  Frag<float> f;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const Bytes16<float> b = *reinterpret_cast<const Bytes16<float>*>(p + 4 * h);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f.w[4 * h + e] = __uint_as_float(b.w[e]);
-  }
-  return f;
-}
-// The first n values (none if n <= 0), then zeros.
-__device__ __forceinline__ Frag<bf16_t> load_frag(const bf16_t* p, int n) {
-  if (n >= 8) return load_frag(p);
-  Frag<bf16_t> f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) f.w[e] = (2 * e < n ? (uint32_t)p[2 * e] : 0u) | (2 * e + 1 < n ? (uint32_t)p[2 * e + 1] << 16 : 0u);
-  return f;
-}
-__device__ __forceinline__ Frag<float> load_frag(const float* p, int n) {
-  if (n >= 8) return load_frag(p);
-  Frag<float> f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f.w[e] = e < n ? p[e] : 0.0f;
-  return f;
-}
-
-// What dropout drops becomes 0 (its scale is applied to the products in fp32, so that bf16 values stay as they are).
-__device__ __forceinline__ void mask_frag(Frag<bf16_t>& f, const Drop& d, const uint4& words) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) f.w[e] &= (drop_keeps(d, words, 2 * e) ? 0xffffu : 0u) | (drop_keeps(d, words, 2 * e + 1) ? 0xffff0000u : 0u);
-}
-__device__ __forceinline__ void mask_frag(Frag<float>& f, const Drop& d, const uint4& words) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f.w[e] = drop_keeps(d, words, e) ? f.w[e] : 0.0f;
-}
-
-// Eight rows of eight values to eight columns.
-__device__ __forceinline__ void transpose(const Frag<bf16_t> (&rows)[8], Frag<bf16_t> (&cols)[8]) {
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int a = 0; a < 4; ++a) {
-      cols[2 * d].w[a] = __builtin_amdgcn_perm(rows[2 * a + 1].w[d], rows[2 * a].w[d], 0x05040100u);
-      cols[2 * d + 1].w[a] = __builtin_amdgcn_perm(rows[2 * a + 1].w[d], rows[2 * a].w[d], 0x07060302u);
-    }
-}
-__device__ __forceinline__ void transpose(const Frag<float> (&rows)[8], Frag<float> (&cols)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) cols[e].w[j] = rows[j].w[e];
-}
-
-// fp32 values as a sum of operands.  bf16: the upper eight bits of the significand, then those of what is left, the last term
-// rounded: two terms carry 16 bits (outputs that are themselves rounded to bf16), three all 24 (gradients of the weights, which
-// stay fp32).  What is left of an infinity would be NaN: 0.  fp32 needs one term.
-template <typename T> struct Terms { static constexpr int OUTPUT = 1, GRADIENT = 1; };
-template <> struct Terms<bf16_t> { static constexpr int OUTPUT = 2, GRADIENT = 3; };
-
-template <int N>
-__device__ __forceinline__ void split(const float (&v)[8], Frag<bf16_t> (&f)[N]) {
-  float rest[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) rest[e] = v[e];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (i < N - 1) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[i].w[e] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * e + 1]), __float_as_uint(rest[2 * e]), 0x07060302u);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float left = rest[e] - __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
-        rest[e] = left == left ? left : 0.0f;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[i].w[e] = (uint32_t)f32_to_bf16(rest[2 * e]) | ((uint32_t)f32_to_bf16(rest[2 * e + 1]) << 16);
-    }
-  }
-}
-__device__ __forceinline__ void split(const float (&v)[8], Frag<float> (&f)[1]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f[0].w[e] = v[e];
-}
-
-__device__ __forceinline__ void unpack(const Frag<bf16_t>& f, float (&v)[8]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    v[2 * e] = __uint_as_float(f.w[e] << 16);
-    v[2 * e + 1] = __uint_as_float(f.w[e] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void unpack(const Frag<float>& f, float (&v)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = f.w[e];
-}
+constexpr int MAX_ADAPTERS = 8191;       // a wave's counts of them fit LDS
 
 // The adapter of a token, or -1.
 __device__ __forceinline__ int adapter_of(const int32_t* ids, int64_t t, int n_adapters) {
@@ -155,9 +36,10 @@ struct TileArgs {
   const int32_t* ids;
   const T* base;          // or null
   T* y;
-  float* u;               // or null
+  float* u;               // [tokens, ldu] or null
   int64_t tokens;
   int d_in, d_out, rank, n_adapters;
+  int ldu;                // at least the rank: zeros from there on
   int slices;             // workgroups that share a tile, each with its part of the columns of y
   Drop drop;
 };
@@ -170,15 +52,17 @@ constexpr int SCAN_TOKENS = 512;         // a workgroup of the scanning form loo
 // up to 16 of them itself.  Weights are then read once per 16 tokens of an adapter whatever the order, as decode batches need it,
 // where every token may have another.  Otherwise 16 consecutive tokens, and one pass for each adapter among them: prompts and
 // training batches come as runs, so that most tiles have one.
+// A row or column of a product that is no token, rank or column of y reads another's values, and its results are not used: a token
+// does not see what another's adapter holds.
 // Without EXPAND: u * scale alone (v of the backward pass).
-template <typename T, int R16, bool SCAN, bool EXPAND>
+template <typename T, int R16, bool SCAN, bool EXPAND, int EDGE>
 __global__ __launch_bounds__(R16 == 4 ? 512 : 1024) void tile_kernel(TileArgs<T> g) {
   constexpr int WAVES = R16 == 4 ? 8 : 16;
   constexpr int CHUNKS = (R16 + 1) / 2;                      // operands along the rank
   constexpr int NT = Terms<T>::OUTPUT;
-  constexpr int LD = R16 * 16 + 4;
+  constexpr int LD = CHUNKS * 32 + 16 / sizeof(T);
   __shared__ float sums[WAVES][R16 * 4 * 64];
-  __shared__ float us[16][LD];
+  __shared__ __align__(16) T us[EXPAND ? NT : 1][16][LD];    // scale * u, in terms
   __shared__ int token[16], id[16], found[16], counts[2][16], n_found;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, q = lane >> 4;
   if (SCAN) {
@@ -227,154 +111,201 @@ __global__ __launch_bounds__(R16 == 4 ? 512 : 1024) void tile_kernel(TileArgs<T>
     if (first) found[__popcll(votes & ((1ull << lane) - 1))] = k;
     if (lane == 0) n_found = __popcll(votes);
   }
-  for (int i = tid; i < 16 * LD; i += WAVES * 64) (&us[0][0])[i] = 0.0f;
+  if (EXPAND && R16 == 1)                                    // (an operand is 32 values along the rank)
+    for (int i = tid; i < (int)sizeof(us) / 4; i += WAVES * 64) reinterpret_cast<uint32_t*>(us)[i] = 0;
   __syncthreads();
   const int64_t t0 = SCAN ? 0 : (int64_t)blockIdx.x * 16;
   const int64_t my_token = t0 + token[m];
   const int my_id = id[m], n_distinct = n_found;
 
-  // u: rows are tokens, columns are the rank.  A row or column that is none reads another's values, and its results are not used.
+  // u: rows are tokens, columns are the rank
   for (int f = 0; f < n_distinct; ++f) {
     const int k = found[f];
-    const T* x = g.x + my_token * g.d_in + q * 8;
-    const T* a[R16];
+    const int64_t x_at = my_token * g.d_in + q * 8;
+    int64_t a_at[R16];
 #pragma unroll
-    for (int r = 0; r < R16; ++r) a[r] = g.a + ((int64_t)k * g.rank + min(r * 16 + m, g.rank - 1)) * g.d_in + q * 8;
-    const int per_row = (g.d_in + 7) >> 3;
-    const uint64_t chunk0 = (uint64_t)my_token * per_row + q;
+    for (int r = 0; r < R16; ++r) a_at[r] = ((int64_t)k * g.rank + min(r * 16 + m, g.rank - 1)) * g.d_in + q * 8;
+    const uint64_t chunk0 = (uint64_t)my_token * ((g.d_in + 7) >> 3) + q;
     f32x4 acc[R16];
 #pragma unroll
     for (int r = 0; r < R16; ++r) acc[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int full = g.d_in / 64;
-    constexpr int DEPTH = R16 == 1 ? 4 : 2;                  // turns whose loads are in flight together
-    int s = wave;
-    for (; s + (DEPTH - 1) * WAVES < full; s += DEPTH * WAVES) {
-      Frag<T> xf[DEPTH][2], af[DEPTH][2][R16];
+    constexpr int DEPTH = R16 == 1 && sizeof(T) == 2 ? 4 : R16 == 4 || sizeof(T) == 2 ? 2 : 1;      // turns whose loads are in flight together
+    auto turns = [&](int s, auto depth) {
+      constexpr int D = decltype(depth)::value;
+      Frag<T> xf[2 * D], af[2 * D][R16];
 #pragma unroll
-      for (int i = 0; i < DEPTH; ++i)
+      for (int i = 0; i < D; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = (s + i * WAVES) * 64 + h * 32;
-          xf[i][h] = load_frag(x + at);
+          xf[2 * i + h] = load_frag(g.x + x_at + at);
 #pragma unroll
-          for (int r = 0; r < R16; ++r) af[i][h][r] = load_frag(a[r] + at);
+          for (int r = 0; r < R16; ++r) af[2 * i + h][r] = load_frag(g.a + a_at[r] + at);
         }
+      if (g.drop.limit) {
+        uint32_t kept[(D + 1) / 2];
+        kept_bits(g.drop, kept, [&](int j) { return chunk0 + (s + (j >> 1) * WAVES) * 8 + (j & 1) * 4; });
+        mask_frags(xf, kept);
+      }
 #pragma unroll
-      for (int i = 0; i < DEPTH; ++i)
+      for (int i = 0; i < 2 * D; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (g.drop.limit) mask_frag(xf[i][h], g.drop, philox_words(g.drop, chunk0 + (s + i * WAVES) * 8 + h * 4));
-#pragma unroll
-          for (int r = 0; r < R16; ++r) mma(acc[r], xf[i][h], af[i][h][r]);
-        }
-    }
-    for (; s * 64 < g.d_in; s += WAVES) {
+        for (int r = 0; r < R16; ++r) mma(acc[r], xf[i], af[i][r]);
+    };
+    int s = wave;
+    for (; s + (DEPTH - 1) * WAVES < full; s += DEPTH * WAVES) turns(s, std::integral_constant<int, DEPTH>{});
+    for (; s < full; s += WAVES) turns(s, std::integral_constant<int, 1>{});
+    if (s == full && (g.d_in & 63)) {                        // the rest of the width
+      Frag<T> xf[2], af[2][R16];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int at = s * 64 + h * 32, n = g.d_in - at - q * 8;
-        Frag<T> xf = load_frag(x + at, n);
-        if (g.drop.limit) mask_frag(xf, g.drop, philox_words(g.drop, chunk0 + s * 8 + h * 4));
+        xf[h] = load_at<EDGE>(g.x, x_at + at, n, g.tokens * g.d_in);
 #pragma unroll
-        for (int r = 0; r < R16; ++r) mma(acc[r], xf, load_frag(a[r] + at, n));
+        for (int r = 0; r < R16; ++r) {
+          af[h][r] = load_at<EDGE>(g.a, a_at[r] + at, n, (int64_t)g.n_adapters * g.rank * g.d_in);
+          keep_first(af[h][r], n);
+        }
+        keep_first(xf[h], n);
       }
+      if (g.drop.limit) {
+        uint32_t kept[1];
+        kept_bits(g.drop, kept, [&](int j) { return chunk0 + s * 8 + (j & 1) * 4; });
+        mask_frags(xf, kept);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < R16; ++r) mma(acc[r], xf[h], af[h][r]);
     }
 #pragma unroll
     for (int r = 0; r < R16; ++r)
 #pragma unroll
       for (int i = 0; i < 4; ++i) sums[wave][(r * 4 + i) * 64 + lane] = acc[r][i];
     __syncthreads();
+    const float scale = g.scale[k];
     for (int v = tid; v < R16 * 256; v += WAVES * 64) {
       const int l = v & 63, row = (l >> 4) * 4 + ((v >> 6) & 3), col = (v >> 8) * 16 + (l & 15);
       float t = sums[0][v];
 #pragma unroll
       for (int w = 1; w < WAVES; ++w) t += sums[w][v];
       if (g.drop.limit) t *= g.drop.scale;
-      if (id[row] == k && col < g.rank) us[row][col] = t;
+      if (id[row] != k) continue;
+      if (col >= g.rank) t = 0.0f;
+      if (g.u && blockIdx.y == 0 && col < g.ldu) g.u[(t0 + token[row]) * g.ldu + col] = EXPAND ? t : t * scale;
+      if (EXPAND) {
+        t *= scale;
+        if constexpr (sizeof(T) == 2) {
+          const uint32_t hi = __float_as_uint(t) & 0xffff0000u;
+          const float left = t - __uint_as_float(hi);
+          us[0][row][col] = (T)(hi >> 16);
+          us[1][row][col] = left == left ? f32_to_bf16(left) : (T)0;
+        } else {
+          us[0][row][col] = t;
+        }
+      }
     }
     __syncthreads();
   }
-
   if (g.u && blockIdx.y == 0)
-    for (int v = tid; v < 16 * g.rank; v += WAVES * 64) {
-      const int row = v / g.rank, col = v % g.rank;
-      if (id[row] > -2) g.u[(t0 + token[row]) * g.rank + col] = EXPAND ? us[row][col] : (id[row] >= 0 ? us[row][col] * g.scale[id[row]] : 0.0f);
-    }
+    for (int v = tid; v < 16 * g.ldu; v += WAVES * 64)
+      if (id[v / g.ldu] == -1) g.u[(t0 + token[v / g.ldu]) * g.ldu + v % g.ldu] = 0.0f;
   if (!EXPAND) return;
 
-  // y: rows are 16 columns of y, columns are tokens.  Two products' rows are dealt so that a lane ends with eight consecutive
-  // columns of its token.  The contracted axis is the rank in chunks of eight; the last chunk of a rank that is no multiple
-  // of eight reaches back, with zeros in u where it overlaps.
+  // y: rows are 16 columns of y, columns are tokens, the contracted axis the rank.  Two products' rows are dealt so that a lane ends
+  // with eight consecutive columns of its token.
   const int units = (g.d_out + 31) >> 5;
   const int first = (int)((int64_t)units * blockIdx.y / g.slices), last = (int)((int64_t)units * (blockIdx.y + 1) / g.slices);
-  const int chunks = (g.rank + 7) >> 3;
-  Frag<T> uf[CHUNKS][NT];
-  int have = -1;
-  for (int unit = first + wave; unit < last; unit += WAVES) {
-    const int o0 = unit * 32;
-    const int64_t at = my_token * g.d_out + o0 + q * 8;
-    const int n = g.d_out - o0 - q * 8;
-    float v[8] = {};
-    if (g.base && n > 0) load8(g.base + at, n, v);
+  const int64_t y_size = g.tokens * g.d_out, b_size = (int64_t)g.n_adapters * g.d_out * g.rank;
+  const int64_t y_at = my_token * g.d_out + q * 8;
+  auto expand = [&](int unit, auto depth) {                  // `depth` units, WAVES apart
+    constexpr int D = decltype(depth)::value;
+    Frag<T> basef[D];
+    float v[D][8];
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      const int o0 = (unit + i * WAVES) * 32;
+      if (g.base) basef[i] = load_at<EDGE>(g.base, y_at + o0, g.d_out - o0 - q * 8, y_size);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+    }
     for (int f = 0; f < n_distinct; ++f) {
       const int k = found[f];
-      f32x4 acc[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
-      Frag<T> bf[2][CHUNKS];
+      Frag<T> bf[D][2][CHUNKS];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int o = min(o0 + (m >> 2) * 8 + e * 4 + (m & 3), g.d_out - 1);
-        const T* row = g.b + ((int64_t)k * g.d_out + o) * g.rank;
+      for (int i = 0; i < D; ++i)
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
-          bf[e][c] = g.rank >= 8 ? load_frag(row + min((c * 4 + q) * 8, g.rank - 8)) : load_frag(row, c * 4 + q == 0 ? g.rank : 0);
-      }
-      if (have != f) {
-        have = f;
-        const float scale = g.scale[k];
+        for (int e = 0; e < 2; ++e) {
+          const int o = min((unit + i * WAVES) * 32 + (m >> 2) * 8 + e * 4 + (m & 3), g.d_out - 1);
+          const int64_t row = ((int64_t)k * g.d_out + o) * g.rank;
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-          const int chunk = c * 4 + q, from = max(min(chunk * 8, g.rank - 8), 0);
-          float t[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) t[j] = chunk < chunks && from + j >= chunk * 8 && my_id == k ? us[m][from + j] * scale : 0.0f;
-          split(t, uf[c]);
+          for (int c = 0; c < CHUNKS; ++c) bf[i][e][c] = load_at<EDGE>(g.b, row + (c * 4 + q) * 8, g.rank - (c * 4 + q) * 8, b_size);
         }
-      }
+      Frag<T> uf[CHUNKS][NT];
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-        for (int p = 0; p < NT; ++p)
+        for (int p = 0; p < NT; ++p) uf[c][p] = *reinterpret_cast<const Frag<T>*>(&us[p][m][(c * 4 + q) * 8]);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) mma(acc[e], bf[e][c], uf[c][p]);
-      // (added by choice, not as a product with 0: a token does not see what another's adapter holds)
+      for (int i = 0; i < D; ++i) {
+        f32x4 acc[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += my_id == k ? acc[e >> 2][e & 3] : 0.0f;
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            if (EDGE == WHOLE) keep_first(bf[i][e][c], g.rank - (c * 4 + q) * 8);
+#pragma unroll
+            for (int p = 0; p < NT; ++p) mma(acc[e], bf[i][e][c], uf[c][p]);
+          }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] += my_id == k ? acc[e >> 2][e & 3] : 0.0f;
+      }
     }
-    if (my_id == -2 || n <= 0) continue;
-    store8(g.y + at, n, v);
-  }
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      const int o0 = (unit + i * WAVES) * 32, n = g.d_out - o0 - q * 8;
+      if (my_id == -2) continue;
+      if (g.base) {
+        float o[8];
+        unpack(basef[i], o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] += o[e];
+      }
+      store_at<EDGE>(g.y + y_at + o0, n, v[i]);
+    }
+  };
+  constexpr int DEPTH = 4 / (R16 == 4 ? 2 : 1) / (sizeof(T) / 2);
+  int unit = first + wave;
+  for (; unit + (DEPTH - 1) * WAVES < last; unit += DEPTH * WAVES) expand(unit, std::integral_constant<int, DEPTH>{});
+  for (; unit < last; unit += WAVES) expand(unit, std::integral_constant<int, 1>{});
 }
 
 // ---- backward: order of the tokens, b transposed -------------------------------------------------------------------
 
+constexpr int HELD = 8;                  // ids that a thread of the ordering workgroup keeps between its two looks at them
+
 // order: the tokens by adapter, in their order within one, those without an adapter last; start[k]: adapter k's first place, start[n]:
 // that of the tokens without one, start[n + 1] = tokens.  One workgroup; each wave counts and places a range of tokens of its own.
-__global__ __launch_bounds__(1024) void order_kernel(const int32_t* ids, int tokens, int n_adapters, int32_t* order, int32_t* start) {
-  extern __shared__ int32_t cursor[];                        // [wave][n + 1]
-  __shared__ int32_t totals[1024], carry;
-  const int n_waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, bins = n_adapters + 1;
-  for (int i = threadIdx.x; i < n_waves * bins; i += blockDim.x) cursor[i] = 0;
+__device__ void order_tokens(const int32_t* ids, int tokens, int n_adapters, int n_waves, int32_t* order, int32_t* start, int32_t* cursor) {
+  __shared__ int32_t totals[16], carry;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, bins = n_adapters + 1;
+  for (int i = threadIdx.x; i < n_waves * bins; i += 1024) cursor[i] = 0;
   if (threadIdx.x == 0) carry = 0;
-  __syncthreads();
   const int per = (((tokens + n_waves - 1) / n_waves) + 63) & ~63;
-  const int first = min(wave * per, tokens), last = min(first + per, tokens);
+  const int first = wave < n_waves ? min(wave * per, tokens) : tokens, last = min(first + per, tokens);
   volatile int32_t* mine = cursor + wave * bins;             // (written by one lane, read by others of its wave)
   auto bin_of = [&](int t) {
+    if (t >= last) return -1;
     const int k = adapter_of(ids, t, n_adapters);
     return k < 0 ? n_adapters : k;
   };
+  int held[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) held[i] = bin_of(first + i * 64 + lane);
+  __syncthreads();
   // f(place among the wave's lanes with this bin, how many, bin) once per lane that holds a token
-  auto by_bin = [&](int t, auto f) {
-    const int bin = t < last ? bin_of(t) : -1;
+  auto by_bin = [&](int bin, auto f) {
     uint64_t left = __ballot(bin >= 0);
     while (left) {
       const int b = __builtin_amdgcn_readlane(bin, __ffsll((unsigned long long)left) - 1);
@@ -383,12 +314,19 @@ __global__ __launch_bounds__(1024) void order_kernel(const int32_t* ids, int tok
       left &= ~same;
     }
   };
-  for (int t = first + lane; t - lane < last; t += 64)
-    by_bin(t, [&](int place, int n, int b) {
+  auto all = [&](auto f) {                                   // f(token, bin) of every 64 tokens of the wave, in order
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (first + i * 64 < last) f(first + i * 64 + lane, held[i]);
+    for (int t = first + HELD * 64; t < last; t += 64) f(t + lane, bin_of(t + lane));
+  };
+  all([&](int, int bin) {
+    by_bin(bin, [&](int place, int n, int b) {
       if (place == 0) mine[b] = mine[b] + n;
     });
+  });
   __syncthreads();
-  for (int b0 = 0; b0 < bins; b0 += blockDim.x) {
+  for (int b0 = 0; b0 < bins; b0 += 1024) {
     const int b = b0 + threadIdx.x;
     int total = 0;
     if (b < bins)
@@ -399,7 +337,7 @@ __global__ __launch_bounds__(1024) void order_kernel(const int32_t* ids, int tok
     int at = carry + upto - total;
     for (int w = 0; w < wave; ++w) at += totals[w];
     __syncthreads();
-    if (threadIdx.x == blockDim.x - 1) carry = at + total;
+    if (threadIdx.x == 1023) carry = at + total;
     if (b < bins) {
       start[b] = at;
       for (int w = 0; w < n_waves; ++w) {
@@ -411,225 +349,281 @@ __global__ __launch_bounds__(1024) void order_kernel(const int32_t* ids, int tok
     __syncthreads();
   }
   if (threadIdx.x == 0) start[bins] = tokens;
-  for (int t = first + lane; t - lane < last; t += 64)
-    by_bin(t, [&](int place, int n, int b) {
+  all([&](int t, int bin) {
+    by_bin(bin, [&](int place, int n, int b) {
       const int at = mine[b];
       order[at + place] = t;
       if (place == 0) mine[b] = at + n;
     });
+  });
 }
 
-// bt[k][j][o] = b[k][o][j]: 64 columns o of one adapter per workgroup, through LDS.
+// The first workgroup orders the tokens; the next ones transpose b, bt[k][j][o] = b[k][o][j], 64 columns o of one adapter each through
+// LDS; the others leave dropout's mask, a byte per chunk.  (The order is a chain of latencies, so the rest is done beside it.)
 template <typename T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* b, T* bt, int d_out, int rank) {
-  __shared__ T tile[MAX_RANK][64 + 2];
-  const int k = blockIdx.y, o0 = blockIdx.x * 64, n = min(64, d_out - o0);
+__global__ __launch_bounds__(1024) void arrange_kernel(const int32_t* ids, int tokens, int n_adapters, int n_waves, int32_t* order, int32_t* start, const T* b,
+                                                       T* bt, int d_out, int rank, int transposes, Drop drop, uint8_t* kept, int64_t chunks) {
+  extern __shared__ int32_t cursor[];                        // [wave][n + 1]
+  __shared__ T tile[MAX_RANK][64 + 4 / sizeof(T)];
+  if (blockIdx.x == 0) {
+    order_tokens(ids, tokens, n_adapters, n_waves, order, start, cursor);
+    return;
+  }
+  if ((int)blockIdx.x > transposes) {
+    const int64_t step = (int64_t)(gridDim.x - 1 - transposes) * 1024;
+    for (int64_t c = (int64_t)(blockIdx.x - 1 - transposes) * 1024 + threadIdx.x; c < chunks; c += step) {
+      const uint4 words = philox_words(drop, c);
+      uint32_t bits = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bits |= drop_keeps(drop, words, e) ? 1u << e : 0u;
+      kept[c] = (uint8_t)bits;
+    }
+    return;
+  }
+  const int per = (d_out + 63) / 64;
+  const int k = (blockIdx.x - 1) / per, o0 = (blockIdx.x - 1) % per * 64, n = min(64, d_out - o0);
   const T* from = b + ((int64_t)k * d_out + o0) * rank;
-  for (int i = threadIdx.x; i < n * rank; i += 256) tile[i % rank][i / rank] = from[i];
+  for (int i = threadIdx.x; i < n * rank; i += 1024) tile[i % rank][i / rank] = from[i];
   __syncthreads();
-  for (int i = threadIdx.x; i < rank * 64; i += 256)
+  for (int i = threadIdx.x; i < rank * 64; i += 1024)
     if ((i & 63) < n) bt[((int64_t)k * rank + (i >> 6)) * d_out + o0 + (i & 63)] = tile[i >> 6][i & 63];
 }
 
 // ---- backward: dx and the gradients of the weights -----------------------------------------------------------------
 
-template <typename T>
-struct OuterArgs {
-  const T* x;             // [tokens, d]: x for da and dx, dy for db
-  const float* v;         // [tokens, rank]: v, or u
-  const T* a;             // dx: [n][rank][d]
-  const T* base;          // dx_base or null
-  T* dx;
-  float* partials;        // [slot][rank][d]
-  const int32_t* order;
-  const int32_t* start;
-  int tokens, d, rank, n_adapters;
-  int chunk;              // places of the order per workgroup
-  Drop drop;
+// Dropout of a batch as the arranging launch leaves it, a bit per element: both dx and da need the mask, and ten rounds of the generator
+// twice would be 15 of the 25 us that their memory traffic takes (4096 tokens, 4096 wide).
+struct Mask {
+  const uint8_t* kept;    // [tokens][ceil(d / 8)], or null
+  float scale;
 };
 
-// A workgroup has 128 columns and a chunk of the places in the order of adapters; its four waves take turns of 32 tokens.  A lane reads
-// eight columns of eight tokens and turns them in its registers into eight operands whose contracted axis is the tokens: operand e's
-// row m is column 8 m + e.  So nothing goes through LDS, every load and store is 16 bytes of a row, and the columns that a lane reads
-// of a token are those that it writes of dx: one evaluation of the mask serves both.  The sums over tokens of an adapter within the
-// chunk go to a slot of their own (slots are numbered chunk + adapter: of two slots in the order one number differs), and
-// are added in the order of chunks by the kernel below.
-template <typename T, int R16, bool DX, bool GRAD>
-__global__ __launch_bounds__(256) void outer_kernel(OuterArgs<T> g) {
-  constexpr int CHUNKS = (R16 + 1) / 2;
-  constexpr int NT = Terms<T>::OUTPUT, NG = Terms<T>::GRADIENT;
-  __shared__ float sums[GRAD ? 3 * 64 * 32 : 1];
+template <typename T>
+struct GradArgs {         // da from x and v, db from dy and u
+  const T* x;             // [tokens, d]
+  const float* v;         // [tokens, ldv]
+  float* slots;           // [slot][rank][d]
+  int d, ldv;
+  Mask mask;
+};
+
+template <typename T>
+struct DxArgs {
+  const float* v;         // [tokens, ldv], ldv a multiple of eight with zeros past the rank
+  const T* a;             // [n][rank][d]
+  const T* base;          // or null
+  T* dx;
+  int d, ldv;
+  Mask mask;
+};
+
+struct OrderArgs {
+  const int32_t* ids;
+  const int32_t* order;
+  const int32_t* start;
+  int64_t tokens;
+  int rank, n_adapters;
+  int chunk;              // places of the order per workgroup, CHUNK_MAX at most
+};
+
+constexpr int CHUNK_MAX = 512;
+
+// A workgroup of these two has 128 columns and a chunk of the places in the order of adapters, and takes it adapter by adapter, its four
+// waves in turns of 32 places.  A lane holds eight columns, m * 8 on, of eight tokens, those of places q * 4 + 0..3 and
+// 16 + q * 4 + 0..3; so every load and store is 16 bytes of a row, and one evaluation of the generator is one lane's chunk.
+struct Places {
+  const int32_t* token;   // LDS
+  int first, last;        // of the chunk
+};
+
+// Sums over tokens: the lane turns its eight rows in registers into eight operands whose contracted axis is the tokens (operand e's row m
+// is column 8 m + e), so nothing goes through LDS.  An adapter's sums within the chunk go to a slot of their own (numbered chunk +
+// adapter: of two neighbours in the order one number is larger), and are added in the order of chunks by the kernel below.
+template <typename T, int R16, int EDGE>
+__device__ __forceinline__ void grad_segment(const GradArgs<T>& g, const OrderArgs& w, const Places& at, int slab, int k, int p0, int p1, float* sums) {
+  constexpr int NG = Terms<T>::GRADIENT;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
-  const int c0 = blockIdx.x * 128 + m * 8;                   // the lane's columns
-  const int n = g.d - c0;
-  const int per_row = (g.d + 7) >> 3;
-  const int chunk0 = blockIdx.y * g.chunk, chunk1 = min(chunk0 + g.chunk, g.tokens);
-  const int chunks = (g.rank + 7) >> 3;
-  // the adapter of the chunk's first place: the last one that starts at or before it (empty ones start where the next does)
-  int k = 0;
-  {
-    int hi = g.n_adapters;                                   // start[n_adapters]: tokens without an adapter
-    while (k < hi) {
-      const int mid = (k + hi + 1) >> 1;
-      if (g.start[mid] <= chunk0) k = mid;
-      else hi = mid - 1;
+  const int c0 = slab * 128 + m * 8, n = g.d - c0, per_row = (g.d + 7) >> 3;
+  f32x4 acc[R16][8];
+#pragma unroll
+  for (int r = 0; r < R16; ++r)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[r][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+  for (int p = p0 + wave * 32; p < p1; p += 128) {
+    auto place = [&](int j) { return p + (j >> 2) * 16 + q * 4 + (j & 3); };
+    Frag<T> rows[8];
+    uint32_t kept[8];
+    float f[R16][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {                            // (past the end: the last one's values, with 0 in v)
+      const int64_t t = at.token[min(place(j), p1 - 1) - at.first];
+      rows[j] = load_at<EDGE>(g.x, t * g.d + c0, n, w.tokens * g.d);
+      if (g.mask.kept) kept[j] = g.mask.kept[t * per_row + min(c0 >> 3, per_row - 1)];
+#pragma unroll
+      for (int r = 0; r < R16; ++r) f[r][j] = g.v[t * g.ldv + min(r * 16 + m, w.rank - 1)];
+    }
+    if (g.mask.kept) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mask_frag<0>(rows[j], kept[j]);
+    }
+    Frag<T> cols[8];
+    transpose(rows, cols);
+#pragma unroll
+    for (int r = 0; r < R16; ++r) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[r][j] = place(j) < p1 ? f[r][j] : 0.0f;
+      Frag<T> vf[NG];
+      split(f[r], vf);
+#pragma unroll
+      for (int i = 0; i < NG; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mma(acc[r][e], cols[e], vf[i]);
     }
   }
-  for (int p0 = chunk0; p0 < chunk1; ++k) {
-    const int p1 = min(g.start[k + 1], chunk1);
-    if (p1 <= p0) continue;
-    const bool none = k == g.n_adapters;
-    if (none && !DX) return;
-    f32x4 acc[GRAD ? R16 : 1][8];
-    Frag<T> af[DX ? CHUNKS : 1][8];
-    if (GRAD) {
+  float* slot = g.slots + (int64_t)(blockIdx.y + k) * w.rank * g.d;
 #pragma unroll
-      for (int r = 0; r < R16; ++r)
+  for (int r = 0; r < R16; ++r) {
+    __syncthreads();
+    if (wave > 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[r][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[((wave - 1) * 32 + e * 4 + i) * 64 + lane] = acc[r][e][i];
     }
-    if (DX && !none) {
+    __syncthreads();
+    if (wave == 0 && r * 16 + m < w.rank) {
+      // the lane's rank is r * 16 + m; its columns q * 32 + i * 8 + e
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          o[e] = acc[r][e][i] + sums[(e * 4 + i) * 64 + lane] + sums[(32 + e * 4 + i) * 64 + lane] + sums[(64 + e * 4 + i) * 64 + lane];
+          if (g.mask.kept) o[e] *= g.mask.scale;
+        }
+        const int c = slab * 128 + q * 32 + i * 8;
+        store_at<EDGE>(slot + (int64_t)(r * 16 + m) * g.d + c, g.d - c, o);
+      }
+    }
+  }
+}
+
+// dx: rows are tokens, columns those of dx, dealt so that a lane ends with eight consecutive ones; a's rows are turned in registers.
+template <typename T, int R16, int EDGE>
+__device__ __forceinline__ void dx_segment(const DxArgs<T>& g, const OrderArgs& w, const Places& at, int slab, int k, int p0, int p1) {
+  constexpr int CHUNKS = (R16 + 1) / 2, NT = Terms<T>::OUTPUT;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
+  const int c0 = slab * 128 + m * 8, n = g.d - c0, per_row = (g.d + 7) >> 3;
+  const bool none = k == w.n_adapters;                       // dx = base
+  Frag<T> af[CHUNKS][8];
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) {
+    Frag<T> rows[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int r = (c * 4 + q) * 8 + j;
+      rows[j] = load_at<EDGE>(g.a, ((int64_t)(none ? 0 : k) * w.rank + min(r, w.rank - 1)) * g.d + c0, n, (int64_t)w.n_adapters * w.rank * g.d);
+      keep_first(rows[j], r < w.rank ? 8 : 0);
+    }
+    transpose(rows, af[c]);
+  }
+#pragma unroll 1
+  for (int p = p0 + wave * 32; p < p1; p += 128) {
+    auto place = [&](int j) { return p + (j >> 2) * 16 + q * 4 + (j & 3); };
+    Frag<T> base[8];
+    float h[2][CHUNKS][8];
+    if (g.base) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) base[j] = load_at<EDGE>(g.base, (int64_t)at.token[min(place(j), p1 - 1) - at.first] * g.d + c0, n, w.tokens * g.d);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c)
+        load8(g.v + (int64_t)at.token[min(p + s * 16 + m, p1 - 1) - at.first] * g.ldv + min((c * 4 + q) * 8, g.ldv - 8), 8, h[s][c]);
+    uint32_t kept[8];
+    if (g.mask.kept) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) kept[j] = g.mask.kept[(int64_t)at.token[min(place(j), p1 - 1) - at.first] * per_row + min(c0 >> 3, per_row - 1)];
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      f32x4 out[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) {
-        Frag<T> rows[8];
+        Frag<T> vf[NT];
+        split(h[s][c], vf);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int r = (c * 4 + q) * 8 + j;
-          rows[j] = load_frag(g.a + ((int64_t)k * g.rank + min(r, g.rank - 1)) * g.d + c0, r < g.rank ? n : 0);
-        }
-        transpose(rows, af[c]);
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) mma(out[e], vf[i], af[c][e]);
       }
-    }
-    for (int p = p0 + wave * 32; p < p1; p += 128) {
-      int64_t t[8];                                          // places q * 4 + 0..3 and 16 + q * 4 + 0..3; a place past the end: none
-      bool valid[8];
-      Frag<T> rows[8], base[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int at = p + (j >> 2) * 16 + q * 4 + (j & 3);
-        valid[j] = at < p1;
-        t[j] = g.order[min(at, p1 - 1)];
-      }
-      if (GRAD || DX) {
+      for (int i = 0; i < 4; ++i) {
+        const int j = s * 4 + i;
+        if (place(j) >= p1) continue;
+        float o[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (GRAD) rows[j] = load_frag(g.x + t[j] * g.d + c0, valid[j] && !none ? n : 0);
-          if (DX) base[j] = load_frag((g.base ? g.base : g.a) + (g.base ? t[j] * g.d + c0 : 0), g.base && valid[j] ? n : 0);
+        for (int e = 0; e < 8; ++e) {
+          o[e] = none ? 0.0f : out[e][i];
+          if (g.mask.kept) o[e] = __uint_as_float(__float_as_uint(o[e] * g.mask.scale) & (uint32_t)__builtin_amdgcn_sbfe(kept[j], e, 1));
         }
-      }
-      uint4 words[8];
-      if (g.drop.limit) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          words[j] = philox_words(g.drop, (uint64_t)t[j] * per_row + (c0 >> 3));
-          if (GRAD) mask_frag(rows[j], g.drop, words[j]);
-        }
-      }
-      if (GRAD && !none) {
-        Frag<T> cols[8];
-        transpose(rows, cols);
-#pragma unroll
-        for (int r = 0; r < R16; ++r) {
-          float f[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = valid[j] && r * 16 + m < g.rank ? g.v[t[j] * g.rank + r * 16 + m] : 0.0f;
-          Frag<T> vf[NG];
-          split(f, vf);
-#pragma unroll
-          for (int i = 0; i < NG; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) mma(acc[r][e], cols[e], vf[i]);
-        }
-      }
-      if (DX) {
-        f32x4 out[2][8];
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) out[s][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (!none) {
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const int at = p + s * 16 + m;
-            const int64_t row = (int64_t)g.order[min(at, p1 - 1)] * g.rank;
-#pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-              float f[8];
-              Frag<T> vf[NT];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const int r = (c * 4 + q) * 8 + j;
-                f[j] = r < g.rank ? g.v[row + r] : 0.0f;
-              }
-              split(f, vf);
-#pragma unroll
-              for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) mma(out[s][e], vf[i], af[c][e]);
-            }
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (!valid[j] || n <= 0) continue;
-          float o[8], b[8];
+        if (g.base) {
+          float b[8];
           unpack(base[j], b);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float d = out[j >> 2][e][j & 3];
-            if (g.drop.limit) d = drop_keeps(g.drop, words[j], e) ? d * g.drop.scale : 0.0f;
-            o[e] = none ? b[e] : b[e] + d;
-          }
-          store8(g.dx + t[j] * g.d + c0, n, o);
+          for (int e = 0; e < 8; ++e) o[e] += b[e];
         }
+        store_at<EDGE>(g.dx + (int64_t)at.token[place(j) - at.first] * g.d + c0, n, o);
       }
     }
-    if (GRAD && !none) {
-      float* slot = g.partials + (int64_t)(blockIdx.y + k) * g.rank * g.d;
-#pragma unroll
-      for (int r = 0; r < R16; ++r) {
-        __syncthreads();
-        if (wave > 0) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[((wave - 1) * 32 + e * 4 + i) * 64 + lane] = acc[r][e][i];
-        }
-        __syncthreads();
-        if (wave == 0 && r * 16 + m < g.rank) {
-          // the lane's rank is r * 16 + m; its columns q * 32 + i * 8 + e
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float o[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              o[e] = acc[r][e][i] + sums[(e * 4 + i) * 64 + lane] + sums[(32 + e * 4 + i) * 64 + lane] + sums[(64 + e * 4 + i) * 64 + lane];
-              if (g.drop.limit) o[e] *= g.drop.scale;
-            }
-            const int c = blockIdx.x * 128 + q * 32 + i * 8;
-            if (c < g.d) store8(slot + (int64_t)(r * 16 + m) * g.d + c, g.d - c, o);
-          }
-        }
-      }
+  }
+}
+
+// Slabs of dx, then of da, then of db.
+template <typename T, int R16, int EDGE>
+__global__ __launch_bounds__(256) void outer_kernel(DxArgs<T> dx, GradArgs<T> da, GradArgs<T> db, OrderArgs w, int slabs_dx, int slabs_da) {
+  __shared__ float sums[3 * 64 * 32];
+  __shared__ int32_t token[CHUNK_MAX];
+  const Places at{token, (int)blockIdx.y * w.chunk, (int)min((int64_t)(blockIdx.y + 1) * w.chunk, w.tokens)};
+  for (int i = threadIdx.x; i < at.last - at.first; i += 256) token[i] = w.order[at.first + i];
+  __syncthreads();
+  const int slab = blockIdx.x;
+  for (int p0 = at.first; p0 < at.last;) {
+    const int id = adapter_of(w.ids, token[p0 - at.first], w.n_adapters), k = id < 0 ? w.n_adapters : id;
+    const int p1 = min(w.start[k + 1], at.last);
+    if (slab < slabs_dx) dx_segment<T, R16, EDGE>(dx, w, at, slab, k, p0, p1);
+    else if (k < w.n_adapters) {
+      const bool first = slab < slabs_dx + slabs_da;
+      grad_segment<T, R16, EDGE>(first ? da : db, w, at, slab - slabs_dx - (first ? 0 : slabs_da), k, p0, p1, sums);
     }
     p0 = p1;
   }
 }
 
-// out = the slots of an adapter added in the order of chunks (0 without one), times the adapter's scale if there is one.
-// TRANSPOSED: out is [n][d][rank].
-__global__ __launch_bounds__(256) void sum_slots_kernel(const float* partials, const int32_t* start, const float* scale, float* out, int d, int rank, int chunk,
-                                                        int transposed) {
+// The slots of an adapter added in the order of chunks (0 without one): da, and db, [n][d_out][rank], times the adapter's scale.
+__global__ __launch_bounds__(256) void sum_slots_kernel(const float* da_slots, const float* db_slots, const int32_t* start, const float* scale, float* da, float* db,
+                                                        int d_in, int d_out, int rank, int chunk, int blocks_in) {
   const int k = blockIdx.y;
-  const int64_t size = (int64_t)rank * d, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const bool first = (int)blockIdx.x < blocks_in;
+  const int d = first ? d_in : d_out;
+  const float* slots = first ? da_slots : db_slots;
+  const int64_t size = (int64_t)rank * d, i = (int64_t)(blockIdx.x - (first ? 0 : blocks_in)) * 256 + threadIdx.x;
   if (i >= size) return;
   const int p0 = start[k], p1 = start[k + 1];
   float t = 0.0f;
   if (p1 > p0) {
-    for (int c = p0 / chunk; c <= (p1 - 1) / chunk; ++c) t += partials[(int64_t)(c + k) * size + i];
-    if (scale) t *= scale[k];
+    const int c0 = p0 / chunk, c1 = (p1 - 1) / chunk;
+    const float* from = slots + (int64_t)(c0 + k) * size + i;
+#pragma unroll 8
+    for (int c = c0; c <= c1; ++c, from += size) t += *from;
+    if (!first) t *= scale[k];
   }
-  out[k * size + (transposed ? (i % d) * rank + i / d : i)] = t;
+  if (first) da[k * size + i] = t;
+  else db[k * size + (i % d) * rank + i / d] = t;
 }
 
 // f(R16) with the rank in blocks of 16 as a compile-time constant
@@ -640,41 +634,57 @@ static void with_rank(int rank, F&& f) {
   else f(std::integral_constant<int, 4>{});
 }
 
+// f(R16, EDGE): ... and how rows end (adapters_device.h).  A width or buffer below eight values is nothing to be fast at: one form.
+template <typename F>
+static void with_shape(int rank, bool whole, bool tiny, F&& f) {
+  if (tiny) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, TINY>{});
+  with_rank(rank, [&](auto r) {
+    if (whole) f(r, std::integral_constant<int, WHOLE>{});
+    else f(r, std::integral_constant<int, RAGGED>{});
+  });
+}
+
 template <typename T, bool EXPAND>
 static void launch_tiles(TileArgs<T> g, hipStream_t s) {
   const int units = EXPAND ? (g.d_out + 31) / 32 : 1;
   const bool scan = g.tokens <= SCAN_TOKENS;
   const int64_t tiles = scan ? g.tokens : (g.tokens + 15) / 16;
   g.slices = EXPAND ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (units + 15) / 16)) : 1;
-  with_rank(g.rank, [&](auto r) {
-    constexpr int R = decltype(r)::value;
+  const bool whole = g.d_in % 8 == 0 && (!EXPAND || (g.d_out % 8 == 0 && g.rank % 8 == 0));
+  const bool tiny = g.d_in < 8 || (EXPAND && std::min(g.tokens * g.d_out, (int64_t)g.n_adapters * g.d_out * g.rank) < 8);
+  with_shape(g.rank, whole, tiny, [&](auto r, auto edge) {
+    constexpr int R = decltype(r)::value, E = decltype(edge)::value;
     const dim3 grid((unsigned)tiles, g.slices), block(R == 4 ? 512 : 1024);
-    if (scan) hipLaunchKernelGGL((tile_kernel<T, R, true, EXPAND>), grid, block, 0, s, g);
-    else hipLaunchKernelGGL((tile_kernel<T, R, false, EXPAND>), grid, block, 0, s, g);
+    if (scan) hipLaunchKernelGGL((tile_kernel<T, R, true, EXPAND, E>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((tile_kernel<T, R, false, EXPAND, E>), grid, block, 0, s, g);
   });
 }
 
 template <typename T>
 static void launch_adapters_forward(const cmoe_adapters_forward_args& p, const Drop& drop, hipStream_t s) {
   launch_tiles<T, true>(TileArgs<T>{(const T*)p.x, (const T*)p.a, (const T*)p.b, p.scale, p.ids, (const T*)p.base, (T*)p.y, p.u, p.tokens, p.d_in, p.d_out,
-                                    p.rank, p.n_adapters, 1, drop}, s);
+                                    p.rank, p.n_adapters, p.rank, 1, drop}, s);
 }
 
 // Workspace of the backward pass: order and starts, v, b transposed, slots of da's and db's partial sums.
 struct BackwardLayout {
-  int chunk, chunks;
-  size_t order, start, v, bt, da, db, total;
+  int chunk, chunks, ldv;
+  size_t order, start, v, bt, kept, da, db, total;
 };
 static BackwardLayout backward_layout(int64_t tokens, int d_in, int d_out, int rank, int n_adapters, int dtype) {
   BackwardLayout l{};
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) & ~(size_t)255; return o; };
-  l.chunk = 256;
+  // Long chunks leave fewer partial sums, short ones more workgroups: about 1024 of them, of one to four turns per wave.
+  const int64_t slabs = 2 * ((d_in + 127) / 128) + (d_out + 127) / 128;
+  for (l.chunk = 128; l.chunk < CHUNK_MAX && tokens * slabs > 1024 * 2 * l.chunk;) l.chunk *= 2;
+  l.ldv = (rank + 7) & ~7;
   l.chunks = (int)((tokens + l.chunk - 1) / l.chunk);
   l.order = take(sizeof(int32_t) * tokens);
   l.start = take(sizeof(int32_t) * (n_adapters + 2));
-  l.v = take(sizeof(float) * tokens * rank);
+  l.v = take(sizeof(float) * tokens * l.ldv);
   l.bt = take(elem_size(dtype) * n_adapters * rank * d_out);
+  l.kept = take(tokens * ((d_in + 7) / 8));
   l.da = take(sizeof(float) * (l.chunks + n_adapters) * rank * d_in);
   l.db = take(sizeof(float) * (l.chunks + n_adapters) * rank * d_out);
   l.total = off;
@@ -688,32 +698,33 @@ static void launch_adapters_backward(const cmoe_adapters_backward_args& p, const
   int32_t *order = (int32_t*)(ws + l.order), *start = (int32_t*)(ws + l.start);
   float *v = (float*)(ws + l.v), *da = (float*)(ws + l.da), *db = (float*)(ws + l.db);
   T* bt = (T*)(ws + l.bt);
+  const bool needs_v = p.tokens > 0 && (p.dx || p.da);
   const int n_waves = std::min(16, (MAX_ADAPTERS + 1) / (p.n_adapters + 1));
-  hipLaunchKernelGGL(order_kernel, dim3(1), dim3(64 * n_waves), sizeof(int32_t) * n_waves * (p.n_adapters + 1), s, p.ids, (int)p.tokens, p.n_adapters, order, start);
-  if (p.tokens > 0 && (p.dx || p.da)) {
-    hipLaunchKernelGGL(transpose_kernel<T>, dim3((p.d_out + 63) / 64, p.n_adapters), dim3(256), 0, s, (const T*)p.b, bt, p.d_out, p.rank);
-    launch_tiles<T, false>(TileArgs<T>{(const T*)p.dy, bt, nullptr, p.scale, p.ids, nullptr, nullptr, v, p.tokens, p.d_out, 0, p.rank, p.n_adapters, 1, Drop{}}, s);
+  const int transposes = needs_v ? (p.d_out + 63) / 64 * p.n_adapters : 0;
+  const int64_t chunks = needs_v && drop.limit ? p.tokens * ((p.d_in + 7) / 8) : 0;
+  const int masks = (int)std::min<int64_t>((chunks + 1023) / 1024, 1024);
+  uint8_t* kept = (uint8_t*)(ws + l.kept);
+  const Mask mask{chunks > 0 ? kept : nullptr, drop.scale};
+  hipLaunchKernelGGL(arrange_kernel<T>, dim3(1 + transposes + masks), dim3(1024), sizeof(int32_t) * n_waves * (p.n_adapters + 1), s, p.ids, (int)p.tokens,
+                     p.n_adapters, n_waves, order, start, (const T*)p.b, bt, p.d_out, p.rank, transposes, drop, kept, chunks);
+  if (needs_v)
+    launch_tiles<T, false>(TileArgs<T>{(const T*)p.dy, bt, nullptr, p.scale, p.ids, nullptr, nullptr, v, p.tokens, p.d_out, 0, p.rank, p.n_adapters, l.ldv, 1, Drop{}}, s);
+  if (p.tokens > 0) {
+    const DxArgs<T> dx{v, (const T*)p.a, (const T*)p.dx_base, (T*)p.dx, p.d_in, l.ldv, mask};
+    const GradArgs<T> ga{(const T*)p.x, v, da, p.d_in, l.ldv, mask}, gb{(const T*)p.dy, p.u, db, p.d_out, p.rank, Mask{}};
+    const OrderArgs w{p.ids, order, start, p.tokens, p.rank, p.n_adapters, l.chunk};
+    const int slabs_in = (p.d_in + 127) / 128, slabs_dx = p.dx ? slabs_in : 0, slabs_da = p.da ? slabs_in : 0, slabs_db = p.db ? (p.d_out + 127) / 128 : 0;
+    const bool whole = (slabs_dx + slabs_da == 0 || p.d_in % 8 == 0) && (slabs_db == 0 || p.d_out % 8 == 0);
+    if (slabs_dx + slabs_da + slabs_db > 0)
+      with_shape(p.rank, whole, std::min(p.d_in, p.d_out) < 8, [&](auto r, auto edge) {
+        hipLaunchKernelGGL((outer_kernel<T, decltype(r)::value, decltype(edge)::value>), dim3(slabs_dx + slabs_da + slabs_db, l.chunks), dim3(256), 0, s, dx, ga, gb,
+                           w, slabs_dx, slabs_da);
+      });
   }
-  with_rank(p.rank, [&](auto r) {
-    constexpr int R = decltype(r)::value;
-    if (l.chunks > 0 && (p.dx || p.da)) {
-      const OuterArgs<T> g{(const T*)p.x, v, (const T*)p.a, (const T*)p.dx_base, (T*)p.dx, da, order, start, (int)p.tokens, p.d_in, p.rank, p.n_adapters, l.chunk, drop};
-      const dim3 grid((p.d_in + 127) / 128, l.chunks);
-      if (p.dx && p.da) hipLaunchKernelGGL((outer_kernel<T, R, true, true>), grid, dim3(256), 0, s, g);
-      else if (p.dx) hipLaunchKernelGGL((outer_kernel<T, R, true, false>), grid, dim3(256), 0, s, g);
-      else hipLaunchKernelGGL((outer_kernel<T, R, false, true>), grid, dim3(256), 0, s, g);
-    }
-    if (l.chunks > 0 && p.db) {
-      const OuterArgs<T> g{(const T*)p.dy, p.u, nullptr, nullptr, nullptr, db, order, start, (int)p.tokens, p.d_out, p.rank, p.n_adapters, l.chunk, Drop{}};
-      hipLaunchKernelGGL((outer_kernel<T, R, false, true>), dim3((p.d_out + 127) / 128, l.chunks), dim3(256), 0, s, g);
-    }
-  });
-  if (p.da)
-    hipLaunchKernelGGL(sum_slots_kernel, dim3((unsigned)(((int64_t)p.rank * p.d_in + 255) / 256), p.n_adapters), dim3(256), 0, s, da, start, (const float*)nullptr, p.da,
-                       p.d_in, p.rank, l.chunk, 0);
-  if (p.db)
-    hipLaunchKernelGGL(sum_slots_kernel, dim3((unsigned)(((int64_t)p.rank * p.d_out + 255) / 256), p.n_adapters), dim3(256), 0, s, db, start, p.scale, p.db, p.d_out,
-                       p.rank, l.chunk, 1);
+  const int blocks_in = p.da ? (int)(((int64_t)p.rank * p.d_in + 255) / 256) : 0, blocks_out = p.db ? (int)(((int64_t)p.rank * p.d_out + 255) / 256) : 0;
+  if (blocks_in + blocks_out > 0)
+    hipLaunchKernelGGL(sum_slots_kernel, dim3(blocks_in + blocks_out, p.n_adapters), dim3(256), 0, s, da, db, start, p.scale, p.da, p.db, p.d_in, p.d_out, p.rank,
+                       l.chunk, blocks_in);
 }
 
 static int check_adapters(const char* what, int dtype, int64_t tokens, int d_in, int d_out, int rank, int n_adapters) {

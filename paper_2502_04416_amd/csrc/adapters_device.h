@@ -1,0 +1,205 @@
+// Operands of the matrix instructions for the adapters: eight values of a row per lane, in registers.
+#pragma once
+#include "dropout_device.h"
+
+namespace cmoe {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Eight consecutive values along the contracted axis of one row: lane l holds row l & 15, values (l >> 4) * 8 on.  A product of
+// two operands leaves column l & 15 (of the second) and rows (l >> 4) * 4 + i (of the first) in lane l.
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> { uint32_t w[4]; };
+template <> struct Frag<float> { float w[8]; };
+
+__device__ __forceinline__ void mma(f32x4& acc, const Frag<bf16_t>& rows, const Frag<bf16_t>& cols) {
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, rows), __builtin_bit_cast(bf16x8, cols), acc, 0, 0, 0);
+}
+// (eight steps of four: both operands number the contracted axis alike, so its order is free)
+__device__ __forceinline__ void mma(f32x4& acc, const Frag<float>& rows, const Frag<float>& cols) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(rows.w[j], cols.w[j], acc, 0, 0, 0);
+}
+
+__device__ __forceinline__ Frag<bf16_t> load_frag(const bf16_t* p) {
+  return __builtin_bit_cast(Frag<bf16_t>, *reinterpret_cast<const Bytes16<bf16_t>*>(p));
+}
+__device__ __forceinline__ Frag<float> load_frag(const float* p) {
+  Frag<float> f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const Bytes16<float> b = *reinterpret_cast<const Bytes16<float>*>(p + 4 * h);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.w[4 * h + e] = __uint_as_float(b.w[e]);
+  }
+  return f;
+}
+// Values from the s-th on, zeros after the last (any s >= 0).
+__device__ __forceinline__ void shift_down(Frag<bf16_t>& f, int s) {
+  const bool four = s & 4, two = s & 2, one = s & 1;
+  f.w[0] = four ? f.w[2] : f.w[0];
+  f.w[1] = four ? f.w[3] : f.w[1];
+  f.w[2] = four ? 0u : f.w[2];
+  f.w[3] = four ? 0u : f.w[3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f.w[i] = two ? (i < 3 ? f.w[i + 1] : 0u) : f.w[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f.w[i] = s > 7 ? 0u : one ? (f.w[i] >> 16) | (i < 3 ? f.w[i + 1] << 16 : 0u) : f.w[i];
+}
+__device__ __forceinline__ void shift_down(Frag<float>& f, int s) {
+#pragma unroll
+  for (int step = 4; step > 0; step >>= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.w[e] = (s & step) ? (e + step < 8 ? f.w[e + step] : 0.0f) : f.w[e];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.w[e] = s > 7 ? 0.0f : f.w[e];
+}
+// The first n values, zeros after them.
+__device__ __forceinline__ void keep_first(Frag<bf16_t>& f, int n) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f.w[e] = n >= 2 * e + 2 ? f.w[e] : n == 2 * e + 1 ? f.w[e] & 0xffffu : 0u;
+}
+__device__ __forceinline__ void keep_first(Frag<float>& f, int n) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.w[e] = e < n ? f.w[e] : 0.0f;
+}
+
+// How the values `at` on of a buffer of `size` are read, of which n (it may be 0 or less, or more than 8) belong to the row:
+//   WHOLE   rows are a multiple of eight values: n >= 8, or n <= 0 and the result is not used
+//   RAGGED  the buffer has eight values at least: eight that do not pass its end, moved into place, zeros from the n-th on
+//   TINY    one by one
+// The first two have no branch, so that a caller's loads are all in flight before the first is waited for.
+enum { WHOLE, RAGGED, TINY };
+template <int EDGE, typename T>
+__device__ __forceinline__ Frag<T> load_at(const T* p, int64_t at, int n, int64_t size) {
+  if constexpr (EDGE == WHOLE) return load_frag(p + (n > 0 ? at : 0));
+  if constexpr (EDGE == RAGGED) {
+    const int64_t from = n > 0 ? min(at, size - 8) : 0;
+    Frag<T> f = load_frag(p + from);
+    shift_down(f, n > 0 ? (int)(at - from) : 8);
+    keep_first(f, n);
+    return f;
+  }
+  Frag<T> f = {};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (e >= n) continue;
+    if constexpr (sizeof(T) == 2) f.w[e >> 1] |= (uint32_t)p[at + e] << (16 * (e & 1));
+    else f.w[e] = p[at + e];
+  }
+  return f;
+}
+
+// What dropout drops becomes 0 (its scale is applied to the products in fp32, so that bf16 values stay as they are).
+// kept: a bit per value, from bit AT on.
+template <int AT>
+__device__ __forceinline__ void mask_frag(Frag<bf16_t>& f, uint32_t kept) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    f.w[e] &= ((uint32_t)__builtin_amdgcn_sbfe(kept, AT + 2 * e, 1) & 0xffffu) | ((uint32_t)__builtin_amdgcn_sbfe(kept, AT + 2 * e + 1, 1) & 0xffff0000u);
+}
+template <int AT>
+__device__ __forceinline__ void mask_frag(Frag<float>& f, uint32_t kept) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.w[e] = __uint_as_float(__float_as_uint(f.w[e]) & (uint32_t)__builtin_amdgcn_sbfe(kept, AT + e, 1));
+}
+
+// ... of N operands, four to a word.
+template <int I = 0, typename T, int N, int W>
+__device__ __forceinline__ void mask_frags(Frag<T> (&f)[N], const uint32_t (&kept)[W]) {
+  mask_frag<(I & 3) * 8>(f[I], kept[I >> 2]);
+  if constexpr (I + 1 < N) mask_frags<I + 1>(f, kept);
+}
+
+// The bits of 4 * N chunks, chunk(j) the j-th one's number, 32 to a word.  A loop, not N copies of the generator: the kernels are
+// short-lived, and what they fetch as code counts (four copies and more of it made the training step a third slower).
+template <int N, typename F>
+__device__ __forceinline__ void kept_bits(const Drop& d, uint32_t (&kept)[N], F&& chunk) {
+  const uint32_t rest = 65536u - d.limit;                    // a half word is at least the limit where the sum carries
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint32_t bits = 0;
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {
+      const uint4 words = philox_words(d, chunk(i * 4 + j));
+      uint32_t b = 0;
+#pragma unroll
+      for (int e = 7; e >= 0; --e) {
+        const uint32_t w = e < 2 ? words.x : e < 4 ? words.y : e < 6 ? words.z : words.w;
+        b = (b << 1) | ((((e & 1) ? w >> 16 : w & 0xffffu) + rest) >> 16);
+      }
+      bits |= b << (8 * j);
+    }
+    kept[i] = bits;
+  }
+}
+
+// Eight rows of eight values to eight columns.
+__device__ __forceinline__ void transpose(const Frag<bf16_t> (&rows)[8], Frag<bf16_t> (&cols)[8]) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      cols[2 * d].w[a] = __builtin_amdgcn_perm(rows[2 * a + 1].w[d], rows[2 * a].w[d], 0x05040100u);
+      cols[2 * d + 1].w[a] = __builtin_amdgcn_perm(rows[2 * a + 1].w[d], rows[2 * a].w[d], 0x07060302u);
+    }
+}
+__device__ __forceinline__ void transpose(const Frag<float> (&rows)[8], Frag<float> (&cols)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) cols[e].w[j] = rows[j].w[e];
+}
+
+// fp32 values as a sum of operands.  bf16: the upper eight bits of the significand, then those of what is left, the last term
+// rounded: two terms carry 16 bits (outputs that are themselves rounded to bf16), three all 24 (gradients of the weights, which
+// stay fp32).  What is left of an infinity would be NaN: 0.  fp32 needs one term.
+template <typename T> struct Terms { static constexpr int OUTPUT = 1, GRADIENT = 1; };
+template <> struct Terms<bf16_t> { static constexpr int OUTPUT = 2, GRADIENT = 3; };
+
+template <int N>
+__device__ __forceinline__ void split(const float (&v)[8], Frag<bf16_t> (&f)[N]) {
+  float rest[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rest[e] = v[e];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i < N - 1) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[i].w[e] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * e + 1]), __float_as_uint(rest[2 * e]), 0x07060302u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float left = rest[e] - __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+        rest[e] = left == left ? left : 0.0f;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[i].w[e] = (uint32_t)f32_to_bf16(rest[2 * e]) | ((uint32_t)f32_to_bf16(rest[2 * e + 1]) << 16);
+    }
+  }
+}
+__device__ __forceinline__ void split(const float (&v)[8], Frag<float> (&f)[1]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[0].w[e] = v[e];
+}
+
+__device__ __forceinline__ void unpack(const Frag<bf16_t>& f, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[2 * e] = __uint_as_float(f.w[e] << 16);
+    v[2 * e + 1] = __uint_as_float(f.w[e] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const Frag<float>& f, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = f.w[e];
+}
+
+// Eight values to a row of which n are left.
+template <int EDGE, typename T>
+__device__ __forceinline__ void store_at(T* p, int n, const float (&v)[8]) {
+  if (n > 0) store8(p, EDGE == WHOLE ? 8 : n, v);
+}
+
+}  // namespace cmoe
