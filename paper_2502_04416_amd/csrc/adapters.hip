@@ -428,15 +428,21 @@ struct OrderArgs {
 
 constexpr int CHUNK_MAX = 512;
 
-// A workgroup of these two has 128 columns and a chunk of the places in the order of adapters, and takes it adapter by adapter, its four
-// waves in turns of 32 places.  A lane holds eight columns, m * 8 on, of eight tokens, those of places q * 4 + 0..3 and
-// 16 + q * 4 + 0..3; so every load and store is 16 bytes of a row, and one evaluation of the generator is one lane's chunk.
+// A workgroup of the gradients and of dx has 128 columns and a chunk of the places in the order of adapters, and takes it adapter by
+// adapter, its four waves in turns.  A lane holds eight columns, m * 8 on, of several tokens, so that every load and store is 16 bytes of a
+// row.  (Two kernels: one for both needed 246 registers where these need 164 and less, two waves per SIMD instead of three or more.)
 struct Places {
   const int32_t* token;   // LDS
   int first, last;        // of the chunk
 };
+__device__ __forceinline__ Places load_places(const OrderArgs& w, int chunk, int32_t* token) {
+  const Places at{token, chunk * w.chunk, (int)min((int64_t)(chunk + 1) * w.chunk, w.tokens)};
+  for (int i = threadIdx.x; i < at.last - at.first; i += 256) token[i] = w.order[at.first + i];
+  __syncthreads();
+  return at;
+}
 
-// Sums over tokens: the lane turns its eight rows in registers into eight operands whose contracted axis is the tokens (operand e's row m
+// Sums over tokens, 32 in a turn, the lane's at places q * 4 + 0..3 and 16 + q * 4 + 0..3: the lane turns its eight rows in registers into eight operands whose contracted axis is the tokens (operand e's row m
 // is column 8 m + e), so nothing goes through LDS.  An adapter's sums within the chunk go to a slot of their own (numbered chunk +
 // adapter: of two neighbours in the order one number is larger), and are added in the order of chunks by the kernel below.
 template <typename T, int R16, int EDGE>
@@ -509,13 +515,30 @@ __device__ __forceinline__ void grad_segment(const GradArgs<T>& g, const OrderAr
   }
 }
 
-// dx: rows are tokens, columns those of dx, dealt so that a lane ends with eight consecutive ones; a's rows are turned in registers.
+// Slabs of da, then of db.
+template <typename T, int R16, int EDGE>
+__global__ __launch_bounds__(256) void grad_kernel(GradArgs<T> da, GradArgs<T> db, OrderArgs w, int slabs_da) {
+  __shared__ float sums[3 * 64 * 32];
+  __shared__ int32_t token[CHUNK_MAX];
+  const Places at = load_places(w, blockIdx.y, token);
+  const bool first = (int)blockIdx.x < slabs_da;
+  for (int p0 = at.first; p0 < at.last;) {
+    const int id = adapter_of(w.ids, token[p0 - at.first], w.n_adapters);
+    if (id < 0) break;                                       // (they are the last)
+    const int p1 = min(w.start[id + 1], at.last);
+    grad_segment<T, R16, EDGE>(first ? da : db, w, at, blockIdx.x - (first ? 0 : slabs_da), id, p0, p1, sums);
+    p0 = p1;
+  }
+}
+
+// dx: rows are tokens, 16 in a turn, columns those of dx, dealt so that a lane ends with eight consecutive ones of four tokens; the adapter's
+// rows are turned in registers once.
 template <typename T, int R16, int EDGE>
 __device__ __forceinline__ void dx_segment(const DxArgs<T>& g, const OrderArgs& w, const Places& at, int slab, int k, int p0, int p1) {
   constexpr int CHUNKS = (R16 + 1) / 2, NT = Terms<T>::OUTPUT;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
   const int c0 = slab * 128 + m * 8, n = g.d - c0, per_row = (g.d + 7) >> 3;
-  const bool none = k == w.n_adapters;                       // dx = base
+  const bool none = k < 0;                                   // dx = base
   Frag<T> af[CHUNKS][8];
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
@@ -529,101 +552,95 @@ __device__ __forceinline__ void dx_segment(const DxArgs<T>& g, const OrderArgs& 
     transpose(rows, af[c]);
   }
 #pragma unroll 1
-  for (int p = p0 + wave * 32; p < p1; p += 128) {
-    auto place = [&](int j) { return p + (j >> 2) * 16 + q * 4 + (j & 3); };
-    Frag<T> base[8];
-    float h[2][CHUNKS][8];
-    if (g.base) {
+  for (int p = p0 + wave * 16; p < p1; p += 64) {
+    Frag<T> base[4];
+    uint32_t kept[4];
+    float h[CHUNKS][8];
+    int64_t row[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) base[j] = load_at<EDGE>(g.base, (int64_t)at.token[min(place(j), p1 - 1) - at.first] * g.d + c0, n, w.tokens * g.d);
+    for (int i = 0; i < 4; ++i) {
+      const int64_t t = at.token[min(p + q * 4 + i, p1 - 1) - at.first];
+      row[i] = t * g.d + c0;
+      if (g.base) base[i] = load_at<EDGE>(g.base, row[i], n, w.tokens * g.d);
+      if (g.mask.kept) kept[i] = g.mask.kept[t * per_row + min(c0 >> 3, per_row - 1)];
     }
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int c = 0; c < CHUNKS; ++c) load8(g.v + (int64_t)at.token[min(p + m, p1 - 1) - at.first] * g.ldv + min((c * 4 + q) * 8, g.ldv - 8), 8, h[c]);
+    f32x4 out[8];
 #pragma unroll
-      for (int c = 0; c < CHUNKS; ++c)
-        load8(g.v + (int64_t)at.token[min(p + s * 16 + m, p1 - 1) - at.first] * g.ldv + min((c * 4 + q) * 8, g.ldv - 8), 8, h[s][c]);
-    uint32_t kept[8];
-    if (g.mask.kept) {
+    for (int e = 0; e < 8; ++e) out[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) kept[j] = g.mask.kept[(int64_t)at.token[min(place(j), p1 - 1) - at.first] * per_row + min(c0 >> 3, per_row - 1)];
+    for (int c = 0; c < CHUNKS; ++c) {
+      Frag<T> vf[NT];
+      split(h[c], vf);
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mma(out[e], vf[i], af[c][e]);
     }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      f32x4 out[8];
+    for (int i = 0; i < 4; ++i) {
+      if (p + q * 4 + i >= p1) continue;
+      float o[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) out[e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) {
-        Frag<T> vf[NT];
-        split(h[s][c], vf);
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) mma(out[e], vf[i], af[c][e]);
+      for (int e = 0; e < 8; ++e) {
+        o[e] = none ? 0.0f : out[e][i];
+        if (g.mask.kept) o[e] = __uint_as_float(__float_as_uint(o[e] * g.mask.scale) & (uint32_t)__builtin_amdgcn_sbfe(kept[i], e, 1));
       }
+      if (g.base) {
+        float b[8];
+        unpack(base[i], b);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = s * 4 + i;
-        if (place(j) >= p1) continue;
-        float o[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          o[e] = none ? 0.0f : out[e][i];
-          if (g.mask.kept) o[e] = __uint_as_float(__float_as_uint(o[e] * g.mask.scale) & (uint32_t)__builtin_amdgcn_sbfe(kept[j], e, 1));
-        }
-        if (g.base) {
-          float b[8];
-          unpack(base[j], b);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += b[e];
-        }
-        store_at<EDGE>(g.dx + (int64_t)at.token[place(j) - at.first] * g.d + c0, n, o);
+        for (int e = 0; e < 8; ++e) o[e] += b[e];
       }
+      store_at<EDGE>(g.dx + row[i], n, o);
     }
   }
 }
 
-// Slabs of dx, then of da, then of db.
-template <typename T, int R16, int EDGE>
-__global__ __launch_bounds__(256) void outer_kernel(DxArgs<T> dx, GradArgs<T> da, GradArgs<T> db, OrderArgs w, int slabs_dx, int slabs_da) {
-  __shared__ float sums[3 * 64 * 32];
-  __shared__ int32_t token[CHUNK_MAX];
-  const Places at{token, (int)blockIdx.y * w.chunk, (int)min((int64_t)(blockIdx.y + 1) * w.chunk, w.tokens)};
-  for (int i = threadIdx.x; i < at.last - at.first; i += 256) token[i] = w.order[at.first + i];
-  __syncthreads();
-  const int slab = blockIdx.x;
-  for (int p0 = at.first; p0 < at.last;) {
-    const int id = adapter_of(w.ids, token[p0 - at.first], w.n_adapters), k = id < 0 ? w.n_adapters : id;
-    const int p1 = min(w.start[k + 1], at.last);
-    if (slab < slabs_dx) dx_segment<T, R16, EDGE>(dx, w, at, slab, k, p0, p1);
-    else if (k < w.n_adapters) {
-      const bool first = slab < slabs_dx + slabs_da;
-      grad_segment<T, R16, EDGE>(first ? da : db, w, at, slab - slabs_dx - (first ? 0 : slabs_da), k, p0, p1, sums);
-    }
-    p0 = p1;
-  }
-}
+struct SumArgs {
+  const float* da_slots;
+  const float* db_slots;
+  const float* scale;
+  float* da;              // [n][rank][d_in]
+  float* db;              // [n][d_out][rank]
+  int d_in, d_out;
+  int blocks_in, blocks;  // workgroups per adapter: of da, of both
+};
 
-// The slots of an adapter added in the order of chunks (0 without one): da, and db, [n][d_out][rank], times the adapter's scale.
-__global__ __launch_bounds__(256) void sum_slots_kernel(const float* da_slots, const float* db_slots, const int32_t* start, const float* scale, float* da, float* db,
-                                                        int d_in, int d_out, int rank, int chunk, int blocks_in) {
-  const int k = blockIdx.y;
-  const bool first = (int)blockIdx.x < blocks_in;
-  const int d = first ? d_in : d_out;
-  const float* slots = first ? da_slots : db_slots;
-  const int64_t size = (int64_t)rank * d, i = (int64_t)(blockIdx.x - (first ? 0 : blocks_in)) * 256 + threadIdx.x;
+// Slots of an adapter added in the order of chunks (0 without one); db times the adapter's scale.
+__device__ __forceinline__ void sum_slots(const SumArgs& g, const OrderArgs& w, int block) {
+  const int k = block / g.blocks, b = block % g.blocks;
+  const bool first = b < g.blocks_in;
+  const int d = first ? g.d_in : g.d_out;
+  const int64_t size = (int64_t)w.rank * d, i = (int64_t)(b - (first ? 0 : g.blocks_in)) * 256 + threadIdx.x;
   if (i >= size) return;
-  const int p0 = start[k], p1 = start[k + 1];
+  const int p0 = w.start[k], p1 = w.start[k + 1];
   float t = 0.0f;
   if (p1 > p0) {
-    const int c0 = p0 / chunk, c1 = (p1 - 1) / chunk;
-    const float* from = slots + (int64_t)(c0 + k) * size + i;
+    const int c0 = p0 / w.chunk, c1 = (p1 - 1) / w.chunk;
+    const float* from = (first ? g.da_slots : g.db_slots) + (int64_t)(c0 + k) * size + i;
 #pragma unroll 8
     for (int c = c0; c <= c1; ++c, from += size) t += *from;
-    if (!first) t *= scale[k];
+    if (!first) t *= g.scale[k];
   }
-  if (first) da[k * size + i] = t;
-  else db[k * size + (i % d) * rank + i / d] = t;
+  if (first) g.da[k * size + i] = t;
+  else g.db[k * size + (i % d) * w.rank + i / d] = t;
+}
+
+// What is left once the slots are written: dx, which only needs v, and the sums of the slots, which are short beside it.
+template <typename T, int R16, int EDGE>
+__global__ __launch_bounds__(256) void finish_kernel(DxArgs<T> dx, SumArgs sums, OrderArgs w, int sum_blocks, int slabs) {
+  __shared__ int32_t token[CHUNK_MAX];
+  if ((int)blockIdx.x < sum_blocks) return sum_slots(sums, w, blockIdx.x);
+  const int block = blockIdx.x - sum_blocks, slab = block % slabs;
+  const Places at = load_places(w, block / slabs, token);
+  for (int p0 = at.first; p0 < at.last;) {
+    const int id = adapter_of(w.ids, token[p0 - at.first], w.n_adapters);
+    const int p1 = min(w.start[id < 0 ? w.n_adapters + 1 : id + 1], at.last);
+    dx_segment<T, R16, EDGE>(dx, w, at, slab, id, p0, p1);
+    p0 = p1;
+  }
 }
 
 // f(R16) with the rank in blocks of 16 as a compile-time constant
@@ -709,22 +726,23 @@ static void launch_adapters_backward(const cmoe_adapters_backward_args& p, const
                      p.n_adapters, n_waves, order, start, (const T*)p.b, bt, p.d_out, p.rank, transposes, drop, kept, chunks);
   if (needs_v)
     launch_tiles<T, false>(TileArgs<T>{(const T*)p.dy, bt, nullptr, p.scale, p.ids, nullptr, nullptr, v, p.tokens, p.d_out, 0, p.rank, p.n_adapters, l.ldv, 1, Drop{}}, s);
-  if (p.tokens > 0) {
-    const DxArgs<T> dx{v, (const T*)p.a, (const T*)p.dx_base, (T*)p.dx, p.d_in, l.ldv, mask};
-    const GradArgs<T> ga{(const T*)p.x, v, da, p.d_in, l.ldv, mask}, gb{(const T*)p.dy, p.u, db, p.d_out, p.rank, Mask{}};
-    const OrderArgs w{p.ids, order, start, p.tokens, p.rank, p.n_adapters, l.chunk};
-    const int slabs_in = (p.d_in + 127) / 128, slabs_dx = p.dx ? slabs_in : 0, slabs_da = p.da ? slabs_in : 0, slabs_db = p.db ? (p.d_out + 127) / 128 : 0;
-    const bool whole = (slabs_dx + slabs_da == 0 || p.d_in % 8 == 0) && (slabs_db == 0 || p.d_out % 8 == 0);
-    if (slabs_dx + slabs_da + slabs_db > 0)
-      with_shape(p.rank, whole, std::min(p.d_in, p.d_out) < 8, [&](auto r, auto edge) {
-        hipLaunchKernelGGL((outer_kernel<T, decltype(r)::value, decltype(edge)::value>), dim3(slabs_dx + slabs_da + slabs_db, l.chunks), dim3(256), 0, s, dx, ga, gb,
-                           w, slabs_dx, slabs_da);
-      });
+  const DxArgs<T> dx{v, (const T*)p.a, (const T*)p.dx_base, (T*)p.dx, p.d_in, l.ldv, mask};
+  const GradArgs<T> ga{(const T*)p.x, v, da, p.d_in, l.ldv, mask}, gb{(const T*)p.dy, p.u, db, p.d_out, p.rank, Mask{}};
+  const OrderArgs w{p.ids, order, start, p.tokens, p.rank, p.n_adapters, l.chunk};
+  const int slabs = (p.d_in + 127) / 128, slabs_da = p.da ? slabs : 0, slabs_db = p.db ? (p.d_out + 127) / 128 : 0;
+  if (p.tokens > 0 && slabs_da + slabs_db > 0) {
+    const bool whole = (!p.da || p.d_in % 8 == 0) && (!p.db || p.d_out % 8 == 0), tiny = (p.da && p.d_in < 8) || (p.db && p.d_out < 8);
+    with_shape(p.rank, whole, tiny, [&](auto r, auto edge) {
+      hipLaunchKernelGGL((grad_kernel<T, decltype(r)::value, decltype(edge)::value>), dim3(slabs_da + slabs_db, l.chunks), dim3(256), 0, s, ga, gb, w, slabs_da);
+    });
   }
   const int blocks_in = p.da ? (int)(((int64_t)p.rank * p.d_in + 255) / 256) : 0, blocks_out = p.db ? (int)(((int64_t)p.rank * p.d_out + 255) / 256) : 0;
-  if (blocks_in + blocks_out > 0)
-    hipLaunchKernelGGL(sum_slots_kernel, dim3(blocks_in + blocks_out, p.n_adapters), dim3(256), 0, s, da, db, start, p.scale, p.da, p.db, p.d_in, p.d_out, p.rank,
-                       l.chunk, blocks_in);
+  const SumArgs sums{da, db, p.scale, p.da, p.db, p.d_in, p.d_out, blocks_in, blocks_in + blocks_out};
+  const int sum_blocks = sums.blocks * p.n_adapters, dx_blocks = p.dx ? slabs * l.chunks : 0;
+  if (sum_blocks + dx_blocks > 0)
+    with_shape(p.rank, p.d_in % 8 == 0, p.d_in < 8, [&](auto r, auto edge) {
+      hipLaunchKernelGGL((finish_kernel<T, decltype(r)::value, decltype(edge)::value>), dim3(sum_blocks + dx_blocks), dim3(256), 0, s, dx, sums, w, sum_blocks, slabs);
+    });
 }
 
 static int check_adapters(const char* what, int dtype, int64_t tokens, int d_in, int d_out, int rank, int n_adapters) {

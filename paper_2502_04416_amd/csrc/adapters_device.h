@@ -175,7 +175,7 @@ __device__ __forceinline__ void split(const float (&v)[8], Frag<bf16_t> (&f)[N])
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f[i].w[e] = (uint32_t)f32_to_bf16(rest[2 * e]) | ((uint32_t)f32_to_bf16(rest[2 * e + 1]) << 16);
+      for (int e = 0; e < 4; ++e) f[i].w[e] = pack_bf16(rest[2 * e], rest[2 * e + 1]);
     }
   }
 }

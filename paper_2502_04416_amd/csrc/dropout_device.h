@@ -79,11 +79,18 @@ __device__ __forceinline__ void load8(const float* p, int n, float (&v)[8]) {
   }
 }
 
+// Two values rounded to bf16 by one conversion.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
+
 __device__ __forceinline__ void store8(bf16_t* p, int n, const float (&v)[8]) {
   if (n >= 8) {
     Bytes16<bf16_t> b;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) b.w[e] = (uint32_t)f32_to_bf16(v[2 * e]) | ((uint32_t)f32_to_bf16(v[2 * e + 1]) << 16);
+    for (int e = 0; e < 4; ++e) b.w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
     *reinterpret_cast<Bytes16<bf16_t>*>(p) = b;
   } else {
 #pragma unroll
