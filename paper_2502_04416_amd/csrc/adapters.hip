@@ -17,6 +17,7 @@
 namespace cmoe {
 
 constexpr int MAX_RANK = 64;
+constexpr int MAX_WIDTH = 1 << 20;       // of SCAN_TOKENS rows an offset fits 31 bits of bytes
 constexpr int MAX_ADAPTERS = 8191;       // a wave's counts of them fit LDS
 
 // The adapter of a token, or -1.
@@ -24,6 +25,16 @@ __device__ __forceinline__ int adapter_of(const int32_t* ids, int64_t t, int n_a
   const int k = ids ? ids[t] : 0;
   return k >= 0 && k < n_adapters ? k : -1;
 }
+
+// A value of which the compiler takes nothing for granted: what is computed from it stays where it is used.  (It computes the addresses of
+// all loads of a loop ahead of it otherwise, 64 bits of each, and spills them.)
+__device__ __forceinline__ int here(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// The number of the wave in the workgroup, known to be the same in its lanes.
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // ---- u and y -------------------------------------------------------------------------------------------------------
 
@@ -46,25 +57,37 @@ struct TileArgs {
 
 constexpr int SCAN_TOKENS = 512;         // a workgroup of the scanning form looks at one id per thread
 
-// A tile is 16 tokens.  Its workgroup first contracts x with the adapter's rows: the waves take turns along the width, 64 values at a
-// time, and their sums meet in LDS; then each wave expands u to its own columns, on to base, straight from memory to memory.
+// Waves of a workgroup, and units of 32 columns of y that a wave has in flight at once.
+template <int R16>
+constexpr int TILE_WAVES = R16 == 1 ? 16 : 8;
+template <typename T, int R16>
+constexpr int UNITS_AT_ONCE = sizeof(T) == 4 || R16 == 4 ? 1 : R16 == 2 ? 4 : 2;
+
+// A tile is 16 tokens.  Its workgroup first contracts x with the adapter's rows: the waves take turns along the width, 64 values each
+// time, each a part of its own, and their sums meet in LDS; then each wave expands u to its own columns, on to base, straight from memory to memory.
 // SCAN: workgroup b is for the adapter of token b, if b is the first of its adapter's tokens or the 16th, 32nd ... after it; it finds
 // up to 16 of them itself.  Weights are then read once per 16 tokens of an adapter whatever the order, as decode batches need it,
-// where every token may have another.  Otherwise 16 consecutive tokens, and one pass for each adapter among them: prompts and
-// training batches come as runs, so that most tiles have one.
+// where every token may have another.  Otherwise 16 consecutive tokens, and one pass for each adapter among them, shared by gridDim.z
+// workgroups: prompts and training batches come as runs, so that most tiles have one, and the tiles with two are not the last to end.
 // A row or column of a product that is no token, rank or column of y reads another's values, and its results are not used: a token
 // does not see what another's adapter holds.
 // Without EXPAND: u * scale alone (v of the backward pass).
 template <typename T, int R16, bool SCAN, bool EXPAND, int EDGE>
-__global__ __launch_bounds__(R16 == 4 ? 512 : 1024) void tile_kernel(TileArgs<T> g) {
-  constexpr int WAVES = R16 == 4 ? 8 : 16;
+__global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_kernel(TileArgs<T> g) {
+  constexpr int WAVES = TILE_WAVES<R16>;
   constexpr int CHUNKS = (R16 + 1) / 2;                      // operands along the rank
   constexpr int NT = Terms<T>::OUTPUT;
   constexpr int LD = CHUNKS * 32 + 16 / sizeof(T);
   __shared__ float sums[WAVES][R16 * 4 * 64];
   __shared__ __align__(16) T us[EXPAND ? NT : 1][16][LD];    // scale * u, in terms
   __shared__ int token[16], id[16], found[16], counts[2][16], n_found;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, q = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), m = lane & 15, q = lane >> 4;
+  const int row = lane >> 2, part_q = lane & 3;              // row and chunk of a lane as rows are loaded and stored
+  const Lanes lanes = lane_orders();
+  // Consecutive tiles on one XCD (workgroups go to the eight in turn): they share adapters, which stay in its L2 cache.
+  const int per_xcd = (gridDim.x + 7) >> 3, tile = SCAN ? (int)blockIdx.x : (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+  if (!SCAN && (int64_t)tile * 16 >= g.tokens) return;
+  const int z = gridDim.z - 1 - blockIdx.z;                  // (the few tiles with a second adapter begin with it)
   if (SCAN) {
     const int me = blockIdx.x;
     const int k = adapter_of(g.ids, me, g.n_adapters);
@@ -94,7 +117,7 @@ __global__ __launch_bounds__(R16 == 4 ? 512 : 1024) void tile_kernel(TileArgs<T>
       n_found = k >= 0;
     }
   } else if (tid < 64) {
-    const int64_t t = (int64_t)blockIdx.x * 16 + m;
+    const int64_t t = (int64_t)tile * 16 + m;
     const bool valid = t < g.tokens;
     const int k = valid ? adapter_of(g.ids, t, g.n_adapters) : -2;
     bool first = k >= 0 && lane < 16;
@@ -105,7 +128,7 @@ __global__ __launch_bounds__(R16 == 4 ? 512 : 1024) void tile_kernel(TileArgs<T>
     }
     const uint64_t votes = __ballot(first);
     if (lane < 16) {
-      token[m] = valid ? m : 0;
+      token[m] = valid ? m : (int)(g.tokens - 1 - (int64_t)tile * 16);
       id[m] = k;
     }
     if (first) found[__popcll(votes & ((1ull << lane) - 1))] = k;
@@ -114,171 +137,185 @@ __global__ __launch_bounds__(R16 == 4 ? 512 : 1024) void tile_kernel(TileArgs<T>
   if (EXPAND && R16 == 1)                                    // (an operand is 32 values along the rank)
     for (int i = tid; i < (int)sizeof(us) / 4; i += WAVES * 64) reinterpret_cast<uint32_t*>(us)[i] = 0;
   __syncthreads();
-  const int64_t t0 = SCAN ? 0 : (int64_t)blockIdx.x * 16;
-  const int64_t my_token = t0 + token[m];
-  const int my_id = id[m], n_distinct = n_found;
+  const int64_t t0 = SCAN ? 0 : (int64_t)tile * 16;
+  const int my_token = token[m], my_id = id[m], row_token = token[row], row_id = id[row], n_distinct = __builtin_amdgcn_readfirstlane(n_found);
 
-  // u: rows are tokens, columns are the rank
-  for (int f = 0; f < n_distinct; ++f) {
-    const int k = found[f];
-    const int64_t x_at = my_token * g.d_in + q * 8;
-    int64_t a_at[R16];
-#pragma unroll
-    for (int r = 0; r < R16; ++r) a_at[r] = ((int64_t)k * g.rank + min(r * 16 + m, g.rank - 1)) * g.d_in + q * 8;
-    const uint64_t chunk0 = (uint64_t)my_token * ((g.d_in + 7) >> 3) + q;
-    f32x4 acc[R16];
-#pragma unroll
-    for (int r = 0; r < R16; ++r) acc[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int full = g.d_in / 64;
-    constexpr int DEPTH = R16 == 1 && sizeof(T) == 2 ? 4 : R16 == 4 || sizeof(T) == 2 ? 2 : 1;      // turns whose loads are in flight together
-    auto turns = [&](int s, auto depth) {
-      constexpr int D = decltype(depth)::value;
-      Frag<T> xf[2 * D], af[2 * D][R16];
-#pragma unroll
-      for (int i = 0; i < D; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int at = (s + i * WAVES) * 64 + h * 32;
-          xf[2 * i + h] = load_frag(g.x + x_at + at);
-#pragma unroll
-          for (int r = 0; r < R16; ++r) af[2 * i + h][r] = load_frag(g.a + a_at[r] + at);
-        }
-      if (g.drop.limit) {
-        uint32_t kept[(D + 1) / 2];
-        kept_bits(g.drop, kept, [&](int j) { return chunk0 + (s + (j >> 1) * WAVES) * 8 + (j & 1) * 4; });
-        mask_frags(xf, kept);
-      }
-#pragma unroll
-      for (int i = 0; i < 2 * D; ++i)
-#pragma unroll
-        for (int r = 0; r < R16; ++r) mma(acc[r], xf[i], af[i][r]);
-    };
-    int s = wave;
-    for (; s + (DEPTH - 1) * WAVES < full; s += DEPTH * WAVES) turns(s, std::integral_constant<int, DEPTH>{});
-    for (; s < full; s += WAVES) turns(s, std::integral_constant<int, 1>{});
-    if (s == full && (g.d_in & 63)) {                        // the rest of the width
-      Frag<T> xf[2], af[2][R16];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int at = s * 64 + h * 32, n = g.d_in - at - q * 8;
-        xf[h] = load_at<EDGE>(g.x, x_at + at, n, g.tokens * g.d_in);
-#pragma unroll
-        for (int r = 0; r < R16; ++r) {
-          af[h][r] = load_at<EDGE>(g.a, a_at[r] + at, n, (int64_t)g.n_adapters * g.rank * g.d_in);
-          keep_first(af[h][r], n);
-        }
-        keep_first(xf[h], n);
-      }
-      if (g.drop.limit) {
-        uint32_t kept[1];
-        kept_bits(g.drop, kept, [&](int j) { return chunk0 + s * 8 + (j & 1) * 4; });
-        mask_frags(xf, kept);
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int r = 0; r < R16; ++r) mma(acc[r], xf[h], af[h][r]);
-    }
-#pragma unroll
-    for (int r = 0; r < R16; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sums[wave][(r * 4 + i) * 64 + lane] = acc[r][i];
-    __syncthreads();
-    const float scale = g.scale[k];
-    for (int v = tid; v < R16 * 256; v += WAVES * 64) {
-      const int l = v & 63, row = (l >> 4) * 4 + ((v >> 6) & 3), col = (v >> 8) * 16 + (l & 15);
-      float t = sums[0][v];
-#pragma unroll
-      for (int w = 1; w < WAVES; ++w) t += sums[w][v];
-      if (g.drop.limit) t *= g.drop.scale;
-      if (id[row] != k) continue;
-      if (col >= g.rank) t = 0.0f;
-      if (g.u && blockIdx.y == 0 && col < g.ldu) g.u[(t0 + token[row]) * g.ldu + col] = EXPAND ? t : t * scale;
-      if (EXPAND) {
-        t *= scale;
-        if constexpr (sizeof(T) == 2) {
-          const uint32_t hi = __float_as_uint(t) & 0xffff0000u;
-          const float left = t - __uint_as_float(hi);
-          us[0][row][col] = (T)(hi >> 16);
-          us[1][row][col] = left == left ? f32_to_bf16(left) : (T)0;
-        } else {
-          us[0][row][col] = t;
-        }
-      }
-    }
-    __syncthreads();
-  }
-  if (g.u && blockIdx.y == 0)
-    for (int v = tid; v < 16 * g.ldu; v += WAVES * 64)
-      if (id[v / g.ldu] == -1) g.u[(t0 + token[v / g.ldu]) * g.ldu + v % g.ldu] = 0.0f;
-  if (!EXPAND) return;
-
-  // y: rows are 16 columns of y, columns are tokens, the contracted axis the rank.  Two products' rows are dealt so that a lane ends
-  // with eight consecutive columns of its token.
+  // What the expansion reads, UNITS units of 32 columns of y at a time (past the wave's last unit: its values).
+  constexpr int UNITS = UNITS_AT_ONCE<T, R16>;
   const int units = (g.d_out + 31) >> 5;
-  const int first = (int)((int64_t)units * blockIdx.y / g.slices), last = (int)((int64_t)units * (blockIdx.y + 1) / g.slices);
+  const int part = blockIdx.y * WAVES + wave, parts = g.slices * WAVES;
+  const int first = (int)((int64_t)units * part / parts), last = (int)((int64_t)units * (part + 1) / parts);      // of the wave
   const int64_t y_size = g.tokens * g.d_out, b_size = (int64_t)g.n_adapters * g.d_out * g.rank;
-  const int64_t y_at = my_token * g.d_out + q * 8;
-  auto expand = [&](int unit, auto depth) {                  // `depth` units, WAVES apart
-    constexpr int D = decltype(depth)::value;
-    Frag<T> basef[D];
-    float v[D][8];
+  const int y_at = row_token * g.d_out + part_q * 8, b_at = ((row >> 2) * 8 + (row & 3)) * g.rank + part_q * 8;
+  const T* base = g.base ? g.base : g.y;                     // (without one the values are not used)
+  auto load_units = [&](int unit, int k, Frag<T> (&basef)[UNITS], Frag<T> (&bf)[UNITS][2][CHUNKS]) {
+    const int y_here = here(y_at), b_here = here(b_at);
 #pragma unroll
-    for (int i = 0; i < D; ++i) {
-      const int o0 = (unit + i * WAVES) * 32;
-      if (g.base) basef[i] = load_at<EDGE>(g.base, y_at + o0, g.d_out - o0 - q * 8, y_size);
+    for (int i = 0; i < UNITS; ++i) {
+      const int o0 = min(unit + i, last - 1) * 32;
+      const int64_t y0 = t0 * g.d_out + o0, b0 = ((int64_t)max(k, 0) * g.d_out + o0) * g.rank;
+      basef[i] = load_near<EDGE>(base + y0, y_here, g.d_out - o0 - part_q * 8, y_size - y0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
-    }
-    for (int f = 0; f < n_distinct; ++f) {
-      const int k = found[f];
-      Frag<T> bf[D][2][CHUNKS];
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-      for (int i = 0; i < D; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int o = min((unit + i * WAVES) * 32 + (m >> 2) * 8 + e * 4 + (m & 3), g.d_out - 1);
-          const int64_t row = ((int64_t)k * g.d_out + o) * g.rank;
-#pragma unroll
-          for (int c = 0; c < CHUNKS; ++c) bf[i][e][c] = load_at<EDGE>(g.b, row + (c * 4 + q) * 8, g.rank - (c * 4 + q) * 8, b_size);
-        }
-      Frag<T> uf[CHUNKS][NT];
-#pragma unroll
-      for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-        for (int p = 0; p < NT; ++p) uf[c][p] = *reinterpret_cast<const Frag<T>*>(&us[p][m][(c * 4 + q) * 8]);
-#pragma unroll
-      for (int i = 0; i < D; ++i) {
-        f32x4 acc[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            if (EDGE == WHOLE) keep_first(bf[i][e][c], g.rank - (c * 4 + q) * 8);
-#pragma unroll
-            for (int p = 0; p < NT; ++p) mma(acc[e], bf[i][e][c], uf[c][p]);
-          }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] += my_id == k ? acc[e >> 2][e & 3] : 0.0f;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < D; ++i) {
-      const int o0 = (unit + i * WAVES) * 32, n = g.d_out - o0 - q * 8;
-      if (my_id == -2) continue;
-      if (g.base) {
-        float o[8];
-        unpack(basef[i], o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] += o[e];
-      }
-      store_at<EDGE>(g.y + y_at + o0, n, v[i]);
+        for (int c = 0; c < CHUNKS; ++c) bf[i][e][c] = load_near<EDGE>(g.b + b0, b_here + e * 4 * g.rank + c * 32, g.rank - (c * 4 + part_q) * 8, b_size - b0);
     }
   };
-  constexpr int DEPTH = 4 / (R16 == 4 ? 2 : 1) / (sizeof(T) / 2);
-  int unit = first + wave;
-  for (; unit + (DEPTH - 1) * WAVES < last; unit += DEPTH * WAVES) expand(unit, std::integral_constant<int, DEPTH>{});
-  for (; unit < last; unit += WAVES) expand(unit, std::integral_constant<int, 1>{});
+
+  // Turns along the width are DEPTH at a time; past the wave's last turn its values, as zeros.
+  constexpr int DEPTH = R16 == 1 && sizeof(T) == 2 ? 4 : R16 == 4 || sizeof(T) == 2 ? 2 : 1;
+  const int full = g.d_in / 64;                              // whole turns
+  const int turns = (full + WAVES - 1) / WAVES, turn0 = min(wave * turns, full), turn1 = min(turn0 + turns, full);
+  auto turn = [&](int s, int i) { return min(s + (i >> 1), turn1 - 1) * 64 + (i & 1) * 32; };
+
+  // A pass per adapter, of those among the tile's tokens that are this workgroup's; the first takes the tokens without one along.
+  for (int f = z; f < n_distinct || f == 0; f += gridDim.z) {
+    const int k = f < n_distinct ? __builtin_amdgcn_readfirstlane(found[f]) : -1;
+    if (k >= 0) {
+      // u: rows are tokens, columns are the rank
+      const float scale = g.scale[k];
+      const T* x = g.x + t0 * g.d_in;
+      const T* a = g.a + (int64_t)k * g.rank * g.d_in;
+      const int x_at = here(row_token * g.d_in + part_q * 8);
+      int a_at[R16];
+#pragma unroll
+      for (int r = 0; r < R16; ++r) a_at[r] = here(min(r * 16 + row, g.rank - 1) * g.d_in + part_q * 8);
+      const uint64_t chunk0 = (uint64_t)(t0 + here(row_token)) * ((g.d_in + 7) >> 3) + part_q;
+      f32x4 acc[R16];
+#pragma unroll
+      for (int r = 0; r < R16; ++r) acc[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      Frag<T> xf[2 * DEPTH];
+      auto load_x = [&](int s) {
+#pragma unroll
+        for (int i = 0; i < 2 * DEPTH; ++i) xf[i] = load_from(x + turn(s, i), x_at);
+      };
+#pragma unroll 1
+      for (int s = turn0; s < turn1; s += DEPTH) {
+        load_x(s);
+        Frag<T> af[2 * DEPTH][R16];
+#pragma unroll
+        for (int i = 0; i < 2 * DEPTH; ++i)
+#pragma unroll
+          for (int r = 0; r < R16; ++r) af[i][r] = load_from(a + turn(s, i), a_at[r]);
+        if (g.drop.limit) {
+          uint32_t kept[(DEPTH + 1) / 2];
+          kept_bits(g.drop, kept, [&](int j) { return chunk0 + (turn(s, j) >> 3); });
+          mask_frags(xf, kept);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * DEPTH; ++i) {
+          if (i > 1) keep_all(xf[i], less_mask(s + (i >> 1), turn1));
+          const Frag<T> xo = exchange(xf[i], lanes.operand);
+#pragma unroll
+          for (int r = 0; r < R16; ++r) mma(acc[r], xo, exchange(af[i][r], lanes.operand));
+        }
+      }
+      if (wave == WAVES - 1 && (g.d_in & 63)) {             // the rest of the width
+        Frag<T> xr[2], ar[2][R16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int at = full * 64 + h * 32, n = g.d_in - at - part_q * 8;
+          xr[h] = load_near<EDGE>(x + at, x_at, n, (g.tokens - t0) * g.d_in - at);
+#pragma unroll
+          for (int r = 0; r < R16; ++r) {
+            ar[h][r] = load_near<EDGE>(a + at, a_at[r], n, (int64_t)(g.n_adapters - k) * g.rank * g.d_in - at);
+            keep_first(ar[h][r], n);
+          }
+          keep_first(xr[h], n);
+        }
+        if (g.drop.limit) {
+          uint32_t kept[1];
+          kept_bits(g.drop, kept, [&](int j) { return chunk0 + full * 8 + (j & 1) * 4; });
+          mask_frags(xr, kept);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < R16; ++r) mma(acc[r], exchange(xr[h], lanes.operand), exchange(ar[h][r], lanes.operand));
+      }
+#pragma unroll
+      for (int r = 0; r < R16; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[wave][(r * 4 + i) * 64 + lane] = acc[r][i];
+      __syncthreads();
+      for (int v = tid; v < R16 * 256; v += WAVES * 64) {
+        const int l = v & 63, row = (l >> 4) * 4 + ((v >> 6) & 3), col = (v >> 8) * 16 + (l & 15);
+        float t = sums[0][v];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) t += sums[w][v];
+        if (g.drop.limit) t *= g.drop.scale;
+        if (col >= g.rank) t = 0.0f;
+        if (g.u && blockIdx.y == 0 && col < g.ldu && id[row] == k) g.u[(t0 + token[row]) * g.ldu + col] = EXPAND ? t : t * scale;
+        if (EXPAND) {
+          t *= scale;
+          if constexpr (sizeof(T) == 2) {
+            const uint32_t hi = __float_as_uint(t) & 0xffff0000u;
+            const float left = t - __uint_as_float(hi);
+            us[0][row][col] = (T)(hi >> 16);
+            us[1][row][col] = left == left ? f32_to_bf16(left) : (T)0;
+          } else {
+            us[0][row][col] = t;
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (f == 0 && g.u && blockIdx.y == 0)
+      for (int v = tid; v < 16 * g.ldu; v += WAVES * 64)
+        if (id[v / g.ldu] == -1) g.u[(t0 + token[v / g.ldu]) * g.ldu + v % g.ldu] = 0.0f;
+    if (!EXPAND) continue;
+
+    // y: rows are 16 columns of y, columns are tokens, the contracted axis the rank.  Two products' rows are dealt so that a lane ends
+    // with eight consecutive columns of its token.
+    Frag<T> uf[CHUNKS][NT];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+      for (int p = 0; p < NT; ++p) uf[c][p] = *reinterpret_cast<const Frag<T>*>(&us[p][m][(c * 4 + q) * 8]);
+    const uint32_t has = my_id == k && k >= 0 ? ~0u : 0u, has_base = g.base ? ~0u : 0u;
+    uint32_t along[CHUNKS];                                  // chunks of the rank
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) along[c] = less_mask((c * 4 + part_q) * 8, g.rank);
+    const bool stores = row_id == k || (f == 0 && row_id == -1);
+    const int y_store = here(y_at);
+#pragma unroll 1
+    for (int unit = first; unit < last; unit += UNITS) {
+      Frag<T> basef[UNITS], bf[UNITS][2][CHUNKS];
+      load_units(unit, k, basef, bf);
+      f32x4 acc[UNITS][2];
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          acc[i][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int c = 0; c < CHUNKS; ++c) {
+            if (EDGE == WHOLE) keep_all(bf[i][e][c], along[c]);
+            const Frag<T> bo = exchange(bf[i][e][c], lanes.operand);
+#pragma unroll
+            for (int p = 0; p < NT; ++p) mma(acc[i][e], bo, uf[c][p]);
+          }
+        }
+      Frag<T> yf[UNITS];
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = keep(acc[i][e >> 2][e & 3], has);
+        float o[8];
+        unpack(exchange(basef[i], lanes.operand), o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += keep(o[e], has_base);
+        pack(v, yf[i]);
+        yf[i] = exchange(yf[i], lanes.rows);
+      }
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) {
+        const int o0 = (unit + i) * 32;
+        if (stores && unit + i < last) store_frag<EDGE>(g.y + t0 * g.d_out + o0 + y_store, g.d_out - o0 - part_q * 8, yf[i]);
+      }
+    }
+  }
 }
 
 // ---- backward: order of the tokens, b transposed -------------------------------------------------------------------
@@ -448,7 +485,7 @@ __device__ __forceinline__ Places load_places(const OrderArgs& w, int chunk, int
 template <typename T, int R16, int EDGE>
 __device__ __forceinline__ void grad_segment(const GradArgs<T>& g, const OrderArgs& w, const Places& at, int slab, int k, int p0, int p1, float* sums) {
   constexpr int NG = Terms<T>::GRADIENT;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = wave_id(), m = lane & 15, q = lane >> 4;
   const int c0 = slab * 128 + m * 8, n = g.d - c0, per_row = (g.d + 7) >> 3;
   f32x4 acc[R16][8];
 #pragma unroll
@@ -478,7 +515,7 @@ __device__ __forceinline__ void grad_segment(const GradArgs<T>& g, const OrderAr
 #pragma unroll
     for (int r = 0; r < R16; ++r) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[r][j] = place(j) < p1 ? f[r][j] : 0.0f;
+      for (int j = 0; j < 8; ++j) f[r][j] = keep(f[r][j], less_mask(place(j), p1));
       Frag<T> vf[NG];
       split(f[r], vf);
 #pragma unroll
@@ -536,9 +573,10 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs<T> da, GradArgs<T> d
 template <typename T, int R16, int EDGE>
 __device__ __forceinline__ void dx_segment(const DxArgs<T>& g, const OrderArgs& w, const Places& at, int slab, int k, int p0, int p1) {
   constexpr int CHUNKS = (R16 + 1) / 2, NT = Terms<T>::OUTPUT;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = wave_id(), m = lane & 15, q = lane >> 4;
   const int c0 = slab * 128 + m * 8, n = g.d - c0, per_row = (g.d + 7) >> 3;
   const bool none = k < 0;                                   // dx = base
+  const uint32_t with = none ? 0u : ~0u;
   Frag<T> af[CHUNKS][8];
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
@@ -547,7 +585,7 @@ __device__ __forceinline__ void dx_segment(const DxArgs<T>& g, const OrderArgs& 
     for (int j = 0; j < 8; ++j) {
       const int r = (c * 4 + q) * 8 + j;
       rows[j] = load_at<EDGE>(g.a, ((int64_t)(none ? 0 : k) * w.rank + min(r, w.rank - 1)) * g.d + c0, n, (int64_t)w.n_adapters * w.rank * g.d);
-      keep_first(rows[j], r < w.rank ? 8 : 0);
+      keep_all(rows[j], less_mask(r, w.rank));
     }
     transpose(rows, af[c]);
   }
@@ -584,7 +622,7 @@ __device__ __forceinline__ void dx_segment(const DxArgs<T>& g, const OrderArgs& 
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        o[e] = none ? 0.0f : out[e][i];
+        o[e] = keep(out[e][i], with);
         if (g.mask.kept) o[e] = __uint_as_float(__float_as_uint(o[e] * g.mask.scale) & (uint32_t)__builtin_amdgcn_sbfe(kept[i], e, 1));
       }
       if (g.base) {
@@ -671,7 +709,7 @@ static void launch_tiles(TileArgs<T> g, hipStream_t s) {
   const bool tiny = g.d_in < 8 || (EXPAND && std::min(g.tokens * g.d_out, (int64_t)g.n_adapters * g.d_out * g.rank) < 8);
   with_shape(g.rank, whole, tiny, [&](auto r, auto edge) {
     constexpr int R = decltype(r)::value, E = decltype(edge)::value;
-    const dim3 grid((unsigned)tiles, g.slices), block(R == 4 ? 512 : 1024);
+    const dim3 grid((unsigned)(scan ? tiles : (tiles + 7) / 8 * 8), g.slices, scan ? 1 : std::min(g.n_adapters, 2)), block(TILE_WAVES<R> * 64);
     if (scan) hipLaunchKernelGGL((tile_kernel<T, R, true, EXPAND, E>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((tile_kernel<T, R, false, EXPAND, E>), grid, block, 0, s, g);
   });
@@ -747,7 +785,7 @@ static void launch_adapters_backward(const cmoe_adapters_backward_args& p, const
 
 static int check_adapters(const char* what, int dtype, int64_t tokens, int d_in, int d_out, int rank, int n_adapters) {
   if (dtype != CMOE_F32 && dtype != CMOE_BF16) return fail(CMOE_EINVAL, "%s: dtype must be CMOE_F32 or CMOE_BF16", what);
-  if (d_in < 1 || d_out < 1 || d_in > (1 << 24) || d_out > (1 << 24)) return fail(CMOE_EINVAL, "%s: d_in and d_out must be 1 to 2^24", what);
+  if (d_in < 1 || d_out < 1 || d_in > MAX_WIDTH || d_out > MAX_WIDTH) return fail(CMOE_EINVAL, "%s: d_in and d_out must be 1 to %d", what, MAX_WIDTH);
   if (rank < 1 || rank > MAX_RANK) return fail(CMOE_EINVAL, "%s: rank must be 1 to %d", what, MAX_RANK);
   if (n_adapters < 1 || n_adapters > MAX_ADAPTERS) return fail(CMOE_EINVAL, "%s: n_adapters must be 1 to %d", what, MAX_ADAPTERS);
   if (tokens < 0 || tokens > (1 << 20)) return fail(CMOE_EINVAL, "%s: tokens must be 0 to 2^20", what);

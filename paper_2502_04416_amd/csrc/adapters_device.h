@@ -35,59 +35,102 @@ __device__ __forceinline__ Frag<float> load_frag(const float* p) {
   }
   return f;
 }
+// All ones where a < b (both far from the ends of the type).  Values are chosen by masks, not by conditions, throughout: of a condition on
+// loaded values the compiler made a branch for each, with a wait of its own.
+__device__ __forceinline__ uint32_t less_mask(int a, int b) { return (uint32_t)((a - b) >> 31); }
+__device__ __forceinline__ uint32_t choose(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
+
 // Values from the s-th on, zeros after the last (any s >= 0).
 __device__ __forceinline__ void shift_down(Frag<bf16_t>& f, int s) {
-  const bool four = s & 4, two = s & 2, one = s & 1;
-  f.w[0] = four ? f.w[2] : f.w[0];
-  f.w[1] = four ? f.w[3] : f.w[1];
-  f.w[2] = four ? 0u : f.w[2];
-  f.w[3] = four ? 0u : f.w[3];
+  const uint32_t four = less_mask(3, s & 4), two = less_mask(1, s & 2), one = less_mask(0, s & 1), any = less_mask(s, 8);
+  f.w[0] = choose(four, f.w[2], f.w[0]);
+  f.w[1] = choose(four, f.w[3], f.w[1]);
+  f.w[2] &= ~four;
+  f.w[3] &= ~four;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f.w[i] = two ? (i < 3 ? f.w[i + 1] : 0u) : f.w[i];
+  for (int i = 0; i < 4; ++i) f.w[i] = choose(two, i < 3 ? f.w[i + 1] : 0u, f.w[i]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f.w[i] = s > 7 ? 0u : one ? (f.w[i] >> 16) | (i < 3 ? f.w[i + 1] << 16 : 0u) : f.w[i];
+  for (int i = 0; i < 4; ++i) f.w[i] = choose(one, (f.w[i] >> 16) | (i < 3 ? f.w[i + 1] << 16 : 0u), f.w[i]) & any;
 }
 __device__ __forceinline__ void shift_down(Frag<float>& f, int s) {
+  const uint32_t any = less_mask(s, 8);
+  uint32_t w[8];
 #pragma unroll
-  for (int step = 4; step > 0; step >>= 1)
+  for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(f.w[e]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.w[e] = (s & step) ? (e + step < 8 ? f.w[e + step] : 0.0f) : f.w[e];
+  for (int step = 4; step > 0; step >>= 1) {
+    const uint32_t by = less_mask(0, s & step);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f.w[e] = s > 7 ? 0.0f : f.w[e];
+    for (int e = 0; e < 8; ++e) w[e] = choose(by, e + step < 8 ? w[e + step] : 0u, w[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.w[e] = __uint_as_float(w[e] & any);
 }
 // The first n values, zeros after them.
 __device__ __forceinline__ void keep_first(Frag<bf16_t>& f, int n) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) f.w[e] = n >= 2 * e + 2 ? f.w[e] : n == 2 * e + 1 ? f.w[e] & 0xffffu : 0u;
+  for (int e = 0; e < 4; ++e) f.w[e] &= choose(0xffffu, less_mask(2 * e, n), less_mask(2 * e + 1, n));
 }
 __device__ __forceinline__ void keep_first(Frag<float>& f, int n) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f.w[e] = e < n ? f.w[e] : 0.0f;
+  for (int e = 0; e < 8; ++e) f.w[e] = __uint_as_float(__float_as_uint(f.w[e]) & less_mask(e, n));
 }
+// All of them or zeros.
+__device__ __forceinline__ void keep_all(Frag<bf16_t>& f, uint32_t mask) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f.w[e] &= mask;
+}
+__device__ __forceinline__ void keep_all(Frag<float>& f, uint32_t mask) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.w[e] = __uint_as_float(__float_as_uint(f.w[e]) & mask);
+}
+__device__ __forceinline__ float keep(float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask); }
 
-// How the values `at` on of a buffer of `size` are read, of which n (it may be 0 or less, or more than 8) belong to the row:
+// How eight values of a row are read, of which n (it may be 0 or less, or more than 8) belong to it:
 //   WHOLE   rows are a multiple of eight values: n >= 8, or n <= 0 and the result is not used
 //   RAGGED  the buffer has eight values at least: eight that do not pass its end, moved into place, zeros from the n-th on
 //   TINY    one by one
 // The first two have no branch, so that a caller's loads are all in flight before the first is waited for.
 enum { WHOLE, RAGGED, TINY };
-template <int EDGE, typename T>
-__device__ __forceinline__ Frag<T> load_at(const T* p, int64_t at, int n, int64_t size) {
-  if constexpr (EDGE == WHOLE) return load_frag(p + (n > 0 ? at : 0));
-  if constexpr (EDGE == RAGGED) {
-    const int64_t from = n > 0 ? min(at, size - 8) : 0;
-    Frag<T> f = load_frag(p + from);
-    shift_down(f, n > 0 ? (int)(at - from) : 8);
-    keep_first(f, n);
-    return f;
-  }
+
+template <typename T>
+__device__ __forceinline__ Frag<T> load_tiny(const T* p, int n) {
   Frag<T> f = {};
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if (e >= n) continue;
-    if constexpr (sizeof(T) == 2) f.w[e >> 1] |= (uint32_t)p[at + e] << (16 * (e & 1));
-    else f.w[e] = p[at + e];
+    if constexpr (sizeof(T) == 2) f.w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+    else f.w[e] = p[e];
   }
+  return f;
+}
+
+// From an address that is the same for the whole wave and an offset of the lane (values, below 2^31 bytes): one register, where a
+// 64-bit address of its own for every load under way took more than the loads' results.  left: from base to the buffer's end.
+template <typename T>
+__device__ __forceinline__ Frag<T> load_from(const T* base, uint32_t at) {
+  return load_frag(reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + (uint32_t)(at * sizeof(T))));
+}
+template <int EDGE, typename T>
+__device__ __forceinline__ Frag<T> load_near(const T* base, int at, int n, int64_t left) {
+  if constexpr (EDGE == TINY) return load_tiny(base + at, n);
+  const int last = (int)min(left - 8, (int64_t)0x40000000), from = min(at, last);
+  if constexpr (EDGE == WHOLE) return load_from(base, (uint32_t)from);
+  Frag<T> f = load_frag(base + from);
+  shift_down(f, at - from);
+  keep_first(f, n);
+  return f;
+}
+
+// From any place of a buffer of `size` values.
+template <int EDGE, typename T>
+__device__ __forceinline__ Frag<T> load_at(const T* p, int64_t at, int n, int64_t size) {
+  if constexpr (EDGE == TINY) return load_tiny(p + at, n);
+  if constexpr (EDGE == WHOLE) return load_frag(p + (n > 0 ? at : 0));
+  const int64_t from = n > 0 ? min(at, size - 8) : 0;
+  Frag<T> f = load_frag(p + from);
+  shift_down(f, n > 0 ? (int)(at - from) : 8);
+  keep_first(f, n);
   return f;
 }
 
@@ -133,6 +176,25 @@ __device__ __forceinline__ void kept_bits(const Drop& d, uint32_t (&kept)[N], F&
     }
     kept[i] = bits;
   }
+}
+
+// A load whose neighbouring lanes are on different rows moves 18 bytes a cycle into a CU, one whose lanes 4 r to 4 r + 3 hold row r's four
+// chunks 55 (measured, from the L2 cache): so rows are loaded and stored in the second order and exchanged with the operands', 16 q + r,
+// between the lanes.
+struct Lanes {
+  int operand, rows;      // byte addresses of the lanes to take from
+};
+__device__ __forceinline__ Lanes lane_orders() {
+  const int l = threadIdx.x & 63;
+  return Lanes{((l & 15) * 4 + (l >> 4)) * 4, ((l & 3) * 16 + (l >> 2)) * 4};
+}
+template <typename T>
+__device__ __forceinline__ Frag<T> exchange(const Frag<T>& f, int from) {
+  Frag<T> out;
+#pragma unroll
+  for (int e = 0; e < (int)(sizeof(f.w) / 4); ++e)
+    out.w[e] = __builtin_bit_cast(decltype(f.w[0] + f.w[0]), __builtin_amdgcn_ds_bpermute(from, __builtin_bit_cast(int, f.w[e])));
+  return out;
 }
 
 // Eight rows of eight values to eight columns.
@@ -194,6 +256,30 @@ __device__ __forceinline__ void unpack(const Frag<bf16_t>& f, float (&v)[8]) {
 __device__ __forceinline__ void unpack(const Frag<float>& f, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = f.w[e];
+}
+
+// Eight values as they are stored.
+__device__ __forceinline__ void pack(const float (&v)[8], Frag<bf16_t>& f) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f.w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+}
+__device__ __forceinline__ void pack(const float (&v)[8], Frag<float>& f) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.w[e] = v[e];
+}
+template <int EDGE>
+__device__ __forceinline__ void store_frag(bf16_t* p, int n, const Frag<bf16_t>& f) {
+  if (n >= 8 || (EDGE == WHOLE && n > 0)) {
+    *reinterpret_cast<Bytes16<bf16_t>*>(p) = __builtin_bit_cast(Bytes16<bf16_t>, f);
+  } else if (EDGE != WHOLE) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = (bf16_t)(f.w[e >> 1] >> (16 * (e & 1)));
+  }
+}
+template <int EDGE>
+__device__ __forceinline__ void store_frag(float* p, int n, const Frag<float>& f) {
+  if (n > 0) store8(p, EDGE == WHOLE ? 8 : n, f.w);
 }
 
 // Eight values to a row of which n are left.
