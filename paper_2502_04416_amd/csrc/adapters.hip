@@ -11,7 +11,7 @@
 
 #include "../../include/cmoe.h"
 #include "cmoe_internal.h"
-#include "adapters_device.h"
+#include "fragments_device.h"
 #include "operator_args.h"
 
 namespace cmoe {
@@ -689,7 +689,7 @@ static void with_rank(int rank, F&& f) {
   else f(std::integral_constant<int, 4>{});
 }
 
-// f(R16, EDGE): ... and how rows end (adapters_device.h).  A width or buffer below eight values is nothing to be fast at: one form.
+// f(R16, EDGE): ... and how rows end (fragments_device.h).  A width or buffer below eight values is nothing to be fast at: one form.
 template <typename F>
 static void with_shape(int rank, bool whole, bool tiny, F&& f) {
   if (tiny) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, TINY>{});

@@ -1,4 +1,4 @@
-// Operands of the matrix instructions for the adapters: eight values of a row per lane, in registers.
+// Eight values of a row per lane, in registers as they are stored: how rows are read and written, and operands of the matrix instructions.
 #pragma once
 #include "dropout_device.h"
 

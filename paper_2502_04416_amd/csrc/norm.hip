@@ -10,7 +10,7 @@
 
 #include "../../include/cmoe.h"
 #include "cmoe_internal.h"
-#include "dropout_device.h"
+#include "fragments_device.h"
 #include "operator_args.h"
 
 namespace cmoe {
@@ -47,7 +47,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[16]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave64_sum(v[i]);
     if constexpr (LANES > 64) {
-      const int wave = threadIdx.x >> 6;
+      const int wave = threadIdx.x >> 6, first = threadIdx.x / LANES * (LANES / 64);
       if ((threadIdx.x & 63) == 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) part[i][wave] = v[i];
@@ -55,9 +55,9 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*part)[16]) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        v[i] = part[i][0];
+        v[i] = part[i][first];
 #pragma unroll
-        for (int w = 1; w < LANES / 64; ++w) v[i] += part[i][w];
+        for (int w = 1; w < LANES / 64; ++w) v[i] += part[i][first + w];
       }
     }
   }
@@ -174,85 +174,133 @@ struct NormBackward {
   Drop drop;
 };
 
-// The same threads per row; a workgroup takes every grid'th set of rows and keeps its share of the sums over rows in registers, in
-// the same columns for every row, so the sums over rows cost one row of partial sums per workgroup.
-template <typename T, int LANES, int CH, bool LAYER>
+// Rows of a workgroup; the threads of a row are LANES, those of a workgroup 256 at least.
+template <int LANES>
+constexpr int BACKWARD_ROWS = LANES >= 256 ? 1 : 256 / LANES;
+
+// A workgroup takes every grid'th set of rows and keeps its share of the sums over rows in registers, in the same columns for every row,
+// so the sums over rows cost one row of partial sums per workgroup.  All that a row reads is loaded while the row before it is worked
+// on: a row has a reduction in its middle, which nothing else would cover (4096 rows of 4096, bf16, all operands: 59 -> 32 us, 168 MB at
+// 5.3 TB/s).  With more than one chunk per thread there are no registers for that, nor for the weights.
+template <typename T, int LANES, int CH, bool LAYER, int EDGE>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_backward_kernel(NormBackward<T> a) {
-  constexpr int ROWS = LANES >= 256 ? 1 : 256 / LANES;
+  constexpr int ROWS = BACKWARD_ROWS<LANES>;
+  constexpr bool AHEAD = CH == 1;
   __shared__ float part[2][2][16];
+  __shared__ float joined[ROWS > 1 ? 2 : 1][ROWS > 1 ? 2048 : 1];
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
   const int per_row = (a.cols + 7) >> 3;
+  const int64_t size = a.rows * a.cols;
   const float inv_cols = 1.0f / a.cols;
-  float dw[CH][8], db[CH][8];
+  float dw[CH][8], db[CH][8], w[8];
 #pragma unroll
-  for (int i = 0; i < CH; ++i)
+  for (int i = 0; i < CH; ++i) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.0f;
-  int buffer = 0;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + group; row < a.rows; row += (int64_t)gridDim.x * ROWS, buffer ^= 1) {
-    const int64_t base = row * a.cols;
-    const float mean = a.mean ? a.mean[row] : 0.0f, rstd = a.rstd[row];
-    float g[CH][8], h[CH][8], t[2] = {0.0f, 0.0f};
+  }
+  auto load_weight = [&](int i) {
+    const int c = (i * LANES + lane) * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = 1.0f;
+    if (a.w) unpack(load_at<EDGE>(a.w, c, a.cols - c, a.cols), w);
+  };
+  if (AHEAD) load_weight(0);
+  Frag<T> dy[CH], s[CH], dsum[CH];
+  float mean = 0.0f, rstd = 0.0f;
+  auto load = [&](int64_t row) {
+    row = min(row, a.rows - 1);
+    if (LAYER) mean = a.mean[row];
+    rstd = a.rstd[row];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int c = i * LANES + lane;
+      const int c = (i * LANES + lane) * 8, n = a.cols - c;
+      dy[i] = load_at<EDGE>(a.dy, row * a.cols + c, n, size);
+      s[i] = load_at<EDGE>(a.s, row * a.cols + c, n, size);
+      if (a.dsum) dsum[i] = load_at<EDGE>(a.dsum, row * a.cols + c, n, size);
+    }
+  };
+  int buffer = 0;
+  int64_t row0 = (int64_t)blockIdx.x * ROWS;
+  if (AHEAD) load(row0 + group);
+  for (; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS, buffer ^= 1) {
+    const int64_t row = row0 + group;
+    const bool valid = row < a.rows;
+    if (!AHEAD) load(row);
+    const float r = rstd;
+    float g[CH][8], h[CH][8], t[2] = {0.0f, 0.0f};
+    Frag<T> past[CH];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[i][e] = h[i][e] = 0.0f;
-      if (c < per_row) {
-        const int n = a.cols - c * 8;
-        float w[8];
-        load8(a.dy + base + c * 8, n, g[i]);
-        load8(a.s + base + c * 8, n, h[i]);
-        if (a.w) load8(a.w + c * 8, n, w);
+    for (int i = 0; i < CH; ++i) {
+      const int n = valid ? a.cols - (i * LANES + lane) * 8 : 0;
+      keep_first(dy[i], n);
+      keep_first(s[i], n);
+      unpack(dy[i], g[i]);
+      unpack(s[i], h[i]);
+      past[i] = dsum[i];
+      if (!AHEAD) load_weight(i);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          h[i][e] = e < n ? (h[i][e] - mean) * rstd : 0.0f;
-          dw[i][e] += g[i][e] * h[i][e];
-          db[i][e] += g[i][e];
-          if (a.w) g[i][e] *= w[e];
-          t[0] += g[i][e] * h[i][e];
-          t[1] += g[i][e];
-        }
+      for (int e = 0; e < 8; ++e) {
+        h[i][e] = (h[i][e] - mean) * r;
+        dw[i][e] += g[i][e] * h[i][e];
+        db[i][e] += g[i][e];
+        g[i][e] *= w[e];
+        t[0] += g[i][e] * h[i][e];
+        t[1] += g[i][e];
       }
     }
+    if (AHEAD) load(row0 + (int64_t)gridDim.x * ROWS + group);
     row_sums<LANES>(t, part[buffer]);
     const float mgh = t[0] * inv_cols, mg = LAYER ? t[1] * inv_cols : 0.0f;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int c = i * LANES + lane;
-      if (c >= per_row) continue;
-      const int n = a.cols - c * 8;
-      float o[8];
-      if (a.dsum) load8(a.dsum + base + c * 8, n, o);
+      const int c = i * LANES + lane, n = a.cols - c * 8;
+      float o[8], past_f[8];
+      unpack(past[i], past_f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = (g[i][e] - mg - h[i][e] * mgh) * rstd;
-        o[e] = a.dsum ? d + o[e] : d;
+        o[e] = (g[i][e] - mg - h[i][e] * mgh) * r;
+        if (a.dsum) o[e] += past_f[e];
       }
-      if (a.dresidual) store8(a.dresidual + base + c * 8, n, o);
+      if (!valid || n <= 0) continue;
+      const int64_t at = row * a.cols + c * 8;
+      if (a.dresidual) store_at<EDGE>(a.dresidual + at, n, o);
       if (a.drop.limit) drop8(o, a.drop, (uint64_t)row * per_row + c);
-      store8(a.dx + base + c * 8, n, o);
+      store_at<EDGE>(a.dx + at, n, o);
     }
   }
   if (!a.partials) return;
-  // one row of partial sums per set of LANES threads
-  float* p = a.partials + ((int64_t)blockIdx.x * ROWS + group) * a.sums * a.cols;
+  float* p = a.partials + (int64_t)blockIdx.x * a.sums * a.cols;
+  if constexpr (ROWS > 1) {
+    // the groups' sums, added in their order by the first
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      joined[0][(group * LANES + lane) * 8 + e] = dw[0][e];
+      joined[1][(group * LANES + lane) * 8 + e] = db[0][e];
+    }
+    __syncthreads();
+    if (group > 0) return;
+    for (int k = 1; k < ROWS; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dw[0][e] += joined[0][(k * LANES + lane) * 8 + e];
+        db[0][e] += joined[1][(k * LANES + lane) * 8 + e];
+      }
+  }
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
-    const int c = i * LANES + lane;
-    if (c >= per_row) continue;
-    store8(p + c * 8, a.cols - c * 8, dw[i]);
-    if (a.sums == 2) store8(p + a.cols + c * 8, a.cols - c * 8, db[i]);
+    const int c = (i * LANES + lane) * 8;
+    store_at<RAGGED>(p + c, a.cols - c, dw[i]);
+    if (a.sums == 2) store_at<RAGGED>(p + a.cols + c, a.cols - c, db[i]);
   }
 }
 
-// out[c] = the sum of n rows of partial sums, in their order: 64 columns per workgroup, each wave a quarter of the rows.
-__global__ __launch_bounds__(256) void sum_rows_kernel(const float* __restrict__ partials, int n, int cols, int sums, float* dw, float* dbias) {
-  __shared__ float part[4][64];
+// out[c] = the sum of n rows of partial sums, in a fixed order: 64 columns per workgroup, each wave a sixteenth of the rows.
+__global__ __launch_bounds__(1024) void sum_rows_kernel(const float* __restrict__ partials, int n, int cols, int sums, float* dw, float* dbias) {
+  __shared__ float part[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int which = blockIdx.y;
   const int c = blockIdx.x * 64 + lane;
-  const int per = (n + 3) / 4, first = wave * per, last = min(n, first + per);
+  const int per = (n + 15) / 16, first = wave * per, last = min(n, first + per);
   float t = 0.0f;
   if (c < cols) {
     const float* p = partials + (int64_t)which * cols + c;
@@ -261,7 +309,9 @@ __global__ __launch_bounds__(256) void sum_rows_kernel(const float* __restrict__
   }
   part[wave][lane] = t;
   __syncthreads();
-  if (wave == 0 && c < cols) (which ? dbias : dw)[c] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+  if (wave > 0 || c >= cols) return;
+  for (int k = 1; k < 16; ++k) t += part[k][lane];
+  (which ? dbias : dw)[c] = t;
 }
 
 // Threads per row and chunks per thread.
@@ -296,9 +346,40 @@ static void with_norm_shape(int cols, F&& f) {
 
 static int rows_per_block(int lanes) { return lanes >= 256 ? 1 : 256 / lanes; }
 
+// The backward pass keeps the columns' sums beside what it loads ahead: one chunk per thread as long as a workgroup has the threads.
+static NormShape backward_shape(int cols) {
+  const int per_row = (cols + 7) / 8;
+  for (const int lanes : {16, 64, 128, 256, 512, 1024})
+    if (per_row <= lanes) return {lanes, 1};
+  return {1024, per_row <= 2048 ? 2 : 4};
+}
+
+// f(lanes, chunks, edge)
+template <typename F>
+static void with_backward_shape(int cols, F&& f) {
+  const NormShape s = backward_shape(cols);
+  const auto whole = std::integral_constant<int, WHOLE>{};
+  const auto ragged = std::integral_constant<int, RAGGED>{};
+  if (cols < 8) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, TINY>{});
+#define CMOE_NORM_SHAPE(L, C) \
+  if (s.lanes == L && s.chunks == C) { \
+    if (cols % 8 == 0) return f(std::integral_constant<int, L>{}, std::integral_constant<int, C>{}, whole); \
+    return f(std::integral_constant<int, L>{}, std::integral_constant<int, C>{}, ragged); \
+  }
+  CMOE_NORM_SHAPE(16, 1)
+  CMOE_NORM_SHAPE(64, 1)
+  CMOE_NORM_SHAPE(128, 1)
+  CMOE_NORM_SHAPE(256, 1)
+  CMOE_NORM_SHAPE(512, 1)
+  CMOE_NORM_SHAPE(1024, 1)
+  CMOE_NORM_SHAPE(1024, 2)
+  CMOE_NORM_SHAPE(1024, 4)
+#undef CMOE_NORM_SHAPE
+}
+
 // Workgroups of the backward pass: enough to fill the chip, few enough that their partial sums stay small beside the rows.
 static int backward_blocks(int64_t rows, int cols) {
-  const int per = rows_per_block(norm_shape(cols).lanes);
+  const int per = rows_per_block(backward_shape(cols).lanes);
   return (int)std::min<int64_t>((rows + per - 1) / per, 512);
 }
 
@@ -319,11 +400,11 @@ template <typename T>
 static void launch_backward(const cmoe_norm_backward_args& p, const Drop& drop, int blocks, hipStream_t s) {
   const NormBackward<T> a{(const T*)p.dy, (const T*)p.s, (const T*)p.dsum, (const T*)p.weight, p.form == CMOE_NORM_LAYER ? p.mean : nullptr, p.rstd,
                           (T*)p.dx, (T*)p.dresidual, p.dweight ? (float*)p.workspace : nullptr, p.rows, p.cols, p.dbias ? 2 : 1, drop};
-  with_norm_shape(p.cols, [&](auto lanes, auto chunks) {
-    constexpr int L = decltype(lanes)::value, C = decltype(chunks)::value;
+  with_backward_shape(p.cols, [&](auto lanes, auto chunks, auto edge) {
+    constexpr int L = decltype(lanes)::value, C = decltype(chunks)::value, E = decltype(edge)::value;
     const dim3 grid((unsigned)blocks), block(L > 256 ? L : 256);
-    if (p.form == CMOE_NORM_LAYER) hipLaunchKernelGGL((norm_backward_kernel<T, L, C, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((norm_backward_kernel<T, L, C, false>), grid, block, 0, s, a);
+    if (p.form == CMOE_NORM_LAYER) hipLaunchKernelGGL((norm_backward_kernel<T, L, C, true, E>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((norm_backward_kernel<T, L, C, false, E>), grid, block, 0, s, a);
   });
 }
 
@@ -362,7 +443,7 @@ extern "C" int cmoe_norm_forward(const cmoe_norm_forward_args* p, void* hip_stre
 extern "C" size_t cmoe_norm_backward_workspace_bytes(int64_t rows, int32_t cols) {
   using namespace cmoe;
   if (rows < 0 || cols < 1 || cols > NORM_MAX_COLS) return 0;
-  return (size_t)backward_blocks(rows, cols) * rows_per_block(norm_shape(cols).lanes) * 2 * cols * sizeof(float);
+  return (size_t)backward_blocks(rows, cols) * 2 * cols * sizeof(float);
 }
 
 extern "C" int cmoe_norm_backward(const cmoe_norm_backward_args* p, void* hip_stream) {
@@ -389,8 +470,8 @@ extern "C" int cmoe_norm_backward(const cmoe_norm_backward_args* p, void* hip_st
   const int blocks = backward_blocks(p->rows, p->cols);
   if (blocks > 0) p->dtype == CMOE_BF16 ? launch_backward<bf16_t>(*p, drop, blocks, s) : launch_backward<float>(*p, drop, blocks, s);
   if (p->dweight)      // (no rows: the sums are zeros)
-    hipLaunchKernelGGL(sum_rows_kernel, dim3((p->cols + 63) / 64, p->dbias ? 2 : 1), dim3(256), 0, s, (const float*)p->workspace,
-                       blocks * rows_per_block(norm_shape(p->cols).lanes), p->cols, p->dbias ? 2 : 1, p->dweight, p->dbias);
+    hipLaunchKernelGGL(sum_rows_kernel, dim3((p->cols + 63) / 64, p->dbias ? 2 : 1), dim3(1024), 0, s, (const float*)p->workspace,
+                       blocks, p->cols, p->dbias ? 2 : 1, p->dweight, p->dbias);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CMOE_OK : fail(CMOE_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
