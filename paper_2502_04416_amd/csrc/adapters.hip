@@ -63,30 +63,30 @@ constexpr int TILE_WAVES = R16 == 1 ? 16 : 8;
 template <typename T, int R16>
 constexpr int UNITS_AT_ONCE = sizeof(T) == 4 || R16 == 4 ? 1 : R16 == 2 ? 4 : 2;
 
-// A tile is 16 tokens.  Its workgroup first contracts x with the adapter's rows: the waves take turns along the width, 64 values each
+// A tile is 16 MT tokens.  Its workgroup first contracts x with the adapter's rows: the waves take turns along the width, 64 values each
 // time, each a part of its own, and their sums meet in LDS; then each wave expands u to its own columns, on to base, straight from memory to memory.
 // SCAN: workgroup b is for the adapter of token b, if b is the first of its adapter's tokens or the 16th, 32nd ... after it; it finds
 // up to 16 of them itself.  Weights are then read once per 16 tokens of an adapter whatever the order, as decode batches need it,
-// where every token may have another.  Otherwise 16 consecutive tokens, and one pass for each adapter among them, shared by gridDim.z
+// where every token may have another.  Otherwise consecutive tokens, and one pass for each adapter among them, shared by gridDim.z
 // workgroups: prompts and training batches come as runs, so that most tiles have one, and the tiles with two are not the last to end.
 // A row or column of a product that is no token, rank or column of y reads another's values, and its results are not used: a token
 // does not see what another's adapter holds.
 // Without EXPAND: u * scale alone (v of the backward pass).
-template <typename T, int R16, bool SCAN, bool EXPAND, int EDGE>
+template <typename T, int R16, int MT, bool SCAN, bool EXPAND, int EDGE>
 __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_kernel(TileArgs<T> g) {
-  constexpr int WAVES = TILE_WAVES<R16>;
+  constexpr int WAVES = TILE_WAVES<R16>, M = 16 * MT;
   constexpr int CHUNKS = (R16 + 1) / 2;                      // operands along the rank
   constexpr int NT = Terms<T>::OUTPUT;
   constexpr int LD = CHUNKS * 32 + 16 / sizeof(T);
-  __shared__ float sums[WAVES][R16 * 4 * 64];
-  __shared__ __align__(16) T us[EXPAND ? NT : 1][16][LD];    // scale * u, in terms
-  __shared__ int token[16], id[16], found[16], counts[2][16], n_found;
+  __shared__ float sums[WAVES][MT * R16 * 4 * 64];
+  __shared__ __align__(16) T us[EXPAND ? NT : 1][M][LD];    // scale * u, in terms
+  __shared__ int token[M], id[M], found[M], counts[2][16], n_found;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), m = lane & 15, q = lane >> 4;
   const int row = lane >> 2, part_q = lane & 3;              // row and chunk of a lane as rows are loaded and stored
   const Lanes lanes = lane_orders();
   // Consecutive tiles on one XCD (workgroups go to the eight in turn): they share adapters, which stay in its L2 cache.
   const int per_xcd = (gridDim.x + 7) >> 3, tile = SCAN ? (int)blockIdx.x : (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if (!SCAN && (int64_t)tile * 16 >= g.tokens) return;
+  if (!SCAN && (int64_t)tile * M >= g.tokens) return;
   const int z = gridDim.z - 1 - blockIdx.z;                  // (the few tiles with a second adapter begin with it)
   if (SCAN) {
     const int me = blockIdx.x;
@@ -117,19 +117,20 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
       n_found = k >= 0;
     }
   } else if (tid < 64) {
-    const int64_t t = (int64_t)tile * 16 + m;
+    const int place = lane & (M - 1);
+    const int64_t t = (int64_t)tile * M + place;
     const bool valid = t < g.tokens;
     const int k = valid ? adapter_of(g.ids, t, g.n_adapters) : -2;
-    bool first = k >= 0 && lane < 16;
+    bool first = k >= 0 && lane < M;
 #pragma unroll
-    for (int i = 0; i < 15; ++i) {
+    for (int i = 0; i < M - 1; ++i) {
       const int other = __shfl(k, i, 64);                    // (by all lanes, before the comparison)
-      first = first && !(i < m && other == k);
+      first = first && !(i < place && other == k);
     }
     const uint64_t votes = __ballot(first);
-    if (lane < 16) {
-      token[m] = valid ? m : (int)(g.tokens - 1 - (int64_t)tile * 16);
-      id[m] = k;
+    if (lane < M) {
+      token[place] = valid ? place : (int)(g.tokens - 1 - (int64_t)tile * M);
+      id[place] = k;
     }
     if (first) found[__popcll(votes & ((1ull << lane) - 1))] = k;
     if (lane == 0) n_found = __popcll(votes);
@@ -137,8 +138,11 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
   if (EXPAND && R16 == 1)                                    // (an operand is 32 values along the rank)
     for (int i = tid; i < (int)sizeof(us) / 4; i += WAVES * 64) reinterpret_cast<uint32_t*>(us)[i] = 0;
   __syncthreads();
-  const int64_t t0 = SCAN ? 0 : (int64_t)tile * 16;
-  const int my_token = token[m], my_id = id[m], row_token = token[row], row_id = id[row], n_distinct = __builtin_amdgcn_readfirstlane(n_found);
+  const int64_t t0 = SCAN ? 0 : (int64_t)tile * M;
+  const int n_distinct = __builtin_amdgcn_readfirstlane(n_found);
+  int row_token[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) row_token[t] = token[t * 16 + row];
 
   // What the expansion reads, UNITS units of 32 columns of y at a time (past the wave's last unit: its values).
   constexpr int UNITS = UNITS_AT_ONCE<T, R16>;
@@ -146,15 +150,16 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
   const int part = blockIdx.y * WAVES + wave, parts = g.slices * WAVES;
   const int first = (int)((int64_t)units * part / parts), last = (int)((int64_t)units * (part + 1) / parts);      // of the wave
   const int64_t y_size = g.tokens * g.d_out, b_size = (int64_t)g.n_adapters * g.d_out * g.rank;
-  const int y_at = row_token * g.d_out + part_q * 8, b_at = ((row >> 2) * 8 + (row & 3)) * g.rank + part_q * 8;
+  const int b_at = ((row >> 2) * 8 + (row & 3)) * g.rank + part_q * 8;
   const T* base = g.base ? g.base : g.y;                     // (without one the values are not used)
-  auto load_units = [&](int unit, int k, Frag<T> (&basef)[UNITS], Frag<T> (&bf)[UNITS][2][CHUNKS]) {
-    const int y_here = here(y_at), b_here = here(b_at);
+  auto load_units = [&](int unit, int k, Frag<T> (&basef)[UNITS][MT], Frag<T> (&bf)[UNITS][2][CHUNKS]) {
+    const int b_here = here(b_at);
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
       const int o0 = min(unit + i, last - 1) * 32;
       const int64_t y0 = t0 * g.d_out + o0, b0 = ((int64_t)max(k, 0) * g.d_out + o0) * g.rank;
-      basef[i] = load_near<EDGE>(base + y0, y_here, g.d_out - o0 - part_q * 8, y_size - y0);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) basef[i][t] = load_near<EDGE>(base + y0, here(row_token[t]) * g.d_out + part_q * 8, g.d_out - o0 - part_q * 8, y_size - y0);
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -163,7 +168,7 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
   };
 
   // Turns along the width are DEPTH at a time; past the wave's last turn its values, as zeros.
-  constexpr int DEPTH = R16 == 1 && sizeof(T) == 2 ? 4 : R16 == 4 || sizeof(T) == 2 ? 2 : 1;
+  constexpr int DEPTH = MT > 1 ? 1 : R16 == 1 && sizeof(T) == 2 ? 4 : R16 == 4 || sizeof(T) == 2 ? 2 : 1;
   const int full = g.d_in / 64;                              // whole turns
   const int turns = (full + WAVES - 1) / WAVES, turn0 = min(wave * turns, full), turn1 = min(turn0 + turns, full);
   auto turn = [&](int s, int i) { return min(s + (i >> 1), turn1 - 1) * 64 + (i & 1) * 32; };
@@ -176,70 +181,95 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
       const float scale = g.scale[k];
       const T* x = g.x + t0 * g.d_in;
       const T* a = g.a + (int64_t)k * g.rank * g.d_in;
-      const int x_at = here(row_token * g.d_in + part_q * 8);
+      int x_at[MT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) x_at[t] = here(row_token[t] * g.d_in + part_q * 8);
       int a_at[R16];
 #pragma unroll
       for (int r = 0; r < R16; ++r) a_at[r] = here(min(r * 16 + row, g.rank - 1) * g.d_in + part_q * 8);
-      const uint64_t chunk0 = (uint64_t)(t0 + here(row_token)) * ((g.d_in + 7) >> 3) + part_q;
-      f32x4 acc[R16];
+      auto chunk0 = [&](int t) { return (uint64_t)(t0 + here(row_token[t])) * ((g.d_in + 7) >> 3) + part_q; };
+      f32x4 acc[MT][R16];
 #pragma unroll
-      for (int r = 0; r < R16; ++r) acc[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      Frag<T> xf[2 * DEPTH];
-      auto load_x = [&](int s) {
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int i = 0; i < 2 * DEPTH; ++i) xf[i] = load_from(x + turn(s, i), x_at);
-      };
+        for (int r = 0; r < R16; ++r) acc[t][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
       for (int s = turn0; s < turn1; s += DEPTH) {
-        load_x(s);
-        Frag<T> af[2 * DEPTH][R16];
+        Frag<T> xf[MT][2 * DEPTH], af[2 * DEPTH][R16];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int i = 0; i < 2 * DEPTH; ++i) xf[t][i] = load_from(x + turn(s, i), x_at[t]);
 #pragma unroll
         for (int i = 0; i < 2 * DEPTH; ++i)
 #pragma unroll
           for (int r = 0; r < R16; ++r) af[i][r] = load_from(a + turn(s, i), a_at[r]);
         if (g.drop.limit) {
-          uint32_t kept[(DEPTH + 1) / 2];
-          kept_bits(g.drop, kept, [&](int j) { return chunk0 + (turn(s, j) >> 3); });
-          mask_frags(xf, kept);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            uint32_t kept[(DEPTH + 1) / 2];
+            const uint64_t chunk = chunk0(t);
+            kept_bits(g.drop, kept, [&](int j) { return chunk + (turn(s, j) >> 3); });
+            mask_frags(xf[t], kept);
+          }
         }
 #pragma unroll
         for (int i = 0; i < 2 * DEPTH; ++i) {
-          if (i > 1) keep_all(xf[i], less_mask(s + (i >> 1), turn1));
-          const Frag<T> xo = exchange(xf[i], lanes.operand);
+          Frag<T> xo[MT];
 #pragma unroll
-          for (int r = 0; r < R16; ++r) mma(acc[r], xo, exchange(af[i][r], lanes.operand));
+          for (int t = 0; t < MT; ++t) {
+            if (i > 1) keep_all(xf[t][i], less_mask(s + (i >> 1), turn1));
+            xo[t] = exchange(xf[t][i], lanes.operand);
+          }
+#pragma unroll
+          for (int r = 0; r < R16; ++r) {
+            const Frag<T> ao = exchange(af[i][r], lanes.operand);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) mma(acc[t][r], xo[t], ao);
+          }
         }
       }
       if (wave == WAVES - 1 && (g.d_in & 63)) {             // the rest of the width
-        Frag<T> xr[2], ar[2][R16];
+        Frag<T> ar[2][R16];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = full * 64 + h * 32, n = g.d_in - at - part_q * 8;
-          xr[h] = load_near<EDGE>(x + at, x_at, n, (g.tokens - t0) * g.d_in - at);
 #pragma unroll
           for (int r = 0; r < R16; ++r) {
             ar[h][r] = load_near<EDGE>(a + at, a_at[r], n, (int64_t)(g.n_adapters - k) * g.rank * g.d_in - at);
             keep_first(ar[h][r], n);
           }
-          keep_first(xr[h], n);
-        }
-        if (g.drop.limit) {
-          uint32_t kept[1];
-          kept_bits(g.drop, kept, [&](int j) { return chunk0 + full * 8 + (j & 1) * 4; });
-          mask_frags(xr, kept);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int t = 0; t < MT; ++t) {
+          Frag<T> xr[2];
 #pragma unroll
-          for (int r = 0; r < R16; ++r) mma(acc[r], exchange(xr[h], lanes.operand), exchange(ar[h][r], lanes.operand));
+          for (int h = 0; h < 2; ++h) {
+            const int at = full * 64 + h * 32, n = g.d_in - at - part_q * 8;
+            xr[h] = load_near<EDGE>(x + at, x_at[t], n, (g.tokens - t0) * g.d_in - at);
+            keep_first(xr[h], n);
+          }
+          if (g.drop.limit) {
+            uint32_t kept[1];
+            const uint64_t chunk = chunk0(t);
+            kept_bits(g.drop, kept, [&](int j) { return chunk + full * 8 + (j & 1) * 4; });
+            mask_frags(xr, kept);
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < R16; ++r) mma(acc[t][r], exchange(xr[h], lanes.operand), exchange(ar[h][r], lanes.operand));
+        }
       }
 #pragma unroll
-      for (int r = 0; r < R16; ++r)
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sums[wave][(r * 4 + i) * 64 + lane] = acc[r][i];
+        for (int r = 0; r < R16; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sums[wave][((t * R16 + r) * 4 + i) * 64 + lane] = acc[t][r][i];
       __syncthreads();
-      for (int v = tid; v < R16 * 256; v += WAVES * 64) {
-        const int l = v & 63, row = (l >> 4) * 4 + ((v >> 6) & 3), col = (v >> 8) * 16 + (l & 15);
+      for (int v = tid; v < MT * R16 * 256; v += WAVES * 64) {
+        const int l = v & 63, row = v / (R16 * 256) * 16 + (l >> 4) * 4 + ((v >> 6) & 3), col = (v >> 8) % R16 * 16 + (l & 15);
         float t = sums[0][v];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) t += sums[w][v];
@@ -261,59 +291,70 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
       __syncthreads();
     }
     if (f == 0 && g.u && blockIdx.y == 0)
-      for (int v = tid; v < 16 * g.ldu; v += WAVES * 64)
+      for (int v = tid; v < M * g.ldu; v += WAVES * 64)
         if (id[v / g.ldu] == -1) g.u[(t0 + token[v / g.ldu]) * g.ldu + v % g.ldu] = 0.0f;
     if (!EXPAND) continue;
 
     // y: rows are 16 columns of y, columns are tokens, the contracted axis the rank.  Two products' rows are dealt so that a lane ends
     // with eight consecutive columns of its token.
-    Frag<T> uf[CHUNKS][NT];
+    Frag<T> uf[MT][CHUNKS][NT];
+    uint32_t has[MT];
+    bool stores[MT];
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
+    for (int t = 0; t < MT; ++t) {
 #pragma unroll
-      for (int p = 0; p < NT; ++p) uf[c][p] = *reinterpret_cast<const Frag<T>*>(&us[p][m][(c * 4 + q) * 8]);
-    const uint32_t has = my_id == k && k >= 0 ? ~0u : 0u, has_base = g.base ? ~0u : 0u;
+      for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int p = 0; p < NT; ++p) uf[t][c][p] = *reinterpret_cast<const Frag<T>*>(&us[p][t * 16 + m][(c * 4 + q) * 8]);
+      const int row_id = id[t * 16 + row];
+      has[t] = id[t * 16 + m] == k && k >= 0 ? ~0u : 0u;
+      stores[t] = row_id == k || (f == 0 && row_id == -1);
+    }
+    const uint32_t has_base = g.base ? ~0u : 0u;
     uint32_t along[CHUNKS];                                  // chunks of the rank
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) along[c] = less_mask((c * 4 + part_q) * 8, g.rank);
-    const bool stores = row_id == k || (f == 0 && row_id == -1);
-    const int y_store = here(y_at);
 #pragma unroll 1
     for (int unit = first; unit < last; unit += UNITS) {
-      Frag<T> basef[UNITS], bf[UNITS][2][CHUNKS];
+      Frag<T> basef[UNITS][MT], bf[UNITS][2][CHUNKS];
       load_units(unit, k, basef, bf);
-      f32x4 acc[UNITS][2];
+      f32x4 acc[UNITS][MT][2];
 #pragma unroll
       for (int i = 0; i < UNITS; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          acc[i][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int t = 0; t < MT; ++t) acc[i][t][e] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int c = 0; c < CHUNKS; ++c) {
             if (EDGE == WHOLE) keep_all(bf[i][e][c], along[c]);
             const Frag<T> bo = exchange(bf[i][e][c], lanes.operand);
 #pragma unroll
-            for (int p = 0; p < NT; ++p) mma(acc[i][e], bo, uf[c][p]);
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+              for (int p = 0; p < NT; ++p) mma(acc[i][t][e], bo, uf[t][c][p]);
           }
         }
-      Frag<T> yf[UNITS];
+      Frag<T> yf[UNITS][MT];
 #pragma unroll
-      for (int i = 0; i < UNITS; ++i) {
-        float v[8];
+      for (int i = 0; i < UNITS; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = keep(acc[i][e >> 2][e & 3], has);
-        float o[8];
-        unpack(exchange(basef[i], lanes.operand), o);
+        for (int t = 0; t < MT; ++t) {
+          float v[8], o[8];
+          unpack(exchange(basef[i][t], lanes.operand), o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += keep(o[e], has_base);
-        pack(v, yf[i]);
-        yf[i] = exchange(yf[i], lanes.rows);
-      }
+          for (int e = 0; e < 8; ++e) v[e] = keep(acc[i][t][e >> 2][e & 3], has[t]) + keep(o[e], has_base);
+          pack(v, yf[i][t]);
+          yf[i][t] = exchange(yf[i][t], lanes.rows);
+        }
 #pragma unroll
-      for (int i = 0; i < UNITS; ++i) {
-        const int o0 = (unit + i) * 32;
-        if (stores && unit + i < last) store_frag<EDGE>(g.y + t0 * g.d_out + o0 + y_store, g.d_out - o0 - part_q * 8, yf[i]);
-      }
+      for (int i = 0; i < UNITS; ++i)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          const int o0 = (unit + i) * 32;
+          if (stores[t] && unit + i < last)
+            store_frag<EDGE>(g.y + t0 * g.d_out + o0 + here(row_token[t]) * g.d_out + part_q * 8, g.d_out - o0 - part_q * 8, yf[i][t]);
+        }
     }
   }
 }
@@ -646,31 +687,65 @@ struct SumArgs {
   int blocks_in, blocks;  // workgroups per adapter: of da, of both
 };
 
-// Slots of an adapter added in the order of chunks (0 without one); db times the adapter's scale.
-__device__ __forceinline__ void sum_slots(const SumArgs& g, const OrderArgs& w, int block) {
+constexpr int SUM_COLUMNS = 32;          // of db per workgroup
+
+// Slots of an adapter added in the order of chunks (0 without one); db times the adapter's scale, and turned in LDS, since its rows are along
+// the rank (written as they are read, 4 bytes a row, they took 40 us of 2048 tokens' training step at rank 64, eight adapters).
+__device__ __forceinline__ void sum_slots(const SumArgs& g, const OrderArgs& w, int block, float* tile) {
   const int k = block / g.blocks, b = block % g.blocks;
   const bool first = b < g.blocks_in;
   const int d = first ? g.d_in : g.d_out;
-  const int64_t size = (int64_t)w.rank * d, i = (int64_t)(b - (first ? 0 : g.blocks_in)) * 256 + threadIdx.x;
-  if (i >= size) return;
+  const int64_t size = (int64_t)w.rank * d;
   const int p0 = w.start[k], p1 = w.start[k + 1];
-  float t = 0.0f;
-  if (p1 > p0) {
-    const int c0 = p0 / w.chunk, c1 = (p1 - 1) / w.chunk;
-    const float* from = (first ? g.da_slots : g.db_slots) + (int64_t)(c0 + k) * size + i;
+  const int c0 = p0 / w.chunk, n = p1 > p0 ? (p1 - 1) / w.chunk - c0 + 1 : 0;
+  const float* slots = (first ? g.da_slots : g.db_slots) + (int64_t)(c0 + k) * size;
+  if (first) {
+    const int64_t i = ((int64_t)b * 256 + threadIdx.x) * 4;
+    const int left = (int)min(size - i, (int64_t)4);
+    if (left <= 0) return;
+    float t[4] = {};
+    if (left == 4) {
 #pragma unroll 8
-    for (int c = c0; c <= c1; ++c, from += size) t += *from;
-    if (!first) t *= g.scale[k];
+      for (int c = 0; c < n; ++c) {
+        const Bytes16<float> v = *reinterpret_cast<const Bytes16<float>*>(slots + c * size + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] += __uint_as_float(v.w[e]);
+      }
+      Bytes16<float> o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o.w[e] = __float_as_uint(t[e]);
+      *reinterpret_cast<Bytes16<float>*>(g.da + k * size + i) = o;
+      return;
+    }
+    for (int c = 0; c < n; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) if (e < left) t[e] += slots[c * size + i + e];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if (e < left) g.da[k * size + i + e] = t[e];
+    return;
   }
-  if (first) g.da[k * size + i] = t;
-  else g.db[k * size + (i % d) * w.rank + i / d] = t;
+  auto sum = [&](int64_t i) {
+    float t = 0.0f;
+#pragma unroll 8
+    for (int c = 0; c < n; ++c) t += slots[c * size + i];
+    return t;
+  };
+  const int o0 = (b - g.blocks_in) * SUM_COLUMNS, columns = min(SUM_COLUMNS, d - o0);
+  const float scale = n > 0 ? g.scale[k] : 0.0f;
+  for (int i = threadIdx.x; i < w.rank * SUM_COLUMNS; i += 256) {
+    const int r = i / SUM_COLUMNS, o = i % SUM_COLUMNS;
+    if (o < columns) tile[o * (w.rank + 1) + r] = n > 0 ? sum((int64_t)r * d + o0 + o) * scale : 0.0f;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < w.rank * columns; i += 256) g.db[k * size + (int64_t)o0 * w.rank + i] = tile[i / w.rank * (w.rank + 1) + i % w.rank];
 }
 
 // What is left once the slots are written: dx, which only needs v, and the sums of the slots, which are short beside it.
 template <typename T, int R16, int EDGE>
 __global__ __launch_bounds__(256) void finish_kernel(DxArgs<T> dx, SumArgs sums, OrderArgs w, int sum_blocks, int slabs) {
   __shared__ int32_t token[CHUNK_MAX];
-  if ((int)blockIdx.x < sum_blocks) return sum_slots(sums, w, blockIdx.x);
+  __shared__ float tile[SUM_COLUMNS * (MAX_RANK + 1)];
+  if ((int)blockIdx.x < sum_blocks) return sum_slots(sums, w, blockIdx.x, tile);
   const int block = blockIdx.x - sum_blocks, slab = block % slabs;
   const Places at = load_places(w, block / slabs, token);
   for (int p0 = at.first; p0 < at.last;) {
@@ -703,15 +778,19 @@ template <typename T, bool EXPAND>
 static void launch_tiles(TileArgs<T> g, hipStream_t s) {
   const int units = EXPAND ? (g.d_out + 31) / 32 : 1;
   const bool scan = g.tokens <= SCAN_TOKENS;
-  const int64_t tiles = scan ? g.tokens : (g.tokens + 15) / 16;
-  g.slices = EXPAND ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (units + 15) / 16)) : 1;
   const bool whole = g.d_in % 8 == 0 && (!EXPAND || (g.d_out % 8 == 0 && g.rank % 8 == 0));
   const bool tiny = g.d_in < 8 || (EXPAND && std::min(g.tokens * g.d_out, (int64_t)g.n_adapters * g.d_out * g.rank) < 8);
   with_shape(g.rank, whole, tiny, [&](auto r, auto edge) {
     constexpr int R = decltype(r)::value, E = decltype(edge)::value;
+    // Wide adapters are read once for 32 tokens where such tiles still fill the chip (rank 64, 4096 wide, us with 16 / 32: 8192 tokens
+    // of one adapter 80 / 62, of eight 107 / 94; 2048 tokens 25 / 39).
+    const bool tall = R == 4 && !scan && g.tokens >= 256 * 32;
+    const int64_t rows = tall ? 32 : 16, tiles = scan ? g.tokens : (g.tokens + rows - 1) / rows;
+    g.slices = EXPAND ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (units + 15) / 16)) : 1;
     const dim3 grid((unsigned)(scan ? tiles : (tiles + 7) / 8 * 8), g.slices, scan ? 1 : std::min(g.n_adapters, 2)), block(TILE_WAVES<R> * 64);
-    if (scan) hipLaunchKernelGGL((tile_kernel<T, R, true, EXPAND, E>), grid, block, 0, s, g);
-    else hipLaunchKernelGGL((tile_kernel<T, R, false, EXPAND, E>), grid, block, 0, s, g);
+    if (scan) hipLaunchKernelGGL((tile_kernel<T, R, 1, true, EXPAND, E>), grid, block, 0, s, g);
+    else if (tall) hipLaunchKernelGGL((tile_kernel<T, R, R == 4 ? 2 : 1, false, EXPAND, E>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((tile_kernel<T, R, 1, false, EXPAND, E>), grid, block, 0, s, g);
   });
 }
 
@@ -774,7 +853,7 @@ static void launch_adapters_backward(const cmoe_adapters_backward_args& p, const
       hipLaunchKernelGGL((grad_kernel<T, decltype(r)::value, decltype(edge)::value>), dim3(slabs_da + slabs_db, l.chunks), dim3(256), 0, s, ga, gb, w, slabs_da);
     });
   }
-  const int blocks_in = p.da ? (int)(((int64_t)p.rank * p.d_in + 255) / 256) : 0, blocks_out = p.db ? (int)(((int64_t)p.rank * p.d_out + 255) / 256) : 0;
+  const int blocks_in = p.da ? (int)(((int64_t)p.rank * p.d_in + 1023) / 1024) : 0, blocks_out = p.db ? (p.d_out + SUM_COLUMNS - 1) / SUM_COLUMNS : 0;
   const SumArgs sums{da, db, p.scale, p.da, p.db, p.d_in, p.d_out, blocks_in, blocks_in + blocks_out};
   const int sum_blocks = sums.blocks * p.n_adapters, dx_blocks = p.dx ? slabs * l.chunks : 0;
   if (sum_blocks + dx_blocks > 0)
