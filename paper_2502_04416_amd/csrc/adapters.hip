@@ -556,7 +556,7 @@ __device__ __forceinline__ void grad_segment(const GradArgs<T>& g, const OrderAr
 #pragma unroll
     for (int r = 0; r < R16; ++r) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[r][j] = keep(f[r][j], less_mask(place(j), p1));
+      for (int j = 0; j < 8; ++j) f[r][j] = keep(f[r][j], less_mask_apart(place(j), p1));
       Frag<T> vf[NG];
       split(f[r], vf);
 #pragma unroll
@@ -626,7 +626,7 @@ __device__ __forceinline__ void dx_segment(const DxArgs<T>& g, const OrderArgs& 
     for (int j = 0; j < 8; ++j) {
       const int r = (c * 4 + q) * 8 + j;
       rows[j] = load_at<EDGE>(g.a, ((int64_t)(none ? 0 : k) * w.rank + min(r, w.rank - 1)) * g.d + c0, n, (int64_t)w.n_adapters * w.rank * g.d);
-      keep_all(rows[j], less_mask(r, w.rank));
+      keep_all(rows[j], less_mask_apart(r, w.rank));
     }
     transpose(rows, af[c]);
   }

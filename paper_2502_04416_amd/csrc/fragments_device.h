@@ -38,6 +38,13 @@ __device__ __forceinline__ Frag<float> load_frag(const float* p) {
 // All ones where a < b (both far from the ends of the type).  Values are chosen by masks, not by conditions, throughout: of a condition on
 // loaded values the compiler made a branch for each, with a wait of its own.
 __device__ __forceinline__ uint32_t less_mask(int a, int b) { return (uint32_t)((a - b) >> 31); }
+// ... that is not to be merged with others: of the products of two sets of masks it made conditions again, hundreds of them, in scalar
+// registers that it had to spill.
+__device__ __forceinline__ uint32_t less_mask_apart(int a, int b) {
+  uint32_t mask = less_mask(a, b);
+  asm("" : "+v"(mask));
+  return mask;
+}
 __device__ __forceinline__ uint32_t choose(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
 
 // Values from the s-th on, zeros after the last (any s >= 0).
@@ -129,6 +136,7 @@ __device__ __forceinline__ Frag<T> load_at(const T* p, int64_t at, int n, int64_
   if constexpr (EDGE == WHOLE) return load_frag(p + (n > 0 ? at : 0));
   const int64_t from = n > 0 ? min(at, size - 8) : 0;
   Frag<T> f = load_frag(p + from);
+  asm("" : "+v"(n));                                         // (as less_mask_apart)
   shift_down(f, n > 0 ? (int)(at - from) : 8);
   keep_first(f, n);
   return f;
