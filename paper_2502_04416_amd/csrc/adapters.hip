@@ -61,7 +61,7 @@ constexpr int SCAN_TOKENS = 512;         // a workgroup of the scanning form loo
 template <int R16>
 constexpr int TILE_WAVES = R16 == 1 ? 16 : 8;
 template <typename T, int R16>
-constexpr int UNITS_AT_ONCE = sizeof(T) == 4 || R16 == 4 ? 1 : R16 == 2 ? 4 : 2;
+constexpr int UNITS_AT_ONCE = sizeof(T) == 4 || R16 == 4 ? 1 : 2;
 
 // A tile is 16 MT tokens.  Its workgroup first contracts x with the adapter's rows: the waves take turns along the width, 64 values each
 // time, each a part of its own, and their sums meet in LDS; then each wave expands u to its own columns, on to base, straight from memory to memory.
@@ -167,8 +167,10 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
     }
   };
 
-  // Turns along the width are DEPTH at a time; past the wave's last turn its values, as zeros.
-  constexpr int DEPTH = MT > 1 ? 1 : R16 == 1 && sizeof(T) == 2 ? 4 : R16 == 4 || sizeof(T) == 2 ? 2 : 1;
+  // Turns along the width are DEPTH at a time; past the wave's last turn its values, as zeros.  The other waves cover a turn's latency, and
+  // code costs time to fetch (kernels of some us are mostly run once through): 2 rather than 4 at one block of ranks, 30.4 -> 28.8 us for
+  // 4096 tokens, 13.7 -> 10.8 for 40 of odd widths; 1 rather than 2 at four, 30.5 -> 25.7 for 1024 tokens.
+  constexpr int DEPTH = MT == 1 && R16 == 1 && sizeof(T) == 2 ? 2 : 1;
   const int full = g.d_in / 64;                              // whole turns
   const int turns = (full + WAVES - 1) / WAVES, turn0 = min(wave * turns, full), turn1 = min(turn0 + turns, full);
   auto turn = [&](int s, int i) { return min(s + (i >> 1), turn1 - 1) * 64 + (i & 1) * 32; };
