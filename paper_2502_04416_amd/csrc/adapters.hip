@@ -438,7 +438,7 @@ __device__ void order_tokens(const int32_t* ids, int tokens, int n_adapters, int
   });
 }
 
-// The first workgroup orders the tokens; the next ones transpose b, bt[k][j][o] = b[k][o][j], 64 columns o of one adapter each through
+// The first workgroup orders the tokens; the next ones transpose b, bt[k][j][o] = b[k][o][j], 64 columns o of one adapter at a time through
 // LDS; the others leave dropout's mask, a byte per chunk.  (The order is a chain of latencies, so the rest is done beside it.)
 template <typename T>
 __global__ __launch_bounds__(1024) void arrange_kernel(const int32_t* ids, int tokens, int n_adapters, int n_waves, int32_t* order, int32_t* start, const T* b,
@@ -460,13 +460,22 @@ __global__ __launch_bounds__(1024) void arrange_kernel(const int32_t* ids, int t
     }
     return;
   }
-  const int per = (d_out + 63) / 64;
-  const int k = (blockIdx.x - 1) / per, o0 = (blockIdx.x - 1) % per * 64, n = min(64, d_out - o0);
-  const T* from = b + ((int64_t)k * d_out + o0) * rank;
-  for (int i = threadIdx.x; i < n * rank; i += 1024) tile[i % rank][i / rank] = from[i];
-  __syncthreads();
-  for (int i = threadIdx.x; i < rank * 64; i += 1024)
-    if ((i & 63) < n) bt[((int64_t)k * rank + (i >> 6)) * d_out + o0 + (i & 63)] = tile[i >> 6][i & 63];
+  const int per = transposes / n_adapters, k = (blockIdx.x - 1) / per;
+  if (n_adapters > 1) {                                      // (a bank holds more adapters than a batch has)
+    bool used = false;
+#pragma unroll 4
+    for (int t = threadIdx.x; t < tokens; t += 1024) used |= adapter_of(ids, t, n_adapters) == k;
+    if (!__syncthreads_or(used)) return;
+  }
+  for (int o0 = (blockIdx.x - 1) % per * 64; o0 < d_out; o0 += per * 64) {
+    const int n = min(64, d_out - o0);
+    const T* from = b + ((int64_t)k * d_out + o0) * rank;
+    for (int i = threadIdx.x; i < n * rank; i += 1024) tile[i % rank][i / rank] = from[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < rank * 64; i += 1024)
+      if ((i & 63) < n) bt[((int64_t)k * rank + (i >> 6)) * d_out + o0 + (i & 63)] = tile[i >> 6][i & 63];
+    __syncthreads();
+  }
 }
 
 // ---- backward: dx and the gradients of the weights -----------------------------------------------------------------
@@ -713,30 +722,26 @@ __device__ __forceinline__ void sum_slots(const SumArgs& g, const OrderArgs& w, 
 #pragma unroll
         for (int e = 0; e < 4; ++e) t[e] += __uint_as_float(v.w[e]);
       }
-      Bytes16<float> o;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o.w[e] = __float_as_uint(t[e]);
-      *reinterpret_cast<Bytes16<float>*>(g.da + k * size + i) = o;
-      return;
+      *reinterpret_cast<Bytes16<float>*>(g.da + k * size + i) = __builtin_bit_cast(Bytes16<float>, t);
+    } else {
+      for (int e = 0; e < left; ++e) {
+        float last = 0.0f;
+        for (int c = 0; c < n; ++c) last += slots[c * size + i + e];
+        g.da[k * size + i + e] = last;
+      }
     }
-    for (int c = 0; c < n; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) if (e < left) t[e] += slots[c * size + i + e];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) if (e < left) g.da[k * size + i + e] = t[e];
     return;
   }
-  auto sum = [&](int64_t i) {
-    float t = 0.0f;
-#pragma unroll 8
-    for (int c = 0; c < n; ++c) t += slots[c * size + i];
-    return t;
-  };
   const int o0 = (b - g.blocks_in) * SUM_COLUMNS, columns = min(SUM_COLUMNS, d - o0);
   const float scale = n > 0 ? g.scale[k] : 0.0f;
   for (int i = threadIdx.x; i < w.rank * SUM_COLUMNS; i += 256) {
     const int r = i / SUM_COLUMNS, o = i % SUM_COLUMNS;
-    if (o < columns) tile[o * (w.rank + 1) + r] = n > 0 ? sum((int64_t)r * d + o0 + o) * scale : 0.0f;
+    if (o >= columns) continue;
+    const float* from = slots + (int64_t)r * d + o0 + o;
+    float t = 0.0f;
+#pragma unroll 8
+    for (int c = 0; c < n; ++c) t += from[c * size];
+    tile[o * (w.rank + 1) + r] = n > 0 ? t * scale : 0.0f;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < w.rank * columns; i += 256) g.db[k * size + (int64_t)o0 * w.rank + i] = tile[i / w.rank * (w.rank + 1) + i % w.rank];
@@ -788,6 +793,8 @@ static void launch_tiles(TileArgs<T> g, hipStream_t s) {
     // of one adapter 80 / 62, of eight 107 / 94; 2048 tokens 25 / 39).
     const bool tall = R == 4 && !scan && g.tokens >= 256 * 32;
     const int64_t rows = tall ? 32 : 16, tiles = scan ? g.tokens : (g.tokens + rows - 1) / rows;
+    // Parts of y's columns, as many as fill the chip if every tile has tokens.  (Each contracts x again, and workgroups that find none of
+    // their own are not free: eight parts for 256 tokens of one adapter, 15 -> 61 us.)
     g.slices = EXPAND ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (units + 15) / 16)) : 1;
     const dim3 grid((unsigned)(scan ? tiles : (tiles + 7) / 8 * 8), g.slices, scan ? 1 : std::min(g.n_adapters, 2)), block(TILE_WAVES<R> * 64);
     if (scan) hipLaunchKernelGGL((tile_kernel<T, R, 1, true, EXPAND, E>), grid, block, 0, s, g);
@@ -836,7 +843,7 @@ static void launch_adapters_backward(const cmoe_adapters_backward_args& p, const
   T* bt = (T*)(ws + l.bt);
   const bool needs_v = p.tokens > 0 && (p.dx || p.da);
   const int n_waves = std::min(16, (MAX_ADAPTERS + 1) / (p.n_adapters + 1));
-  const int transposes = needs_v ? (p.d_out + 63) / 64 * p.n_adapters : 0;
+  const int transposes = needs_v ? std::min((p.d_out + 63) / 64, std::max(1, 512 / p.n_adapters)) * p.n_adapters : 0;
   const int64_t chunks = needs_v && drop.limit ? p.tokens * ((p.d_in + 7) / 8) : 0;
   const int masks = (int)std::min<int64_t>((chunks + 1023) / 1024, 1024);
   uint8_t* kept = (uint8_t*)(ws + l.kept);
