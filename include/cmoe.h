@@ -379,7 +379,7 @@ size_t cmoe_norm_backward_workspace_bytes(int64_t rows, int32_t cols);
 int cmoe_norm_backward(const cmoe_norm_backward_args* args, void* hip_stream);
 
 /* Low-rank adapters of many requests beside a shared projection: y[t] = base[t] + scale[k] * B_k (A_k drop(x[t])), k = ids[t].
- * A token whose id is not in [0, n_adapters) has no adapter (y = base).  rank <= 64. */
+ * A token whose id is not in [0, n_adapters) has no adapter (y = base).  rank <= 64, n_adapters <= 8191, tokens and widths <= 2^20. */
 typedef struct {
   const void* x;             /* [tokens, d_in] */
   const void* a;             /* [n_adapters, rank, d_in] */
@@ -389,15 +389,12 @@ typedef struct {
   const void* base;          /* [tokens, d_out], or NULL: 0 */
   void* y;
   float* u;                  /* [tokens, rank] fp32: A_k drop(x[t]) (0 without an adapter), for the backward pass, or NULL */
-  void* workspace;           /* 16-byte aligned */
-  uint64_t workspace_bytes;
   int64_t tokens;
   double p;                  /* dropout of x */
   uint64_t seed, offset;
   int32_t struct_bytes;      /* sizeof(cmoe_adapters_forward_args) */
   int32_t dtype, d_in, d_out, rank, n_adapters;
 } cmoe_adapters_forward_args;
-size_t cmoe_adapters_forward_workspace_bytes(int64_t tokens, int32_t d_in, int32_t d_out, int32_t rank, int32_t n_adapters, int32_t dtype);
 int cmoe_adapters_forward(const cmoe_adapters_forward_args* args, void* hip_stream);
 
 /* dx = dx_base + drop's backward of scale[k] * A_k^T (B_k^T dy[t]); da, db: the gradients of every adapter of the bank (0 where no

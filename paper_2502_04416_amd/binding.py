@@ -44,7 +44,7 @@ EXPORTS = [
     "cmoe_set_tuning", "cmoe_set_neuron_sparsity", "cmoe_forward_static", "cmoe_static_scratch_bytes", "cmoe_forward_static_max_tokens",
     "cmoe_forward_plan", "cmoe_hier_forward_plan", "cmoe_scorer_plan",
     "cmoe_dropout", "cmoe_norm_forward", "cmoe_norm_backward", "cmoe_norm_backward_workspace_bytes",
-    "cmoe_adapters_forward", "cmoe_adapters_forward_workspace_bytes", "cmoe_adapters_backward", "cmoe_adapters_backward_workspace_bytes",
+    "cmoe_adapters_forward", "cmoe_adapters_backward", "cmoe_adapters_backward_workspace_bytes",
 ]
 
 
@@ -116,9 +116,8 @@ def load():
         getattr(lib, name).argtypes = [C.c_char_p, vp]                   # the packed bytes of an argument struct
     lib.cmoe_norm_backward_workspace_bytes.argtypes = [i64, C.c_int32]
     lib.cmoe_norm_backward_workspace_bytes.restype = sz
-    for name in ("cmoe_adapters_forward_workspace_bytes", "cmoe_adapters_backward_workspace_bytes"):
-        getattr(lib, name).argtypes = [i64] + [C.c_int32] * 5
-        getattr(lib, name).restype = sz
+    lib.cmoe_adapters_backward_workspace_bytes.argtypes = [i64] + [C.c_int32] * 5
+    lib.cmoe_adapters_backward_workspace_bytes.restype = sz
     lib.cmoe_last_error.restype = C.c_char_p
     lib.cmoe_version.restype = C.c_char_p
     _lib = lib
@@ -393,7 +392,7 @@ def cmoe_version() -> str:
 
 _NORM_FORWARD = struct.Struct("=8QqdQQ4ifi")         # cmoe_norm_forward_args
 _NORM_BACKWARD = struct.Struct("=12QqdQQ4i")         # cmoe_norm_backward_args
-_ADAPTERS_FORWARD = struct.Struct("=10QqdQQ6i")      # cmoe_adapters_forward_args
+_ADAPTERS_FORWARD = struct.Struct("=8QqdQQ6i")       # cmoe_adapters_forward_args
 _ADAPTERS_BACKWARD = struct.Struct("=13QqdQQ6i")     # cmoe_adapters_backward_args
 _FORMS = {"layer": 0, "rms": 1}
 
@@ -533,9 +532,7 @@ def adapters_forward(x, y, a, b, scale, *, ids=None, base=None, dropout: Optiona
         _operand("x", x, dtype, (t, d_in), dev), _operand("a", a, dtype, (n, rank, d_in), dev), _operand("b", b, dtype, (n, d_out, rank), dev),
         _operand("scale", scale, torch.float32, (n,), dev), _operand("ids", ids, torch.int32, (t,), dev), _operand("base", base, dtype, (t, d_out), dev),
         _operand("y", y, dtype, (t, d_out), dev), _operand("u", u, torch.float32, (t, rank), dev))
-    nbytes = load().cmoe_adapters_forward_workspace_bytes(t, d_in, d_out, rank, n, code)
-    ws = _workspace(nbytes) if nbytes else None
-    args = _ADAPTERS_FORWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, d.p, d.seed, d.offset, _ADAPTERS_FORWARD.size, code, d_in,
+    args = _ADAPTERS_FORWARD.pack(*operands, t, d.p, d.seed, d.offset, _ADAPTERS_FORWARD.size, code, d_in,
                                   d_out, rank, n)
     _check(load().cmoe_adapters_forward(args, stream), "cmoe_adapters_forward")
 

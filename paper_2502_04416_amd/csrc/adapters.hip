@@ -58,10 +58,10 @@ struct TileArgs {
 constexpr int SCAN_TOKENS = 512;         // a workgroup of the scanning form looks at one id per thread
 
 // Waves of a workgroup, and units of 32 columns of y that a wave has in flight at once.
-template <int R16>
-constexpr int TILE_WAVES = R16 == 1 ? 16 : 8;
+template <int R16, bool SCAN>
+constexpr int TILE_WAVES = R16 == 1 || (R16 == 2 && SCAN) ? 16 : 8;
 template <typename T, int R16>
-constexpr int UNITS_AT_ONCE = sizeof(T) == 4 || R16 == 4 ? 1 : 2;
+constexpr int UNITS_AT_ONCE = R16 == 4 || sizeof(T) == 4 ? 1 : 2;
 
 // A tile is 16 MT tokens.  Its workgroup first contracts x with the adapter's rows: the waves take turns along the width, 64 values each
 // time, each a part of its own, and their sums meet in LDS; then each wave expands u to its own columns, on to base, straight from memory to memory.
@@ -72,9 +72,13 @@ constexpr int UNITS_AT_ONCE = sizeof(T) == 4 || R16 == 4 ? 1 : 2;
 // A row or column of a product that is no token, rank or column of y reads another's values, and its results are not used: a token
 // does not see what another's adapter holds.
 // Without EXPAND: u * scale alone (v of the backward pass).
+// One launch, since a second costs what the sums of u take to meet.  4096 tokens, 4096 wide, rank 8, bf16 with dropout: 29 us for 101 MB (a
+// copy 19), of which the launch is 3, the first latencies 3, and the generator 7 in a part that waits for x meanwhile.  2048 tokens of
+// eleven adapters of rank 32: 22 us; 64 tokens of 35 adapters, 4096 by 11008, rank 16: 13.6 us for 18 MB; one token 8.8 us.  What bounds
+// the small ones is one round trip after another (ids, x and a, b) and the fetching of code that runs once.
 template <typename T, int R16, int MT, bool SCAN, bool EXPAND, int EDGE>
-__global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_kernel(TileArgs<T> g) {
-  constexpr int WAVES = TILE_WAVES<R16>, M = 16 * MT;
+__global__ __launch_bounds__((TILE_WAVES<R16, SCAN>) * 64, R16 == 4 ? 2 : 4) void tile_kernel(TileArgs<T> g) {
+  constexpr int WAVES = TILE_WAVES<R16, SCAN>, M = 16 * MT;
   constexpr int CHUNKS = (R16 + 1) / 2;                      // operands along the rank
   constexpr int NT = Terms<T>::OUTPUT;
   constexpr int LD = CHUNKS * 32 + 16 / sizeof(T);
@@ -84,9 +88,6 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id(), m = lane & 15, q = lane >> 4;
   const int row = lane >> 2, part_q = lane & 3;              // row and chunk of a lane as rows are loaded and stored
   const Lanes lanes = lane_orders();
-  // Consecutive tiles on one XCD (workgroups go to the eight in turn): they share adapters, which stay in its L2 cache.
-  const int per_xcd = (gridDim.x + 7) >> 3, tile = SCAN ? (int)blockIdx.x : (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if (!SCAN && (int64_t)tile * M >= g.tokens) return;
   const int z = gridDim.z - 1 - blockIdx.z;                  // (the few tiles with a second adapter begin with it)
   if (SCAN) {
     const int me = blockIdx.x;
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
     }
   } else if (tid < 64) {
     const int place = lane & (M - 1);
-    const int64_t t = (int64_t)tile * M + place;
+    const int64_t t = (int64_t)blockIdx.x * M + place;
     const bool valid = t < g.tokens;
     const int k = valid ? adapter_of(g.ids, t, g.n_adapters) : -2;
     bool first = k >= 0 && lane < M;
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
     }
     const uint64_t votes = __ballot(first);
     if (lane < M) {
-      token[place] = valid ? place : (int)(g.tokens - 1 - (int64_t)tile * M);
+      token[place] = valid ? place : (int)(g.tokens - 1 - (int64_t)blockIdx.x * M);
       id[place] = k;
     }
     if (first) found[__popcll(votes & ((1ull << lane) - 1))] = k;
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(TILE_WAVES<R16> * 64, R16 == 4 ? 2 : 4) void tile_k
   if (EXPAND && R16 == 1)                                    // (an operand is 32 values along the rank)
     for (int i = tid; i < (int)sizeof(us) / 4; i += WAVES * 64) reinterpret_cast<uint32_t*>(us)[i] = 0;
   __syncthreads();
-  const int64_t t0 = SCAN ? 0 : (int64_t)tile * M;
+  const int64_t t0 = SCAN ? 0 : (int64_t)blockIdx.x * M;
   const int n_distinct = __builtin_amdgcn_readfirstlane(n_found);
   int row_token[MT];
 #pragma unroll
@@ -438,7 +439,7 @@ __device__ void order_tokens(const int32_t* ids, int tokens, int n_adapters, int
   });
 }
 
-// The first workgroup orders the tokens; the next ones transpose b, bt[k][j][o] = b[k][o][j], 64 columns o of one adapter at a time through
+// 4096 tokens: 8 us, of which the order takes 6.5.  The first workgroup orders the tokens; the next ones transpose b, bt[k][j][o] = b[k][o][j], 64 columns o of one adapter at a time through
 // LDS; the others leave dropout's mask, a byte per chunk.  (The order is a chain of latencies, so the rest is done beside it.)
 template <typename T>
 __global__ __launch_bounds__(1024) void arrange_kernel(const int32_t* ids, int tokens, int n_adapters, int n_waves, int32_t* order, int32_t* start, const T* b,
@@ -533,7 +534,8 @@ __device__ __forceinline__ Places load_places(const OrderArgs& w, int chunk, int
 
 // Sums over tokens, 32 in a turn, the lane's at places q * 4 + 0..3 and 16 + q * 4 + 0..3: the lane turns its eight rows in registers into eight operands whose contracted axis is the tokens (operand e's row m
 // is column 8 m + e), so nothing goes through LDS.  An adapter's sums within the chunk go to a slot of their own (numbered chunk +
-// adapter: of two neighbours in the order one number is larger), and are added in the order of chunks by the kernel below.
+// adapter: of two neighbours in the order one number is larger), and are added in the order of chunks by the kernel below.  Bound by
+// memory: 4096 tokens, da and db 4096 wide at rank 8, 67 MB in 18.5 us.
 template <typename T, int R16, int EDGE>
 __device__ __forceinline__ void grad_segment(const GradArgs<T>& g, const OrderArgs& w, const Places& at, int slab, int k, int p0, int p1, float* sums) {
   constexpr int NG = Terms<T>::GRADIENT;
@@ -747,7 +749,13 @@ __device__ __forceinline__ void sum_slots(const SumArgs& g, const OrderArgs& w, 
   for (int i = threadIdx.x; i < w.rank * columns; i += 256) g.db[k * size + (int64_t)o0 * w.rank + i] = tile[i / w.rank * (w.rank + 1) + i % w.rank];
 }
 
-// What is left once the slots are written: dx, which only needs v, and the sums of the slots, which are short beside it.
+__global__ __launch_bounds__(256) void sum_kernel(SumArgs sums, OrderArgs w) {
+  __shared__ float tile[SUM_COLUMNS * (MAX_RANK + 1)];
+  sum_slots(sums, w, blockIdx.x, tile);
+}
+
+// What is left once the slots are written: dx, which only needs v, and the sums of the slots, which are short beside it (together 18 us for
+// 4096 tokens of 4096 at rank 8, of 72 MB).
 template <typename T, int R16, int EDGE>
 __global__ __launch_bounds__(256) void finish_kernel(DxArgs<T> dx, SumArgs sums, OrderArgs w, int sum_blocks, int slabs) {
   __shared__ int32_t token[CHUNK_MAX];
@@ -796,7 +804,7 @@ static void launch_tiles(TileArgs<T> g, hipStream_t s) {
     // Parts of y's columns, as many as fill the chip if every tile has tokens.  (Each contracts x again, and workgroups that find none of
     // their own are not free: eight parts for 256 tokens of one adapter, 15 -> 61 us.)
     g.slices = EXPAND ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (units + 15) / 16)) : 1;
-    const dim3 grid((unsigned)(scan ? tiles : (tiles + 7) / 8 * 8), g.slices, scan ? 1 : std::min(g.n_adapters, 2)), block(TILE_WAVES<R> * 64);
+    const dim3 grid((unsigned)tiles, g.slices, scan ? 1 : std::min(g.n_adapters, 2)), block((scan ? TILE_WAVES<R, true> : TILE_WAVES<R, false>) * 64);
     if (scan) hipLaunchKernelGGL((tile_kernel<T, R, 1, true, EXPAND, E>), grid, block, 0, s, g);
     else if (tall) hipLaunchKernelGGL((tile_kernel<T, R, R == 4 ? 2 : 1, false, EXPAND, E>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((tile_kernel<T, R, 1, false, EXPAND, E>), grid, block, 0, s, g);
@@ -864,7 +872,15 @@ static void launch_adapters_backward(const cmoe_adapters_backward_args& p, const
   }
   const int blocks_in = p.da ? (int)(((int64_t)p.rank * p.d_in + 1023) / 1024) : 0, blocks_out = p.db ? (p.d_out + SUM_COLUMNS - 1) / SUM_COLUMNS : 0;
   const SumArgs sums{da, db, p.scale, p.da, p.db, p.d_in, p.d_out, blocks_in, blocks_in + blocks_out};
-  const int sum_blocks = sums.blocks * p.n_adapters, dx_blocks = p.dx ? slabs * l.chunks : 0;
+  int sum_blocks = sums.blocks * p.n_adapters;
+  // Beside dx there is room for two or three workgroups on a CU.  Where the sums alone are many times that, a launch of their own, of eight
+  // (us of both: 34 adapters of rank 24, 2368 by 8896, 128 tokens 50 / 36; eight of rank 64, 4096 wide, 2048 tokens 42 / 40; one of rank 8,
+  // 160 workgroups, 19.6 beside dx and 2 more apart).
+  if (sum_blocks > 2048) {
+    hipLaunchKernelGGL(sum_kernel, dim3(sum_blocks), dim3(256), 0, s, sums, w);
+    sum_blocks = 0;
+  }
+  const int dx_blocks = p.dx ? slabs * l.chunks : 0;
   if (sum_blocks + dx_blocks > 0)
     with_shape(p.rank, p.d_in % 8 == 0, p.d_in < 8, [&](auto r, auto edge) {
       hipLaunchKernelGGL((finish_kernel<T, decltype(r)::value, decltype(edge)::value>), dim3(sum_blocks + dx_blocks), dim3(256), 0, s, dx, sums, w, sum_blocks, slabs);
@@ -882,12 +898,6 @@ static int check_adapters(const char* what, int dtype, int64_t tokens, int d_in,
 
 }  // namespace cmoe
 
-extern "C" size_t cmoe_adapters_forward_workspace_bytes(int64_t tokens, int32_t d_in, int32_t d_out, int32_t rank, int32_t n_adapters, int32_t dtype) {
-  using namespace cmoe;
-  if (check_adapters("cmoe_adapters_forward_workspace_bytes", dtype, tokens, d_in, d_out, rank, n_adapters)) return 0;
-  return 0;
-}
-
 extern "C" int cmoe_adapters_forward(const cmoe_adapters_forward_args* p, void* hip_stream) {
   using namespace cmoe;
   const char* what = "cmoe_adapters_forward";
@@ -903,7 +913,7 @@ extern "C" int cmoe_adapters_forward(const cmoe_adapters_forward_args* p, void* 
   if (int rc = check_operands(what, {{"base", p->base, out, es}}, {y}, true)) return rc;
   if (int rc = check_operands(what, {{"x", p->x, in, es}, {"a", p->a, n * p->rank * p->d_in * es, es}, {"b", p->b, n * p->d_out * p->rank * es, es},
                                      {"scale", p->scale, n * 4, 4}, {"ids", p->ids, t * 4, 4}},
-                              {y, {"u", p->u, t * p->rank * 4, 4}, {"workspace", p->workspace, p->workspace_bytes, 16}}, false))
+                              {y, {"u", p->u, t * p->rank * 4, 4}}, false))
     return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   p->dtype == CMOE_BF16 ? launch_adapters_forward<bf16_t>(*p, drop, s) : launch_adapters_forward<float>(*p, drop, s);

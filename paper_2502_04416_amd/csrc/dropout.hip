@@ -9,7 +9,8 @@
 namespace cmoe {
 
 // A thread per chunk of eight elements.  The row of a workgroup's first chunk is a division of uniform 64-bit values, a
-// thread's own row one of 32-bit values.
+// thread's own row one of 32-bit values.  Bound by memory: 16384 rows of 4096 with a residual, bf16, 403 MB in 70 us (5.8 TB/s); the
+// generator is 20 wide multiplications for eight elements, 28 us of the vector units, which run beside the loads.
 template <typename T>
 __global__ __launch_bounds__(256) void dropout_kernel(const T* x, const T* residual, T* y, int64_t rows, int cols, Drop drop) {
   const uint32_t per_row = (cols + 7) >> 3;

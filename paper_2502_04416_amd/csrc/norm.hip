@@ -80,7 +80,9 @@ struct NormForward {
 };
 
 // A row of LANES threads; a thread holds CH chunks of eight elements, LANES chunks apart, in registers from the one time they
-// are read to the one time they are written: the variance is taken around the mean without a second pass over memory.
+// are read to the one time they are written: the variance is taken around the mean without a second pass over memory.  Bound by memory:
+// 8192 rows of 4096 with a residual, bf16, 268 MB in 51 us (5.3 TB/s; a copy of that size 5.4).  A single row is a chain of latencies
+// (3.4 us), behind 3 us of the launch on the host and 3.5 us of the binding.
 template <typename T, int LANES, int CH, bool LAYER>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_forward_kernel(NormForward<T> a) {
   constexpr int ROWS = LANES >= 256 ? 1 : 256 / LANES;
@@ -294,7 +296,8 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_backward_kerne
   }
 }
 
-// out[c] = the sum of n rows of partial sums, in a fixed order: 64 columns per workgroup, each wave a sixteenth of the rows.
+// out[c] = the sum of n rows of partial sums, in a fixed order: 64 columns per workgroup, each wave a sixteenth of the rows (512 rows of
+// two times 4096 columns 4.8 us; by four waves 7.1).
 __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* __restrict__ partials, int n, int cols, int sums, float* dw, float* dbias) {
   __shared__ float part[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

@@ -308,6 +308,16 @@ def test_adapters(B, dtype, case):
     m.intact()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("case", [
+    # tiles of 32 tokens; banks whose counts leave the ordering two waves and one, and sums a launch of their own
+    (8200, 136, 72, 40, 3, "runs", 0.1, True), (8225, 70, 104, 64, 5, "mixed", 0.0, True), (8193, 64, 33, 33, 2, "odd", 0.2, False),
+    (600, 16, 24, 2, 3000, "mixed", 0.1, True), (530, 24, 40, 3, 8191, "mixed", 0.0, True),
+], ids=lambda c: "-".join(map(str, c)))
+def test_adapters_of_large_batches_and_banks(B, dtype, case):
+    test_adapters(B, dtype, case)
+
+
 @pytest.mark.parametrize("t", [3, 200, 900])
 def test_adapters_without_ids_and_in_place(B, t):
     m = Arena(t, shift=0)

@@ -119,7 +119,7 @@ def test_dropout_refuses(lib, change, msg):
 
 def _adapter_args(forward, **kw):
     if forward:
-        f = dict(x=1 << 24, a=2 << 24, b=3 << 24, scale=4 << 24, ids=5 << 24, base=6 << 24, y=7 << 24, u=8 << 24, workspace=9 << 24, workspace_bytes=1 << 22)
+        f = dict(x=1 << 24, a=2 << 24, b=3 << 24, scale=4 << 24, ids=5 << 24, base=6 << 24, y=7 << 24, u=8 << 24)
     else:
         f = dict(dy=1 << 24, x=2 << 24, u=3 << 24, a=4 << 24, b=5 << 24, scale=6 << 24, ids=7 << 24, dx_base=8 << 24, dx=9 << 24, da=10 << 24,
                  db=11 << 24, workspace=12 << 24, workspace_bytes=1 << 22)
@@ -138,7 +138,7 @@ SIZES = [
 
 @pytest.mark.parametrize("change,msg", SIZES + [
     (dict(x=0), "null"), (dict(y=0), "null"), (dict(y=(6 << 24) + 4), "y overlaps base"), (dict(y=1 << 24), "overlaps"), (dict(u=7 << 24), "overlaps"),
-    (dict(ids=(5 << 24) + 2), "aligned"), (dict(workspace=(9 << 24) + 4), "aligned"),
+    (dict(ids=(5 << 24) + 2), "aligned"),
 ])
 def test_adapters_forward_refuses(lib, change, msg):
     with pytest.raises(binding.CmoeError, match=msg):
@@ -163,8 +163,7 @@ def test_workspace_sizes(lib):
     """Sizes that are refused take no workspace; others take more with more tokens."""
     assert lib.cmoe_norm_backward_workspace_bytes(-1, 16) == 0 and lib.cmoe_norm_backward_workspace_bytes(4, 40000) == 0
     assert lib.cmoe_norm_backward_workspace_bytes(4, 16) > 0
-    for fn in (lib.cmoe_adapters_forward_workspace_bytes, lib.cmoe_adapters_backward_workspace_bytes):
-        assert fn(4, 32, 64, 65, 2, 0) == 0 and fn(4, 32, 64, 8, 2, 9) == 0
+    assert lib.cmoe_adapters_backward_workspace_bytes(4, 32, 64, 65, 2, 0) == 0 and lib.cmoe_adapters_backward_workspace_bytes(4, 32, 64, 8, 2, 9) == 0
     small, large = (lib.cmoe_adapters_backward_workspace_bytes(t, 4096, 4096, 8, 2, 1) for t in (1, 4096))
     assert 0 < small < large
 
