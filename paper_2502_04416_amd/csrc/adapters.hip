@@ -236,10 +236,10 @@ __global__ __launch_bounds__((TILE_WAVES<R16, SCAN>) * 64, R16 == 4 ? 2 : 4) voi
         Frag<T> ar[2][R16];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int at = full * 64 + h * 32, n = g.d_in - at - part_q * 8;
+          const int n = g.d_in - full * 64 - h * 32 - part_q * 8, at = rest_base(g.d_in, h);
 #pragma unroll
           for (int r = 0; r < R16; ++r) {
-            ar[h][r] = load_near<EDGE>(a + at, a_at[r], n, (int64_t)(g.n_adapters - k) * g.rank * g.d_in - at);
+            ar[h][r] = load_near<EDGE>(a + at, a_at[r], n, rest_left((int64_t)(g.n_adapters - k) * g.rank, g.d_in, h));
             keep_first(ar[h][r], n);
           }
         }
@@ -248,8 +248,8 @@ __global__ __launch_bounds__((TILE_WAVES<R16, SCAN>) * 64, R16 == 4 ? 2 : 4) voi
           Frag<T> xr[2];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int at = full * 64 + h * 32, n = g.d_in - at - part_q * 8;
-            xr[h] = load_near<EDGE>(x + at, x_at[t], n, (g.tokens - t0) * g.d_in - at);
+            const int n = g.d_in - full * 64 - h * 32 - part_q * 8, at = rest_base(g.d_in, h);
+            xr[h] = load_near<EDGE>(x + at, x_at[t], n, rest_left(g.tokens - t0, g.d_in, h));
             keep_first(xr[h], n);
           }
           if (g.drop.limit) {

@@ -1,6 +1,7 @@
 // Eight values of a row per lane, in registers as they are stored: how rows are read and written, and operands of the matrix instructions.
 #pragma once
 #include "dropout_device.h"
+#include "row_reads.h"
 
 namespace cmoe {
 
@@ -113,7 +114,8 @@ __device__ __forceinline__ Frag<T> load_tiny(const T* p, int n) {
 }
 
 // From an address that is the same for the whole wave and an offset of the lane (values, below 2^31 bytes): one register, where a
-// 64-bit address of its own for every load under way took more than the loads' results.  left: from base to the buffer's end.
+// 64-bit address of its own for every load under way took more than the loads' results.  left: from base to the buffer's end; WHOLE
+// adds the offset unsigned, so eight at least.
 template <typename T>
 __device__ __forceinline__ Frag<T> load_from(const T* base, uint32_t at) {
   return load_frag(reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + (uint32_t)(at * sizeof(T))));
@@ -121,7 +123,7 @@ __device__ __forceinline__ Frag<T> load_from(const T* base, uint32_t at) {
 template <int EDGE, typename T>
 __device__ __forceinline__ Frag<T> load_near(const T* base, int at, int n, int64_t left) {
   if constexpr (EDGE == TINY) return load_tiny(base + at, n);
-  const int last = (int)min(left - 8, (int64_t)0x40000000), from = min(at, last);
+  const int from = near_first(at, left);
   if constexpr (EDGE == WHOLE) return load_from(base, (uint32_t)from);
   Frag<T> f = load_frag(base + from);
   shift_down(f, at - from);
