@@ -122,7 +122,7 @@ __device__ __forceinline__ Frag<T> load_from(const T* base, uint32_t at) {
 }
 template <int EDGE, typename T>
 __device__ __forceinline__ Frag<T> load_near(const T* base, int at, int n, int64_t left) {
-  if constexpr (EDGE == TINY) return load_tiny(base + at, n);
+  if constexpr (EDGE == TINY) return load_tiny(base + at, tiny_count(at, n, left));
   const int from = near_first(at, left);
   if constexpr (EDGE == WHOLE) return load_from(base, (uint32_t)from);
   Frag<T> f = load_frag(base + from);

@@ -11,6 +11,9 @@ constexpr int near_first(int at, int64_t left) {
   return at < last ? at : last;
 }
 
+// How many of n values `at` past a base are read one by one: none past the buffer's end (rows of a tile may lie behind it).
+constexpr int tiny_count(int at, int n, int64_t left) { return n < left - at ? n : (int)(left - at); }
+
 // What a row of d values has behind its last 64 is read in two halves of 32.  The half's base, and what a buffer of `rows` such rows has
 // left from there: a half that begins past the row's end (its values are zeros) reads the row's last chunk, since behind the buffer's
 // last row there is nothing.  With d a multiple of eight, at least eight values are left.

@@ -24,3 +24,12 @@ def B():
 ], ids=lambda c: "-".join(map(str, c)))
 def test_adapters_of_a_last_token(B, dtype, case):
     T.test_adapters(B, dtype, case)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("case", [
+    # widths and buffers below eight values, wide ranks: most rows of a unit of b lie behind its last column
+    (1, 4, 40, 64, 1, "one", 0.0, True), (3, 5, 33, 64, 2, "mixed", 0.2, True), (600, 7, 1, 33, 3, "one", 0.1, True), (1, 640, 3, 64, 1, "one", 0.0, False),
+], ids=lambda c: "-".join(map(str, c)))
+def test_adapters_of_tiny_widths(B, dtype, case):
+    T.test_adapters(B, dtype, case)

@@ -80,3 +80,41 @@ int main() {
   return 0;
 }
 ''')
+
+
+def test_values_read_one_by_one_end_with_their_buffers(tmp_path):
+    """The form of widths and buffers below eight values: every value that a tile asks for, rows of b past the last column among them."""
+    run(tmp_path, "tiny", r'''
+static void check(const char* what, int64_t start, int64_t size, int at, int n, bool whole_row) {
+  const int count = tiny_count(at, n, size - start);
+  if ((count > 0 && start + at + (count < 8 ? count : 8) > size) || (whole_row && count != n)) {
+    printf("%s: %d of %d values, %d past %ld of %ld\n", what, count, n, at, (long)start, (long)size);
+    exit(1);
+  }
+}
+int main() {
+  for (int d = 1; d <= 70; ++d)
+    for (int rank : {1, 2, 3, 7, 8, 33, 64})
+      for (int n : {1, 2, 5})
+        for (int k = 0; k < n; ++k)
+          for (int o0 = 0; o0 < d; o0 += 32)
+            for (int row = 0; row < 16; ++row)
+              for (int part = 0; part < 4; ++part)
+                for (int c = 0; c < 2; ++c)
+                  for (int e = 0; e < 2; ++e) {
+                    const int column = (row >> 2) * 8 + (row & 3) + e * 4, left = rank - (c * 4 + part) * 8;
+                    check("b", ((int64_t)k * d + o0) * rank, (int64_t)n * d * rank, column * rank + part * 8 + c * 32, left, o0 + column < d);
+                  }
+  for (int d = 1; d <= 70; ++d)
+    for (long rows : {1, 2, 16, 33})
+      for (int row = 0; row < 16 && row < rows; ++row)
+        for (int part = 0; part < 4; ++part) {
+          for (int half = 0; half < 2; ++half) {
+            const int n = d - d / 64 * 64 - half * 32 - part * 8;
+            check("x", rest_base(d, half), rows * d, row * d + part * 8, n, n > 0);
+          }
+          for (int o0 = 0; o0 < d; o0 += 32) check("base", o0, rows * d, row * d + part * 8, d - o0 - part * 8, d - o0 - part * 8 > 0);
+        }
+  return 0;
+}
+''')
