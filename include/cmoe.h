@@ -320,7 +320,7 @@ int cmoe_scorer_plan(const cmoe_layer* layer, int64_t T, int32_t plan[2]);
 
 /* ---- operators around the feed-forward layer: dropout, norm, low-rank adapters ------------- *
  * Batches are [rows, cols] in their dtype, contiguous; addresses need only the alignment of an element (16 bytes is faster).
- * All only enqueue work.  An output may be the very buffer of an input of its own size (for the adapters: y of base, dx of
+ * All only enqueue work.  An output that is a batch may be the very buffer of an input that is one (for the adapters: y of base, dx of
  * dx_base alone); other overlaps are refused.  Statistics and sums are fp32.
  *
  * Dropout masks are not stored: element (r, c) of a batch is a function of (seed, offset, r * ceil(cols / 8) + c / 8), by

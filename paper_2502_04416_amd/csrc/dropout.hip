@@ -50,7 +50,7 @@ extern "C" int cmoe_dropout(const void* x, void* y, const void* residual, int64_
   if (!x || !y) return fail(CMOE_EINVAL, "%s: x or y is null", what);
   const size_t es = elem_size(dtype);
   const uint64_t bytes = (uint64_t)rows * cols * es;
-  if (int rc = check_operands(what, {{"x", x, bytes, es}, {"residual", residual, bytes, es}}, {{"y", y, bytes, es}}, true)) return rc;
+  if (int rc = check_operands(what, {{"x", x, bytes, es, true}, {"residual", residual, bytes, es, true}}, {{"y", y, bytes, es, true}})) return rc;
   const dim3 grid((unsigned)(((uint64_t)rows * per_row + 255) / 256));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (dtype == CMOE_BF16) hipLaunchKernelGGL(dropout_kernel<bf16_t>, grid, dim3(256), 0, s, (const bf16_t*)x, (const bf16_t*)residual, (bf16_t*)y, rows, cols, drop);

@@ -434,8 +434,8 @@ extern "C" int cmoe_norm_forward(const cmoe_norm_forward_args* p, void* hip_stre
   if (!p->x || !p->y) return fail(CMOE_EINVAL, "%s: x or y is null", what);
   const size_t es = elem_size(p->dtype);
   const uint64_t batch = (uint64_t)p->rows * p->cols * es, row = (uint64_t)p->cols * es, stat = (uint64_t)p->rows * 4;
-  if (int rc = check_operands(what, {{"x", p->x, batch, es}, {"residual", p->residual, batch, es}, {"weight", p->weight, row, es}, {"bias", p->bias, row, es}},
-                              {{"y", p->y, batch, es}, {"sum_out", p->sum_out, batch, es}, {"mean", p->mean, stat, 4}, {"rstd", p->rstd, stat, 4}}, true))
+  if (int rc = check_operands(what, {{"x", p->x, batch, es, true}, {"residual", p->residual, batch, es, true}, {"weight", p->weight, row, es}, {"bias", p->bias, row, es}},
+                              {{"y", p->y, batch, es, true}, {"sum_out", p->sum_out, batch, es, true}, {"mean", p->mean, stat, 4}, {"rstd", p->rstd, stat, 4}}))
     return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   p->dtype == CMOE_BF16 ? launch_forward<bf16_t>(*p, drop, s) : launch_forward<float>(*p, drop, s);
@@ -463,10 +463,10 @@ extern "C" int cmoe_norm_backward(const cmoe_norm_backward_args* p, void* hip_st
   const uint64_t batch = (uint64_t)p->rows * p->cols * es, row = (uint64_t)p->cols * es, stat = (uint64_t)p->rows * 4;
   if (p->dweight && p->rows > 0 && (!p->workspace || p->workspace_bytes < cmoe_norm_backward_workspace_bytes(p->rows, p->cols)))
     return fail(CMOE_EINVAL, "%s: the workspace is missing or too small", what);
-  if (int rc = check_operands(what, {{"dy", p->dy, batch, es}, {"s", p->s, batch, es}, {"dsum", p->dsum, batch, es}, {"weight", p->weight, row, es},
+  if (int rc = check_operands(what, {{"dy", p->dy, batch, es, true}, {"s", p->s, batch, es, true}, {"dsum", p->dsum, batch, es, true}, {"weight", p->weight, row, es},
                                      {"mean", p->mean, stat, 4}, {"rstd", p->rstd, stat, 4}},
-                              {{"dx", p->dx, batch, es}, {"dresidual", p->dresidual, batch, es}, {"dweight", p->dweight, (uint64_t)p->cols * 4, 4},
-                               {"dbias", p->dbias, (uint64_t)p->cols * 4, 4}, {"workspace", p->workspace, p->workspace_bytes, 16}}, true))
+                              {{"dx", p->dx, batch, es, true}, {"dresidual", p->dresidual, batch, es, true}, {"dweight", p->dweight, (uint64_t)p->cols * 4, 4},
+                               {"dbias", p->dbias, (uint64_t)p->cols * 4, 4}, {"workspace", p->workspace, p->workspace_bytes, 16}}))
     return rc;
   if (p->rows == 0 && !p->dweight) return CMOE_OK;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

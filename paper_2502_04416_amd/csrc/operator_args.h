@@ -10,12 +10,15 @@
 
 namespace cmoe {
 
-// A buffer of a call: its name in messages, address (null: not given) and bytes.
+// A buffer of a call: its name in messages, address (null: not given) and bytes.  In place: an output may be the very buffer of an input
+// where both say so, which they may if every element of the output is written by the thread that has read it, and by then nothing
+// else reads it.  Not what several rows read (weights), nor statistics, gradients of weights or workspaces.
 struct Operand {
   const char* name;
   const void* ptr;
   uint64_t bytes;
   size_t align;
+  bool in_place = false;
 };
 
 inline bool overlap(const Operand& a, const Operand& b) {
@@ -23,15 +26,15 @@ inline bool overlap(const Operand& a, const Operand& b) {
   return a.ptr && b.ptr && pa < pb + b.bytes && pb < pa + a.bytes;
 }
 
-// 0, or the code of a failure that has been recorded.  No output may overlap another, or an input in part; it may be the very
-// buffer of an input where `in_place` says so (an element is then written by the thread that has read it).
-inline int check_operands(const char* what, std::initializer_list<Operand> inputs, std::initializer_list<Operand> outputs, bool in_place) {
+// 0, or the code of a failure that has been recorded.  No output may overlap another or, but in place, an input.
+inline int check_operands(const char* what, std::initializer_list<Operand> inputs, std::initializer_list<Operand> outputs) {
   for (const auto* list : {&inputs, &outputs})
     for (const Operand& o : *list)
       if ((uint64_t)(uintptr_t)o.ptr % o.align != 0) return fail(CMOE_EINVAL, "%s: %s is not aligned to %d bytes", what, o.name, (int)o.align);
   for (const Operand& o : outputs) {
     for (const Operand& i : inputs)
-      if (overlap(o, i) && !(in_place && o.ptr == i.ptr && o.bytes == i.bytes)) return fail(CMOE_EINVAL, "%s: %s overlaps %s", what, o.name, i.name);
+      if (overlap(o, i) && !(o.in_place && i.in_place && o.ptr == i.ptr && o.bytes == i.bytes))
+        return fail(CMOE_EINVAL, "%s: %s overlaps %s", what, o.name, i.name);
     for (const Operand& q : outputs)
       if (&q != &o && overlap(o, q)) return fail(CMOE_EINVAL, "%s: %s overlaps %s", what, o.name, q.name);
   }
