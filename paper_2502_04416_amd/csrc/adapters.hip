@@ -909,11 +909,9 @@ extern "C" int cmoe_adapters_forward(const cmoe_adapters_forward_args* p, void* 
   if (!p->x || !p->y || !p->a || !p->b || !p->scale) return fail(CMOE_EINVAL, "%s: x, a, b, scale or y is null", what);
   const size_t es = elem_size(p->dtype);
   const uint64_t t = p->tokens, in = t * p->d_in * es, out = t * p->d_out * es, n = p->n_adapters;
-  const Operand y{"y", p->y, out, es, true};
-  if (int rc = check_operands(what, {{"base", p->base, out, es, true}}, {y})) return rc;
   if (int rc = check_operands(what, {{"x", p->x, in, es}, {"a", p->a, n * p->rank * p->d_in * es, es}, {"b", p->b, n * p->d_out * p->rank * es, es},
-                                     {"scale", p->scale, n * 4, 4}, {"ids", p->ids, t * 4, 4}},
-                              {y, {"u", p->u, t * p->rank * 4, 4}}))
+                                     {"scale", p->scale, n * 4, 4}, {"ids", p->ids, t * 4, 4}, {"base", p->base, out, es, true}},
+                              {{"y", p->y, out, es, true}, {"u", p->u, t * p->rank * 4, 4}}))
     return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   p->dtype == CMOE_BF16 ? launch_adapters_forward<bf16_t>(*p, drop, s) : launch_adapters_forward<float>(*p, drop, s);
@@ -940,11 +938,9 @@ extern "C" int cmoe_adapters_backward(const cmoe_adapters_backward_args* p, void
     return fail(CMOE_EINVAL, "%s: the workspace is missing or too small", what);
   const size_t es = elem_size(p->dtype);
   const uint64_t t = p->tokens, in = t * p->d_in * es, out = t * p->d_out * es, n = p->n_adapters, wa = n * p->rank * p->d_in, wb = n * p->d_out * p->rank;
-  const Operand dx{"dx", p->dx, in, es, true};
-  if (int rc = check_operands(what, {{"dx_base", p->dx_base, in, es, true}}, {dx})) return rc;
   if (int rc = check_operands(what, {{"dy", p->dy, out, es}, {"x", p->x, in, es}, {"u", p->u, t * p->rank * 4, 4}, {"a", p->a, wa * es, es}, {"b", p->b, wb * es, es},
-                                     {"scale", p->scale, n * 4, 4}, {"ids", p->ids, t * 4, 4}},
-                              {dx, {"da", p->da, wa * 4, 4}, {"db", p->db, wb * 4, 4}, {"workspace", p->workspace, p->workspace_bytes, 16}}))
+                                     {"scale", p->scale, n * 4, 4}, {"ids", p->ids, t * 4, 4}, {"dx_base", p->dx_base, in, es, true}},
+                              {{"dx", p->dx, in, es, true}, {"da", p->da, wa * 4, 4}, {"db", p->db, wb * 4, 4}, {"workspace", p->workspace, p->workspace_bytes, 16}}))
     return rc;
   if (p->tokens == 0 && !p->da && !p->db) return CMOE_OK;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2502_04416_amd import binding
-from test_operators_cpu import _norm_args, _norm_backward_args, lib  # noqa: F401
+from test_operators_cpu import _adapter_args, _norm_args, _norm_backward_args, lib  # noqa: F401
 
 
 def refused(entry, args, msg):
@@ -29,3 +29,19 @@ def test_norm_forward_refuses_what_is_no_batch_in_place(lib, change, msg):  # no
 def test_norm_backward_refuses_what_is_no_batch_in_place(lib, change, msg):  # noqa: F811
     # (a workspace of a batch's very size)
     refused(lib.cmoe_norm_backward, _norm_backward_args(**{**dict(dweight=6 << 20, rows=64, workspace_bytes=64 * 16 * 4), **change}), msg)
+
+
+@pytest.mark.parametrize("change,msg", [
+    (dict(u=6 << 24), "u overlaps base"), (dict(u=(6 << 24) + 64), "u overlaps base"), (dict(u=6 << 24, rank=32, d_out=32), "u overlaps base"),
+    (dict(y=6 << 24, x=6 << 24, d_in=64), "y overlaps x"),
+])
+def test_adapters_forward_refuses_outputs_over_the_base(lib, change, msg):  # noqa: F811
+    refused(lib.cmoe_adapters_forward, _adapter_args(True, **change), msg)
+
+
+@pytest.mark.parametrize("change,msg", [
+    (dict(da=8 << 24), "da overlaps dx_base"), (dict(db=(8 << 24) + 128), "db overlaps dx_base"), (dict(workspace=8 << 24), "workspace overlaps dx_base"),
+    (dict(workspace=(8 << 24) - (1 << 21)), "workspace overlaps dx_base"), (dict(dx=8 << 24, x=8 << 24), "dx overlaps x"),
+])
+def test_adapters_backward_refuses_outputs_over_the_base(lib, change, msg):  # noqa: F811
+    refused(lib.cmoe_adapters_backward, _adapter_args(False, **change), msg)
