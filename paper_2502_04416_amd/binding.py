@@ -425,6 +425,11 @@ def _dtype_of(name: str, t):
     raise CmoeError("%s must be bfloat16 or float32, not %s" % (name, t.dtype))
 
 
+def _beyond_32_bits(name: str, size: int) -> CmoeError:
+    """For a size that the entry points take in 32 bits: ctypes would cut it off."""
+    return CmoeError("%s: a size of %d does not fit 32 bits" % (name, size))
+
+
 def _operand(name: str, t, dtype, shape, device: int = -2) -> int:
     """Address of a contiguous tensor of that type and shape on the device; 0 if it is None."""
     if t is None:
@@ -459,6 +464,8 @@ def dropout(x, y, dropout: Dropout, residual=None) -> None:
     if x.dim() != 2:
         raise CmoeError("x must be [rows, cols]")
     shape, d = x.shape, _drop(dropout)
+    if shape[1] >> 31:
+        raise _beyond_32_bits("x", shape[1])
     dev, stream = _place("x", x)
     args = _operand("x", x, dtype, shape, dev), _operand("y", y, dtype, shape, dev), _operand("residual", residual, dtype, shape, dev)
     _check(load().cmoe_dropout(*args, shape[0], shape[1], code, d.p, d.seed, d.offset, stream), "cmoe_dropout")
@@ -475,6 +482,10 @@ def norm_forward(x, y, weight=None, bias=None, *, form: str = "layer", eps: floa
         raise CmoeError("x must be [rows, cols] and form one of %s" % ", ".join(_FORMS))
     shape, d = x.shape, _drop(dropout)
     rows, cols = shape
+    if cols >> 31:
+        raise _beyond_32_bits("x", cols)
+    if not 0.0 <= eps <= 3e38:
+        raise CmoeError("eps must be finite and not negative")
     dev, stream = _place("x", x)
     import torch
     args = _NORM_FORWARD.pack(
@@ -496,6 +507,8 @@ def norm_backward(dy, s, dx, mean, rstd, weight=None, *, form: str = "layer", ds
         raise CmoeError("dy must be [rows, cols] and form one of %s" % ", ".join(_FORMS))
     shape, d = dy.shape, _drop(dropout)
     rows, cols = shape
+    if cols >> 31:
+        raise _beyond_32_bits("dy", cols)
     dev, stream = _place("dy", dy)
     import torch
     f32 = torch.float32
@@ -516,7 +529,10 @@ def _adapter_shapes(x_name: str, x, a, b):
     if x.dim() != 2 or a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
         raise CmoeError("adapters: %s must be [tokens, width], a [n, rank, d_in] and b [n, d_out, rank]" % x_name)
     n, rank, d_in = a.shape
-    return dtype, code, x.shape[0], d_in, b.shape[1], rank, n
+    d_out = b.shape[1]
+    if (n | rank | d_in | d_out) >> 31:
+        raise _beyond_32_bits("adapters", max(n, rank, d_in, d_out))
+    return dtype, code, x.shape[0], d_in, d_out, rank, n
 
 
 def adapters_forward(x, y, a, b, scale, *, ids=None, base=None, dropout: Optional[Dropout] = None, u=None) -> None:
