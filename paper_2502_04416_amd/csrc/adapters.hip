@@ -704,8 +704,7 @@ constexpr int SUM_COLUMNS = 32;          // of db per workgroup
 
 // Slots of an adapter added in the order of chunks (0 without one); db times the adapter's scale, and turned in LDS, since its rows are along
 // the rank (written as they are read, 4 bytes a row, they took 40 us of 2048 tokens' training step at rank 64, eight adapters).
-__device__ __forceinline__ void sum_slots(const SumArgs& g, const OrderArgs& w, int block, float* tile) {
-  const int k = block / g.blocks, b = block % g.blocks;
+__device__ __forceinline__ void sum_slots(const SumArgs& g, const OrderArgs& w, int k, int b, float* tile) {
   const bool first = b < g.blocks_in;
   const int d = first ? g.d_in : g.d_out;
   const int64_t size = (int64_t)w.rank * d;
@@ -749,9 +748,10 @@ __device__ __forceinline__ void sum_slots(const SumArgs& g, const OrderArgs& w, 
   for (int i = threadIdx.x; i < w.rank * columns; i += 256) g.db[k * size + (int64_t)o0 * w.rank + i] = tile[i / w.rank * (w.rank + 1) + i % w.rank];
 }
 
+// A row of workgroups per adapter: of a bank of thousands, all in one row would be more threads than a launch's axis holds (2^32).
 __global__ __launch_bounds__(256) void sum_kernel(SumArgs sums, OrderArgs w) {
   __shared__ float tile[SUM_COLUMNS * (MAX_RANK + 1)];
-  sum_slots(sums, w, blockIdx.x, tile);
+  sum_slots(sums, w, blockIdx.y, blockIdx.x, tile);
 }
 
 // What is left once the slots are written: dx, which only needs v, and the sums of the slots, which are short beside it (together 18 us for
@@ -760,7 +760,7 @@ template <typename T, int R16, int EDGE>
 __global__ __launch_bounds__(256) void finish_kernel(DxArgs<T> dx, SumArgs sums, OrderArgs w, int sum_blocks, int slabs) {
   __shared__ int32_t token[CHUNK_MAX];
   __shared__ float tile[SUM_COLUMNS * (MAX_RANK + 1)];
-  if ((int)blockIdx.x < sum_blocks) return sum_slots(sums, w, blockIdx.x, tile);
+  if ((int)blockIdx.x < sum_blocks) return sum_slots(sums, w, blockIdx.x / sums.blocks, blockIdx.x % sums.blocks, tile);
   const int block = blockIdx.x - sum_blocks, slab = block % slabs;
   const Places at = load_places(w, block / slabs, token);
   for (int p0 = at.first; p0 < at.last;) {
@@ -877,7 +877,7 @@ static void launch_adapters_backward(const cmoe_adapters_backward_args& p, const
   // (us of both: 34 adapters of rank 24, 2368 by 8896, 128 tokens 50 / 36; eight of rank 64, 4096 wide, 2048 tokens 42 / 40; one of rank 8,
   // 160 workgroups, 19.6 beside dx and 2 more apart).
   if (sum_blocks > 2048) {
-    hipLaunchKernelGGL(sum_kernel, dim3(sum_blocks), dim3(256), 0, s, sums, w);
+    hipLaunchKernelGGL(sum_kernel, dim3(sums.blocks, p.n_adapters), dim3(256), 0, s, sums, w);
     sum_blocks = 0;
   }
   const int dx_blocks = p.dx ? slabs * l.chunks : 0;

@@ -1,7 +1,9 @@
 """Calls of the operators around the feed-forward layer at the edges of their buffers, against the 64-bit oracle.  Where the loads of such calls
 begin is gone through on the host (test_operator_reads_cpu.py)."""
 import pytest
+import torch
 
+import operator_oracle as O
 import test_gpu_operators as T
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +35,21 @@ def test_adapters_of_a_last_token(B, dtype, case):
 ], ids=lambda c: "-".join(map(str, c)))
 def test_adapters_of_tiny_widths(B, dtype, case):
     T.test_adapters(B, dtype, case)
+
+
+def test_gradients_of_a_bank_of_many_wide_adapters(B):
+    """More sums than one axis of a launch takes (2^32 threads): every adapter without a token has gradients of 0."""
+    n, d_in, d_out, t = 8191, 8, 65568, 2
+    z = dict(device="cuda")
+    ids = torch.tensor([n - 1, 0], dtype=torch.int32, **z)
+    rng = torch.Generator().manual_seed(4)
+    dy, x = (torch.randn(t, d, generator=rng).to("cuda", torch.bfloat16) for d in (d_out, d_in))
+    u, scale = torch.randn(t, 1, generator=rng).cuda(), torch.full((n,), 2.0, **z)
+    a, b = torch.ones(n, 1, d_in, dtype=torch.bfloat16, **z), torch.zeros(n, d_out, 1, dtype=torch.bfloat16, **z)
+    da, db = torch.full((n, 1, d_in), float("nan"), **z), torch.full((n, d_out, 1), float("nan"), **z)
+    B.adapters_backward(dy, x, u, a, b, scale, ids=ids, da=da, db=db)
+    assert not da.any()                                     # (b is 0)
+    for i, k in enumerate(ids.tolist()):                    # one product of three roundings
+        want = 2.0 * dy[i].double() * u[i].double()
+        assert bool(((db[k, :, 0].double() - want).abs() <= 4 * O.U32 * want.abs()).all()), k
+    assert not db[1:n - 1].any()
