@@ -5,7 +5,7 @@
 //   dx = dx_base + drop's mask and scale on A_k^T v
 //   dA_k = sum over its tokens of v drop(x)^T,   dB_k = scale_k * sum over its tokens of dy u^T
 // The batches are read and written once and the adapters are small beside them, so all of it is bound by memory; the products run
-// on the matrix cores to stay out of the way, bf16 ones with factors kept in fp32 (u, v) entering as two or three bf16 terms.
+// on the matrix cores to stay out of the way, bf16 ones with factors kept in fp32 (u, v) entering as three bf16 terms.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 
@@ -80,7 +80,7 @@ template <typename T, int R16, int MT, bool SCAN, bool EXPAND, int EDGE>
 __global__ __launch_bounds__((TILE_WAVES<R16, SCAN>) * 64, R16 == 4 ? 2 : 4) void tile_kernel(TileArgs<T> g) {
   constexpr int WAVES = TILE_WAVES<R16, SCAN>, M = 16 * MT;
   constexpr int CHUNKS = (R16 + 1) / 2;                      // operands along the rank
-  constexpr int NT = Terms<T>::OUTPUT;
+  constexpr int NT = TERMS<T>;
   constexpr int LD = CHUNKS * 32 + 16 / sizeof(T);
   __shared__ float sums[WAVES][MT * R16 * 4 * 64];
   __shared__ __align__(16) T us[EXPAND ? NT : 1][M][LD];    // scale * u, in terms
@@ -279,17 +279,7 @@ __global__ __launch_bounds__((TILE_WAVES<R16, SCAN>) * 64, R16 == 4 ? 2 : 4) voi
         if (g.drop.limit) t *= g.drop.scale;
         if (col >= g.rank) t = 0.0f;
         if (g.u && blockIdx.y == 0 && col < g.ldu && id[row] == k) g.u[(t0 + token[row]) * g.ldu + col] = EXPAND ? t : t * scale;
-        if (EXPAND) {
-          t *= scale;
-          if constexpr (sizeof(T) == 2) {
-            const uint32_t hi = __float_as_uint(t) & 0xffff0000u;
-            const float left = t - __uint_as_float(hi);
-            us[0][row][col] = (T)(hi >> 16);
-            us[1][row][col] = left == left ? f32_to_bf16(left) : (T)0;
-          } else {
-            us[0][row][col] = t;
-          }
-        }
+        if (EXPAND) split(t * scale, &us[0][row][col], M * LD);
       }
       __syncthreads();
     }
@@ -538,7 +528,7 @@ __device__ __forceinline__ Places load_places(const OrderArgs& w, int chunk, int
 // memory: 4096 tokens, da and db 4096 wide at rank 8, 67 MB in 18.5 us.
 template <typename T, int R16, int EDGE>
 __device__ __forceinline__ void grad_segment(const GradArgs<T>& g, const OrderArgs& w, const Places& at, int slab, int k, int p0, int p1, float* sums) {
-  constexpr int NG = Terms<T>::GRADIENT;
+  constexpr int NG = TERMS<T>;
   const int lane = threadIdx.x & 63, wave = wave_id(), m = lane & 15, q = lane >> 4;
   const int c0 = slab * 128 + m * 8, n = g.d - c0, per_row = (g.d + 7) >> 3;
   f32x4 acc[R16][8];
@@ -626,7 +616,7 @@ __global__ __launch_bounds__(256) void grad_kernel(GradArgs<T> da, GradArgs<T> d
 // rows are turned in registers once.
 template <typename T, int R16, int EDGE>
 __device__ __forceinline__ void dx_segment(const DxArgs<T>& g, const OrderArgs& w, const Places& at, int slab, int k, int p0, int p1) {
-  constexpr int CHUNKS = (R16 + 1) / 2, NT = Terms<T>::OUTPUT;
+  constexpr int CHUNKS = (R16 + 1) / 2, NT = TERMS<T>;
   const int lane = threadIdx.x & 63, wave = wave_id(), m = lane & 15, q = lane >> 4;
   const int c0 = slab * 128 + m * 8, n = g.d - c0, per_row = (g.d + 7) >> 3;
   const bool none = k < 0;                                   // dx = base
