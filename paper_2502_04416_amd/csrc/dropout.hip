@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, const T* resid
   float v[8], r[8];
   load8(x + at, n, v);
   if (residual) load8(residual + at, n, r);
-  drop8(v, drop, first + threadIdx.x);
+  if (drop.limit) drop8(v, drop, first + threadIdx.x);
   if (residual) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += r[e];
