@@ -11,15 +11,26 @@ feed-forward layer is frozen.  `Block.serve` runs the block for a batch of reque
 """
 from __future__ import annotations
 
+import itertools
+from typing import Optional
+
 from . import binding, synth
+
+_blocks = itertools.count()
 
 
 class Block:
-    """A restructured layer (binding.Layer, uploaded), a bank of adapters beside it and the norm that follows."""
+    """A restructured layer (binding.Layer, uploaded), a bank of adapters beside it and the norm that follows.
+
+    seed: of the adapters' first values and of the dropout masks, another for every block of a model, or two of them drop the same
+    elements in the same step.  None: the number of blocks made without one before this, which a program that makes its blocks in the same
+    order finds again."""
 
     def __init__(self, layer: binding.Layer, n_adapters: int = 1, rank: int = 8, alpha: float = 32.0, p: float = 0.05, form: str = "rms",
-                 eps: float = 1e-5, seed: int = 0):
+                 eps: float = 1e-5, seed: Optional[int] = None):
         import torch
+        if seed is None:
+            seed = next(_blocks)
         self.layer, self.form, self.eps, self.p, self.seed, self.steps = layer, form, eps, p, seed, 0
         d = layer.cfg.d_model
         self.dtype = torch.bfloat16 if layer.bf16 else torch.float32
@@ -79,7 +90,7 @@ def main(steps: int = 200, tokens: int = 1024):
     cfg = synth.scaled(synth.CONFIGS[1], d_model=512, d_ff=2752, n_centres=16)
     weights, source = synth.make_weights(cfg), synth.make_token_source(cfg)
     layer = binding.Layer.build(cfg, *weights, source.calibration())
-    block = Block(layer)
+    block = Block(layer, seed=0)
 
     def batch(i):
         x = torch.from_numpy(source.eval_batch(i, n=tokens)).to("cuda", block.dtype)
