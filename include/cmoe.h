@@ -411,7 +411,7 @@ typedef struct {
   void* dx;                  /* [tokens, d_in] or NULL */
   float* da;                 /* [n_adapters, rank, d_in] fp32 or NULL */
   float* db;                 /* [n_adapters, d_out, rank] fp32 or NULL */
-  void* workspace;
+  void* workspace;           /* 16-byte aligned; needed with tokens, da or db */
   uint64_t workspace_bytes;
   int64_t tokens;
   double p;

@@ -74,7 +74,7 @@ constexpr int UNITS_AT_ONCE = R16 == 4 || sizeof(T) == 4 ? 1 : 2;
 // Without EXPAND: u * scale alone (v of the backward pass).
 // One launch, since a second costs what the sums of u take to meet.  4096 tokens, 4096 wide, rank 8, bf16 with dropout: 29 us for 101 MB (a
 // copy 19), of which the launch is 3, the first latencies 3, and the generator 7 in a part that waits for x meanwhile.  2048 tokens of
-// eleven adapters of rank 32: 22 us; 64 tokens of 35 adapters, 4096 by 11008, rank 16: 13.6 us for 18 MB; one token 8.8 us.  What bounds
+// eleven adapters of rank 32: 22.8 us; 64 tokens of 35 adapters, 4096 by 11008, rank 16: 13.9 us for 18 MB; one token 8.9 us.  What bounds
 // the small ones is one round trip after another (ids, x and a, b) and the fetching of code that runs once.
 template <typename T, int R16, int MT, bool SCAN, bool EXPAND, int EDGE>
 __global__ __launch_bounds__((TILE_WAVES<R16, SCAN>) * 64, R16 == 4 ? 2 : 4) void tile_kernel(TileArgs<T> g) {
@@ -510,7 +510,7 @@ constexpr int CHUNK_MAX = 512;
 
 // A workgroup of the gradients and of dx has 128 columns and a chunk of the places in the order of adapters, and takes it adapter by
 // adapter, its four waves in turns.  A lane holds eight columns, m * 8 on, of several tokens, so that every load and store is 16 bytes of a
-// row.  (Two kernels: one for both needed 246 registers where these need 164 and less, two waves per SIMD instead of three or more.)
+// row.  (Two kernels: one for both needed 246 registers; up to rank 16 the gradients need 130, three waves per SIMD, and dx 170.)
 struct Places {
   const int32_t* token;   // LDS
   int first, last;        // of the chunk
@@ -744,7 +744,7 @@ __global__ __launch_bounds__(256) void sum_kernel(SumArgs sums, OrderArgs w) {
   sum_slots(sums, w, blockIdx.y, blockIdx.x, tile);
 }
 
-// What is left once the slots are written: dx, which only needs v, and the sums of the slots, which are short beside it (together 18 us for
+// What is left once the slots are written: dx, which only needs v, and the sums of the slots, which are short beside it (together 20 us for
 // 4096 tokens of 4096 at rank 8, of 72 MB).
 template <typename T, int R16, int EDGE>
 __global__ __launch_bounds__(256) void finish_kernel(DxArgs<T> dx, SumArgs sums, OrderArgs w, int sum_blocks, int slabs) {
@@ -788,7 +788,7 @@ static void launch_tiles(TileArgs<T> g, hipStream_t s) {
   with_shape(g.rank, whole, tiny, [&](auto r, auto edge) {
     constexpr int R = decltype(r)::value, E = decltype(edge)::value;
     // Wide adapters are read once for 32 tokens where such tiles still fill the chip (rank 64, 4096 wide, us with 16 / 32: 8192 tokens
-    // of one adapter 80 / 62, of eight 107 / 94; 2048 tokens 25 / 39).
+    // of one adapter 77 / 63, of eight 98 / 89; 2048 tokens 21.5 / 23.5 and 32 / 38).
     const bool tall = R == 4 && !scan && g.tokens >= 256 * 32;
     const int64_t rows = tall ? 32 : 16, tiles = scan ? g.tokens : (g.tokens + rows - 1) / rows;
     // Parts of y's columns, as many as fill the chip if every tile has tokens.  (Each contracts x again, and workgroups that find none of

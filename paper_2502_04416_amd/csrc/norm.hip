@@ -183,7 +183,10 @@ constexpr int BACKWARD_ROWS = LANES >= 256 ? 1 : 256 / LANES;
 // A workgroup takes every grid'th set of rows and keeps its share of the sums over rows in registers, in the same columns for every row,
 // so the sums over rows cost one row of partial sums per workgroup.  All that a row reads is loaded while the row before it is worked
 // on: a row has a reduction in its middle, which nothing else would cover (4096 rows of 4096, bf16, all operands: 59 -> 32 us, 168 MB at
-// 5.3 TB/s).  With more than one chunk per thread there are no registers for that, nor for the weights.
+// 5.3 TB/s).  Beyond 8192 columns a workgroup of 1024 threads has more than one chunk per thread and 128 registers for each: nothing is loaded
+// ahead, the weights are read for every row, and what does not fit is spilled (two chunks: 3 to 30 registers; four: 142 to 195).  All
+// operands: bf16 2048 x 8192 without spills 168 MB in 38 us; of 336 MB each (62 us at 5.4 TB/s) bf16 2048 x 16384 102, 1024 x 32768 279, fp32
+// 1024 x 16384 90, 512 x 32768 202.
 template <typename T, int LANES, int CH, bool LAYER, int EDGE>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_backward_kernel(NormBackward<T> a) {
   constexpr int ROWS = BACKWARD_ROWS<LANES>;
