@@ -287,7 +287,7 @@ int cmoe_probe_hbm(size_t bytes, int reps, double* gbytes_per_s);
  * CMOE_GEMM1_CFG, CMOE_GEMM2_CFG, CMOE_XCD_REMAP, CMOE_SPLITK, CMOE_ZERO_PAD, CMOE_DECODE_FUSE,
  * CMOE_FRONT_SHARED, CMOE_FORCE_SIMT, CMOE_LDPAD, CMOE_HOST_THREADS, CMOE_SKIP_ROWS, CMOE_DECODE_SPLIT,
  * CMOE_WS_DOWN, CMOE_SKIP_STAGE, CMOE_REPEAT_STAGE, CMOE_FRONT_ALL, CMOE_FRONT_TILE, CMOE_F32_ROWS1,
- * CMOE_F32_ROWS2) takes `value` from the next call on; -1
+ * CMOE_F32_ROWS2, CMOE_MAT_TILE, CMOE_MAT_SPLIT) takes `value` from the next call on; -1
  * restores the per-batch choice of the tile-shape switches.  For A/B measurements and tests inside one process; every default is the measured best.  Not
  * synchronised against forwards being enqueued from other host threads.  CMOE_SKIP_STAGE = 3, 4 or 5 is a
  * measurement aid: every forward then leaves out its gate/up, down or combine launch (its output is
@@ -421,6 +421,118 @@ typedef struct {
 } cmoe_adapters_backward_args;
 size_t cmoe_adapters_backward_workspace_bytes(int64_t tokens, int32_t d_in, int32_t d_out, int32_t rank, int32_t n_adapters, int32_t dtype);
 int cmoe_adapters_backward(const cmoe_adapters_backward_args* args, void* hip_stream);
+
+/* ---- operators of a training step: the feed-forward block, the loss, the gradients' norm --- *
+ * Conventions as above: contiguous [rows, cols] batches at any address an element may have (rows of multiples of 8 elements at 16-byte
+ * addresses run on faster kernels), sums in fp32, enqueue only, no atomics, outputs that overlap nothing but, where it is said, the very
+ * buffer of an input.  Workspaces are 16-byte aligned and may be shared by calls that one stream orders; the functions that say their size
+ * return 0 where none is needed.  Tokens, widths and vocabularies are at most 2^20. */
+
+/* The gated feed-forward block F(x) of Eq. 3 on matrices that are trained: gate = x w_gate, up = x w_up,
+ * hidden = gate / (1 + exp(-gate)) * up, each rounded to dtype where it is stored; y = base + hidden w_down (of hidden as stored).
+ * y may be base itself. */
+typedef struct {
+  const void* x;             /* [tokens, d] */
+  const void* w_gate;        /* [d, d_ff] */
+  const void* w_up;          /* [d, d_ff] */
+  const void* w_down;        /* [d_ff, d] */
+  const void* base;          /* [tokens, d], or NULL: 0 */
+  void* hidden;              /* [tokens, d_ff]: for the product behind it, and for the backward pass */
+  void* gate;                /* [tokens, d_ff]: for the backward pass, or NULL, with up */
+  void* up;
+  void* y;                   /* [tokens, d] */
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t tokens;
+  int32_t struct_bytes;      /* sizeof(cmoe_ffn_forward_args) */
+  int32_t dtype, d, d_ff;
+} cmoe_ffn_forward_args;
+size_t cmoe_ffn_forward_workspace_bytes(int64_t tokens, int32_t d, int32_t d_ff, int32_t dtype);
+int cmoe_ffn_forward(const cmoe_ffn_forward_args* args, void* hip_stream);
+
+/* Gradients, from what the forward pass stored, with s = 1 / (1 + exp(-gate)) and dh = dy w_down^T (not rounded):
+ * dgate = dh * up * s * (1 + gate * (1 - s)), dup = dh * gate * s, rounded to dtype; from these as stored dx = dx_base + dgate w_gate^T +
+ * dup w_up^T, dw_gate = x^T dgate, dw_up = x^T dup; dw_down = hidden^T dy.  Gradients of matrices have the matrices' dtype.  dgate and dup may be
+ * gate and up themselves, dx may be dx_base.  No tokens: gradients of zeros. */
+typedef struct {
+  const void* dy;            /* [tokens, d] */
+  const void* x;             /* needed for dw_gate and dw_up */
+  const void* gate;
+  const void* up;
+  const void* hidden;        /* needed for dw_down */
+  const void* w_gate;        /* needed for dx */
+  const void* w_up;          /* needed for dx */
+  const void* w_down;
+  const void* dx_base;       /* [tokens, d], or NULL: 0 */
+  void* dgate;               /* [tokens, d_ff] */
+  void* dup;                 /* [tokens, d_ff] */
+  void* dx;                  /* [tokens, d] or NULL */
+  void* dw_gate;             /* [d, d_ff] or NULL */
+  void* dw_up;               /* [d, d_ff] or NULL */
+  void* dw_down;             /* [d_ff, d] or NULL */
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t tokens;
+  int32_t struct_bytes;      /* sizeof(cmoe_ffn_backward_args) */
+  int32_t dtype, d, d_ff;
+} cmoe_ffn_backward_args;
+size_t cmoe_ffn_backward_workspace_bytes(int64_t tokens, int32_t d, int32_t d_ff, int32_t dtype);
+int cmoe_ffn_backward(const cmoe_ffn_backward_args* args, void* hip_stream);
+
+/* Softmax cross entropy of a head over a vocabulary, whose logits z = x weight^T are never stored: lse[t] = log sum_v exp(z[t, v]),
+ * loss[t] = lse[t] - z[t, ids[t]].  A token whose id is not in [0, vocab) has no target: its loss is 0.  A row whose logits
+ * hold a NaN or +infinity has an lse that is NaN. */
+typedef struct {
+  const void* x;             /* [tokens, d] */
+  const void* weight;        /* [vocab, d] */
+  const int32_t* ids;        /* [tokens] */
+  float* loss;               /* [tokens], or NULL */
+  float* lse;                /* [tokens]: for the backward pass, or NULL */
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t tokens;
+  int32_t struct_bytes;      /* sizeof(cmoe_head_loss_forward_args) */
+  int32_t dtype, d, vocab;
+} cmoe_head_loss_forward_args;
+size_t cmoe_head_loss_forward_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int32_t dtype);
+int cmoe_head_loss_forward(const cmoe_head_loss_forward_args* args, void* hip_stream);
+
+/* Gradients of scale * sum over t of dloss[t] * loss[t]: dz[t, v] = dloss[t] * (exp(z[t, v] - lse[t]) - [v == ids[t]]), 0 for a token without a
+ * target, rounded to dtype, in pieces of the vocabulary; dx = scale * dz weight, dweight = scale * dz^T x, of the tensors' dtype.
+ * No tokens: a dweight of zeros. */
+typedef struct {
+  const void* x;
+  const void* weight;
+  const int32_t* ids;
+  const float* lse;          /* of the forward pass */
+  const float* dloss;        /* [tokens], or NULL: 1 */
+  void* dx;                  /* [tokens, d] or NULL */
+  void* dweight;             /* [vocab, d] or NULL */
+  void* workspace;
+  uint64_t workspace_bytes;
+  int64_t tokens;
+  int32_t struct_bytes;      /* sizeof(cmoe_head_loss_backward_args) */
+  int32_t dtype, d, vocab;
+  float scale;
+  int32_t reserved;
+} cmoe_head_loss_backward_args;
+size_t cmoe_head_loss_backward_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int32_t dtype);
+int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args, void* hip_stream);
+
+/* The norm n of all tensors of a list together and, with c = min(1, max_norm / (n + eps)), out = c * g of each, rounded to its dtype.
+ * Squares and sums are fp64.  out may be g itself (and then nothing is written where c = 1); the same tensor may be listed twice only with
+ * outputs of their own.  max_norm = infinity: c = 1, whatever the norm.  A norm that is infinite or NaN shows in every gradient:
+ * c is 0 or NaN.  The list is host memory, read during the call. */
+typedef struct {
+  const void* g;
+  void* out;
+  int64_t elements;          /* 0: the addresses are not looked at */
+  int32_t dtype;
+  int32_t reserved;
+} cmoe_gradient;
+size_t cmoe_clip_gradients_workspace_bytes(const cmoe_gradient* list, int32_t count);
+int cmoe_clip_gradients(const cmoe_gradient* list, int32_t count, float max_norm, float eps, float* norm, void* workspace,
+                        size_t workspace_bytes, void* hip_stream);
 
 const char* cmoe_last_error(void);   /* thread-local, never NULL */
 const char* cmoe_version(void);

@@ -45,6 +45,9 @@ EXPORTS = [
     "cmoe_forward_plan", "cmoe_hier_forward_plan", "cmoe_scorer_plan",
     "cmoe_dropout", "cmoe_norm_forward", "cmoe_norm_backward", "cmoe_norm_backward_workspace_bytes",
     "cmoe_adapters_forward", "cmoe_adapters_backward", "cmoe_adapters_backward_workspace_bytes",
+    "cmoe_ffn_forward", "cmoe_ffn_forward_workspace_bytes", "cmoe_ffn_backward", "cmoe_ffn_backward_workspace_bytes",
+    "cmoe_head_loss_forward", "cmoe_head_loss_forward_workspace_bytes", "cmoe_head_loss_backward", "cmoe_head_loss_backward_workspace_bytes",
+    "cmoe_clip_gradients", "cmoe_clip_gradients_workspace_bytes",
 ]
 
 
@@ -112,12 +115,19 @@ def load():
     lib.cmoe_hier_forward_plan.argtypes = [vp, C.c_int, i64, i32p]
     lib.cmoe_scorer_plan.argtypes = [vp, i64, i32p]
     lib.cmoe_dropout.argtypes = [vp, vp, vp, i64, C.c_int32, C.c_int32, C.c_double, C.c_uint64, C.c_uint64, vp]
-    for name in ("cmoe_norm_forward", "cmoe_norm_backward", "cmoe_adapters_forward", "cmoe_adapters_backward"):
+    for name in ("cmoe_norm_forward", "cmoe_norm_backward", "cmoe_adapters_forward", "cmoe_adapters_backward", "cmoe_ffn_forward", "cmoe_ffn_backward",
+                 "cmoe_head_loss_forward", "cmoe_head_loss_backward"):
         getattr(lib, name).argtypes = [C.c_char_p, vp]                   # the packed bytes of an argument struct
     lib.cmoe_norm_backward_workspace_bytes.argtypes = [i64, C.c_int32]
     lib.cmoe_norm_backward_workspace_bytes.restype = sz
     lib.cmoe_adapters_backward_workspace_bytes.argtypes = [i64] + [C.c_int32] * 5
     lib.cmoe_adapters_backward_workspace_bytes.restype = sz
+    for name in ("cmoe_ffn_forward", "cmoe_ffn_backward", "cmoe_head_loss_forward", "cmoe_head_loss_backward"):
+        size = getattr(lib, name + "_workspace_bytes")
+        size.argtypes, size.restype = [i64] + [C.c_int32] * 3, sz
+    lib.cmoe_clip_gradients_workspace_bytes.argtypes = [C.c_char_p, C.c_int32]      # the packed bytes of the list
+    lib.cmoe_clip_gradients_workspace_bytes.restype = sz
+    lib.cmoe_clip_gradients.argtypes = [C.c_char_p, C.c_int32, C.c_float, C.c_float, vp, vp, sz, vp]
     lib.cmoe_last_error.restype = C.c_char_p
     lib.cmoe_version.restype = C.c_char_p
     _lib = lib
@@ -570,6 +580,142 @@ def adapters_backward(dy, x, u, a, b, scale, *, ids=None, dx=None, dx_base=None,
     args = _ADAPTERS_BACKWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, d.p, d.seed, d.offset, _ADAPTERS_BACKWARD.size, code,
                                    d_in, d_out, rank, n)
     _check(load().cmoe_adapters_backward(args, stream), "cmoe_adapters_backward")
+
+
+# ---- operators of a training step ------------------------------------------------------------------
+
+_FFN_FORWARD = struct.Struct("=11Qq4i")              # cmoe_ffn_forward_args
+_FFN_BACKWARD = struct.Struct("=17Qq4i")             # cmoe_ffn_backward_args
+_HEAD_LOSS_FORWARD = struct.Struct("=7Qq4i")         # cmoe_head_loss_forward_args
+_HEAD_LOSS_BACKWARD = struct.Struct("=9Qq4ifi")      # cmoe_head_loss_backward_args
+_GRADIENT = struct.Struct("=QQqii")                  # cmoe_gradient
+
+
+def _ffn_shapes(x_name: str, x, w_down):
+    dtype, code = _dtype_of(x_name, x)
+    if x.dim() != 2 or w_down.dim() != 2 or x.shape[1] != w_down.shape[1]:
+        raise CmoeError("ffn: %s must be [tokens, d] and w_down [d_ff, d]" % x_name)
+    t, d = x.shape
+    f = w_down.shape[0]
+    if (d | f) >> 31:
+        raise _beyond_32_bits("ffn", max(d, f))
+    return dtype, code, t, d, f
+
+
+def ffn_forward(x, y, w_gate, w_up, w_down, hidden, *, gate=None, up=None, base=None) -> None:
+    """gate = x @ w_gate, up = x @ w_up, hidden = gate / (1 + exp(-gate)) * up, y = base + hidden @ w_down, on matrices that are trained.
+
+    x, y, base: [tokens, d] (y may be base itself; without a base it is 0); w_gate, w_up: [d, d_ff]; w_down: [d_ff, d]; hidden and, for the
+    backward pass, gate and up: [tokens, d_ff], all of one type.  y is the product of hidden as it is stored."""
+    dtype, code, t, d, f = _ffn_shapes("x", x, w_down)
+    dev, stream = _place("x", x)
+    operands = (
+        _operand("x", x, dtype, (t, d), dev), _operand("w_gate", w_gate, dtype, (d, f), dev), _operand("w_up", w_up, dtype, (d, f), dev),
+        _operand("w_down", w_down, dtype, (f, d), dev), _operand("base", base, dtype, (t, d), dev), _operand("hidden", hidden, dtype, (t, f), dev),
+        _operand("gate", gate, dtype, (t, f), dev), _operand("up", up, dtype, (t, f), dev), _operand("y", y, dtype, (t, d), dev))
+    lib = load()
+    nbytes = lib.cmoe_ffn_forward_workspace_bytes(t, d, f, code)
+    ws = _workspace(nbytes) if nbytes else None
+    _check(lib.cmoe_ffn_forward(_FFN_FORWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, _FFN_FORWARD.size, code, d, f), stream), "cmoe_ffn_forward")
+
+
+def ffn_backward(dy, x, gate, up, hidden, w_gate, w_up, w_down, dgate, dup, *, dx=None, dx_base=None, dw_gate=None, dw_up=None, dw_down=None) -> None:
+    """Gradients of ffn_forward from what it stored.
+
+    dgate, dup: [tokens, d_ff], the gradients of gate and up (which they may be themselves); from these as stored dx = dx_base + what reaches x
+    through the block (dx may be dx_base itself), dw_gate and dw_up; dw_down from hidden.  All of one type, the matrices' gradients too."""
+    dtype, code, t, d, f = _ffn_shapes("dy", dy, w_down)
+    dev, stream = _place("dy", dy)
+    operands = (
+        _operand("dy", dy, dtype, (t, d), dev), _operand("x", x, dtype, (t, d), dev), _operand("gate", gate, dtype, (t, f), dev),
+        _operand("up", up, dtype, (t, f), dev), _operand("hidden", hidden, dtype, (t, f), dev), _operand("w_gate", w_gate, dtype, (d, f), dev),
+        _operand("w_up", w_up, dtype, (d, f), dev), _operand("w_down", w_down, dtype, (f, d), dev), _operand("dx_base", dx_base, dtype, (t, d), dev),
+        _operand("dgate", dgate, dtype, (t, f), dev), _operand("dup", dup, dtype, (t, f), dev), _operand("dx", dx, dtype, (t, d), dev),
+        _operand("dw_gate", dw_gate, dtype, (d, f), dev), _operand("dw_up", dw_up, dtype, (d, f), dev), _operand("dw_down", dw_down, dtype, (f, d), dev))
+    lib = load()
+    nbytes = lib.cmoe_ffn_backward_workspace_bytes(t, d, f, code)
+    ws = _workspace(nbytes) if nbytes else None
+    _check(lib.cmoe_ffn_backward(_FFN_BACKWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, _FFN_BACKWARD.size, code, d, f), stream), "cmoe_ffn_backward")
+
+
+def _head_shapes(x, weight):
+    dtype, code = _dtype_of("x", x)
+    if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[1]:
+        raise CmoeError("head: x must be [tokens, d] and weight [vocab, d]")
+    t, d = x.shape
+    v = weight.shape[0]
+    if (d | v) >> 31:
+        raise _beyond_32_bits("head", max(d, v))
+    return dtype, code, t, d, v
+
+
+def head_loss_forward(x, weight, ids, loss=None, lse=None) -> None:
+    """Softmax cross entropy of a head over a vocabulary, without its logits z = x @ weight.t() in memory: lse = log sum exp z,
+    loss = lse - z[ids], 0 for a token whose id is not in [0, vocab).
+
+    x: [tokens, d]; weight: [vocab, d]; ids: [tokens] int32; loss, lse (for the backward pass): [tokens] fp32, one of them at least."""
+    dtype, code, t, d, v = _head_shapes(x, weight)
+    dev, stream = _place("x", x)
+    import torch
+    operands = (
+        _operand("x", x, dtype, (t, d), dev), _operand("weight", weight, dtype, (v, d), dev), _operand("ids", ids, torch.int32, (t,), dev),
+        _operand("loss", loss, torch.float32, (t,), dev), _operand("lse", lse, torch.float32, (t,), dev))
+    lib = load()
+    nbytes = lib.cmoe_head_loss_forward_workspace_bytes(t, d, v, code)
+    ws = _workspace(nbytes) if nbytes else None
+    _check(lib.cmoe_head_loss_forward(_HEAD_LOSS_FORWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, _HEAD_LOSS_FORWARD.size, code, d, v), stream),
+           "cmoe_head_loss_forward")
+
+
+def head_loss_backward(x, weight, ids, lse, *, dx=None, dweight=None, dloss=None, scale: float = 1.0) -> None:
+    """Gradients of scale * sum(dloss * loss) from the forward pass's lse: dx and dweight, of x's type; one of them at least.
+
+    dloss: [tokens] fp32, None: 1 for every token.  A factor that all tokens share, 1 / their number for instance, belongs into scale,
+    which is not rounded to the type on the way."""
+    dtype, code, t, d, v = _head_shapes(x, weight)
+    if not -3.4e38 <= scale <= 3.4e38:
+        raise CmoeError("scale must be finite")
+    dev, stream = _place("x", x)
+    import torch
+    operands = (
+        _operand("x", x, dtype, (t, d), dev), _operand("weight", weight, dtype, (v, d), dev), _operand("ids", ids, torch.int32, (t,), dev),
+        _operand("lse", lse, torch.float32, (t,), dev), _operand("dloss", dloss, torch.float32, (t,), dev), _operand("dx", dx, dtype, (t, d), dev),
+        _operand("dweight", dweight, dtype, (v, d), dev))
+    lib = load()
+    nbytes = lib.cmoe_head_loss_backward_workspace_bytes(t, d, v, code)
+    ws = _workspace(nbytes) if nbytes else None
+    args = _HEAD_LOSS_BACKWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, _HEAD_LOSS_BACKWARD.size, code, d, v, scale, 0)
+    _check(lib.cmoe_head_loss_backward(args, stream), "cmoe_head_loss_backward")
+
+
+def clip_gradients(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6) -> None:
+    """norm[0] = the norm of all tensors of the list together; each scaled by min(1, max_norm / (norm + eps)), in place or into out's.
+
+    grads, out: lists of contiguous tensors of any shapes, bfloat16 or float32 each; norm: [1] fp32.  max_norm = inf: the norm alone (out's
+    tensors are then copies)."""
+    if not max_norm >= 0.0 or not 0.0 <= eps <= 3e38:
+        raise CmoeError("clip_gradients: max_norm and eps must not be negative, eps finite")
+    if max_norm > 3.4e38:
+        max_norm = float("inf")
+    if out is None:
+        out = grads
+    elif len(out) != len(grads):
+        raise CmoeError("clip_gradients: out must have a tensor for each of grads")
+    dev, stream = _place("norm", norm)
+    import torch
+    to = _operand("norm", norm, torch.float32, (1,), dev)
+    listed, code = [], {torch.bfloat16: CMOE_BF16, torch.float32: CMOE_F32}
+    for g, o in zip(grads, out):
+        dtype = g.dtype
+        if dtype not in code:
+            raise CmoeError("grads must be bfloat16 or float32, not %s" % dtype)
+        at = _operand("grads", g, dtype, g.shape, dev)
+        listed.append(_GRADIENT.pack(at, at if o is g else _operand("out", o, dtype, g.shape, dev), g.numel(), code[dtype], 0))
+    packed, n = b"".join(listed), len(listed)
+    lib = load()
+    nbytes = lib.cmoe_clip_gradients_workspace_bytes(packed, n)
+    ws = _workspace(nbytes) if nbytes else None
+    _check(lib.cmoe_clip_gradients(packed, n, max_norm, eps, to, ws.data_ptr() if nbytes else 0, nbytes, stream), "cmoe_clip_gradients")
 
 
 # ---- conveniences for tests and the bench ----------------------------------------------------------

@@ -52,6 +52,8 @@ static const TuningField kTuningFields[] = {
     {"CMOE_REPEAT_STAGE", &Tuning::repeat_stage}, {"CMOE_FRONT_ALL", &Tuning::front_all},
     {"CMOE_FRONT_TILE", &Tuning::front_tile},   {"CMOE_F32_ROWS1", &Tuning::f32_rows1},
     {"CMOE_F32_ROWS2", &Tuning::f32_rows2},
+    {"CMOE_MAT_TILE", &Tuning::mat_tile},
+    {"CMOE_MAT_SPLIT", &Tuning::mat_split},
 };
 
 Tuning& tuning() {

@@ -175,6 +175,8 @@ struct Tuning {
                            // issues twice (the second finds the weights in the cache: a lower bound).  6: the
                            // decode front end's scoring launch twice (small operands, cached either way), so
                            // that (loop without the down launch) - (this gain) is the selection launch's cost.
+  int mat_tile = -1;       // tile of the training operators' products (enum Tile of matmul_launch.h) where it can run; -1: per call
+  int mat_split = -1;      // K split of those that can be split; -1: per call
 };
 Tuning& tuning();
 

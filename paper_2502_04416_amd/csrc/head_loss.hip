@@ -1,0 +1,190 @@
+// Softmax cross entropy of a head over a vocabulary, without its logits in memory.
+//   forward    z = X W^T piece by piece in registers: every tile leaves the largest logit m of its columns of a row and the sum of
+//              exp(z - m), and the target's logit; lse = log sum exp z over the ranges, loss = lse - z[target], 0 without a target
+//   backward   in pieces of the vocabulary: z once more, dZ = weight * (exp(z - lse) - [target]) of a piece in the type, then
+//              dX += dZ W (fp32 between the pieces) and dW = scale * dZ^T X, complete for the piece's rows
+// What a piece costs beside its products is dX's sums, read and written, so pieces are as wide as 128 MB of dZ (in bf16) allow:
+// it is read twice soon after it is written, and this part's last cache holds 256 MB.
+// `scale` is applied to the sums in fp32, and not to dZ: what all tokens share would round the entries of all targets, which are all
+// close to -scale, to the same side.
+#include <algorithm>
+
+#include "../../include/cmoe.h"
+#include "cmoe_internal.h"
+#include "matmul_device.h"
+#include "operator_args.h"
+
+namespace cmoe {
+namespace {
+
+constexpr int64_t MOST = 1 << 20;
+constexpr int64_t PIECE_ELEMS = 64 << 20;
+constexpr int64_t PIECE_LEAST = 1024;
+
+int check_sizes(const char* what, int32_t dtype, int64_t tokens, int32_t d, int32_t vocab) {
+  if (dtype != CMOE_F32 && dtype != CMOE_BF16) return fail(CMOE_EINVAL, "%s: dtype must be CMOE_F32 or CMOE_BF16", what);
+  if (tokens < 0 || tokens > MOST || d < 1 || d > MOST || vocab < 1 || vocab > MOST)
+    return fail(CMOE_EINVAL, "%s: need 0 <= tokens <= 2^20, d and vocab from 1 to 2^20", what);
+  return CMOE_OK;
+}
+
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+
+struct ForwardSpace {
+  size_t part, picked, total;              // offsets of the ranges and of the targets' logits
+  ForwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
+    part = 0;
+    picked = round16((size_t)lse_ranges(dtype, t, vocab, d) * t * sizeof(float2));
+    total = picked + round16((size_t)t * 4);
+  }
+};
+
+struct BackwardSpace {
+  int64_t piece, ld;                       // vocabulary entries of a piece, elements of a row of dZ
+  size_t acc, slab, total, slab_bytes;     // dZ at 0
+  BackwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
+    piece = std::max(PIECE_LEAST, PIECE_ELEMS / std::max<int64_t>(t, 1) / 256 * 256);
+    piece = std::min(piece, vocab);
+    ld = (piece + 7) / 8 * 8;
+    acc = round16((size_t)t * ld * elem_size(dtype));
+    slab = acc + (piece < vocab ? (size_t)round16((size_t)t * d * 4) : 0);
+    slab_bytes = 0;
+    const int64_t last = vocab - (vocab - 1) / piece * piece;
+    for (int64_t w : {piece, last})
+      slab_bytes = std::max({slab_bytes, matmul_slab_bytes(PRODUCT_DHEAD, dtype, t, d, (w + 7) / 8 * 8), matmul_slab_bytes(PRODUCT_DW, dtype, w, d, t)});
+    total = slab + slab_bytes;
+  }
+};
+
+// A row's ranges joined: ROWS rows to a workgroup, its threads over the ranges, then in LDS.
+template <int ROWS>
+__global__ __launch_bounds__(256) void head_finish(const float2* part, int ranges, const float* picked, const int32_t* ids, int vocab, int64_t tokens, float* loss,
+                                                   float* lse) {
+  __shared__ float2 joined[256];
+  constexpr int GROUPS = 256 / ROWS;
+  const int r = threadIdx.x % ROWS, g = threadIdx.x / ROWS;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + r;
+  float2 mine = {-INFINITY, 0.0f};
+  if (row < tokens) {
+#pragma unroll 4
+    for (int i = g; i < ranges; i += GROUPS) mine = join_ranges(mine, part[(int64_t)i * tokens + row]);
+  }
+  joined[threadIdx.x] = mine;
+  for (int half = GROUPS / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (g < half) joined[threadIdx.x] = mine = join_ranges(mine, joined[threadIdx.x + half * ROWS]);
+  }
+  if (g == 0 && row < tokens) {
+    const float l = mine.x + logf(mine.y);
+    if (lse) lse[row] = l;
+    if (loss) loss[row] = (uint32_t)ids[row] < (uint32_t)vocab ? l - picked[row] : 0.0f;
+  }
+}
+
+int check_workspace(const char* what, const void* ws, uint64_t have, size_t need) {
+  if (!ws || (uintptr_t)ws % 16 != 0) return fail(CMOE_EINVAL, "%s: the workspace is null or not aligned to 16 bytes", what);
+  if (have < need) return fail(CMOE_EINVAL, "%s: the workspace has %llu bytes and needs %llu", what, (unsigned long long)have, (unsigned long long)need);
+  return CMOE_OK;
+}
+
+int launched(const char* what, hipError_t e) { return e == hipSuccess ? CMOE_OK : fail(CMOE_EHIP, "%s: %s", what, hipGetErrorString(e)); }
+
+}  // namespace
+}  // namespace cmoe
+
+extern "C" size_t cmoe_head_loss_forward_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int32_t dtype) {
+  using namespace cmoe;
+  return check_sizes("cmoe_head_loss_forward", dtype, tokens, d, vocab) || tokens == 0 ? 0 : ForwardSpace(dtype, tokens, d, vocab).total;
+}
+
+extern "C" int cmoe_head_loss_forward(const cmoe_head_loss_forward_args* args, void* hip_stream) {
+  using namespace cmoe;
+  const char* what = "cmoe_head_loss_forward";
+  if (!args || args->struct_bytes != (int32_t)sizeof(*args)) return fail(CMOE_EINVAL, "%s: the arguments are null or a struct of another version", what);
+  const auto& a = *args;
+  if (int rc = check_sizes(what, a.dtype, a.tokens, a.d, a.vocab)) return rc;
+  if (a.tokens == 0) return CMOE_OK;
+  if (!a.x || !a.weight || !a.ids) return fail(CMOE_EINVAL, "%s: x, weight or ids is null", what);
+  if (!a.loss && !a.lse) return fail(CMOE_EINVAL, "%s: neither loss nor lse is given", what);
+  const size_t es = elem_size(a.dtype);
+  const ForwardSpace ws(a.dtype, a.tokens, a.d, a.vocab);
+  if (int rc = check_workspace(what, a.workspace, a.workspace_bytes, ws.total)) return rc;
+  const uint64_t rows = (uint64_t)a.tokens * 4;
+  if (int rc = check_operands(what, {{"x", a.x, (uint64_t)a.tokens * a.d * es, es}, {"weight", a.weight, (uint64_t)a.vocab * a.d * es, es}, {"ids", a.ids, rows, 4}},
+                              {{"loss", a.loss, rows, 4}, {"lse", a.lse, rows, 4}, {"the workspace", a.workspace, ws.total, 16}}))
+    return rc;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  char* base = static_cast<char*>(a.workspace);
+  MatArgs p = {};
+  p.a = a.x, p.lda = a.d, p.b = a.weight, p.ldb = a.d;
+  p.m = (int)a.tokens, p.n = a.vocab, p.k = a.d;
+  p.ids = a.ids, p.vocab = a.vocab;
+  p.part = reinterpret_cast<float2*>(base + ws.part), p.picked = reinterpret_cast<float*>(base + ws.picked);
+  int ranges = 0;
+  if (hipError_t e = matmul(PRODUCT_LSE, a.dtype, p, 0, s, &ranges)) return launched(what, e);
+  // few rows: all threads to a row; many: neighbouring threads read neighbouring rows
+  auto finish = [&](auto kernel, int rows_of) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.tokens + rows_of - 1) / rows_of)), dim3(256), 0, s, p.part, ranges, p.picked, a.ids, a.vocab, a.tokens, a.loss, a.lse);
+  };
+  if (a.tokens <= 512) finish(head_finish<1>, 1);
+  else if (a.tokens <= 2048) finish(head_finish<8>, 8);
+  else finish(head_finish<32>, 32);
+  return launched(what, hipGetLastError());
+}
+
+extern "C" size_t cmoe_head_loss_backward_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int32_t dtype) {
+  using namespace cmoe;
+  return check_sizes("cmoe_head_loss_backward", dtype, tokens, d, vocab) || tokens == 0 ? 0 : BackwardSpace(dtype, tokens, d, vocab).total;
+}
+
+extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args, void* hip_stream) {
+  using namespace cmoe;
+  const char* what = "cmoe_head_loss_backward";
+  if (!args || args->struct_bytes != (int32_t)sizeof(*args)) return fail(CMOE_EINVAL, "%s: the arguments are null or a struct of another version", what);
+  const auto& a = *args;
+  if (int rc = check_sizes(what, a.dtype, a.tokens, a.d, a.vocab)) return rc;
+  if (!a.dx && !a.dweight) return fail(CMOE_EINVAL, "%s: neither dx nor dweight is given", what);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const size_t es = elem_size(a.dtype);
+  MatArgs w = {};
+  w.b = a.x, w.ldb = a.d, w.n = a.d, w.k = (int)a.tokens, w.ldc = a.d, w.alpha = a.scale;
+  if (a.tokens == 0) {                     // nothing to learn: a gradient of zeros
+    if (!a.dweight) return CMOE_OK;
+    if (int rc = check_operands(what, {}, {{"dweight", a.dweight, (uint64_t)a.vocab * a.d * es, es}})) return rc;
+    w.m = a.vocab, w.lda = a.vocab, w.c = a.dweight;
+    return launched(what, matmul(PRODUCT_DW, a.dtype, w, 0, s));
+  }
+  if (!a.x || !a.weight || !a.ids || !a.lse) return fail(CMOE_EINVAL, "%s: x, weight, ids or lse is null", what);
+  const BackwardSpace ws(a.dtype, a.tokens, a.d, a.vocab);
+  if (int rc = check_workspace(what, a.workspace, a.workspace_bytes, ws.total)) return rc;
+  const uint64_t rows = (uint64_t)a.tokens * 4, td = (uint64_t)a.tokens * a.d * es, vd = (uint64_t)a.vocab * a.d * es;
+  if (int rc = check_operands(what, {{"x", a.x, td, es}, {"weight", a.weight, vd, es}, {"ids", a.ids, rows, 4}, {"lse", a.lse, rows, 4}, {"dloss", a.dloss, rows, 4}},
+                              {{"dx", a.dx, td, es}, {"dweight", a.dweight, vd, es}, {"the workspace", a.workspace, ws.total, 16}}))
+    return rc;
+  char* base = static_cast<char*>(a.workspace);
+  float* slab = ws.slab_bytes ? reinterpret_cast<float*>(base + ws.slab) : nullptr;
+  for (int64_t first = 0; first < a.vocab; first += ws.piece) {
+    const int n = (int)std::min<int64_t>(ws.piece, a.vocab - first), padded = (n + 7) / 8 * 8;
+    const char* rows_of_w = static_cast<const char*>(a.weight) + (size_t)first * a.d * es;
+    MatArgs p = {};
+    p.a = a.x, p.lda = a.d, p.b = rows_of_w, p.ldb = a.d;
+    p.m = (int)a.tokens, p.n = padded, p.n_b = n, p.k = a.d;
+    p.c = base, p.ldc = ws.ld;
+    p.ids = a.ids, p.vocab = a.vocab, p.col0 = (int)first, p.lse = a.lse, p.dloss = a.dloss;
+    if (hipError_t e = matmul(PRODUCT_DLOGITS, a.dtype, p, 0, s)) return launched(what, e);
+    if (a.dx) {
+      MatArgs q = {};
+      q.a = base, q.lda = ws.ld, q.b = rows_of_w, q.ldb = a.d;
+      q.m = (int)a.tokens, q.n = a.d, q.k = padded, q.k_b = n;
+      q.acc = reinterpret_cast<float*>(base + ws.acc), q.first = first == 0, q.last = first + n == a.vocab;
+      q.c = a.dx, q.ldc = a.d, q.alpha = a.scale, q.slab = slab;
+      if (hipError_t e = matmul(PRODUCT_DHEAD, a.dtype, q, ws.slab_bytes, s)) return launched(what, e);
+    }
+    if (a.dweight) {
+      w.a = base, w.lda = ws.ld, w.m = n, w.m_a = padded;
+      w.c = static_cast<char*>(a.dweight) + (size_t)first * a.d * es, w.slab = slab;
+      if (hipError_t e = matmul(PRODUCT_DW, a.dtype, w, ws.slab_bytes, s)) return launched(what, e);
+    }
+  }
+  return CMOE_OK;
+}

@@ -1,0 +1,56 @@
+// Products of the training operators (ffn.hip, head_loss.hip): C = A * B with what each operator does to the result while it is in
+// registers.  Host interface; the kernels are in matmul_device.h.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "cmoe_internal.h"
+
+namespace cmoe {
+
+// An operand "by rows" has K along its rows (A [m, k], B [n, k]); "by columns" K runs down its columns (A [k, m], B [k, n]).
+enum Product {
+  PRODUCT_GATED,    // A by rows, B and B2 by columns: G = A B, U = A B2; c = silu(G) U, c2 = G, c3 = U (c2, c3 may be null)
+  PRODUCT_DOWN,     // A by rows, B by columns: c = e1 + A B (e1 may be null)
+  PRODUCT_DGATED,   // A, B by rows: from dH = A B^T, G = e1, U = e2: c = dG, c2 = dU
+  PRODUCT_DX,       // A, B by rows, K in two parts: c = e1 + A B^T + A2 B2^T (e1 may be null)
+  PRODUCT_DW,       // A, B by columns: c = alpha A^T B, and c2 = alpha A^T B2 where c2 is given
+  PRODUCT_LSE,      // A, B by rows: per row and column range the largest logit and the sum of exponentials; the target's logit
+  PRODUCT_DLOGITS,  // A, B by rows: c = row weight * (exp(A B^T - lse) - [target])
+  PRODUCT_DHEAD,    // A by rows, B by columns: acc (+)= A B over the pieces of a vocabulary, c = alpha * acc with the last one
+};
+
+struct MatArgs {
+  const void *a, *a2, *b, *b2;
+  int64_t lda, ldb;          // elements from one row of memory to the next (of both parts)
+  int m, n, k;               // the result is [m, n]; k: of each part
+  // what of an operand may be read where that is more or less than its part in the result: rows or columns of A (m_a >= m: padding, in
+  // any state), of B (n_b <= n: zeros behind it), and B's K (k_b <= k: zeros behind it; A has zeros there itself)
+  int m_a, n_b, k_b;
+  void *c, *c2, *c3;
+  const void *e1, *e2;
+  int64_t ldc;               // of c, c2, c3, e1 and e2
+  float alpha;
+  // head
+  float* acc;                // [m, n]
+  int first, last;           // pieces of the vocabulary
+  int col0;                  // vocabulary index of column 0
+  int vocab;
+  const int32_t* ids;        // [m]
+  const float* lse;          // [m]
+  const float* dloss;        // [m] or null
+  float2* part;              // [column ranges][m]
+  float* picked;             // [m]
+  // K split: part s of a tile stores its sums to slab [k_split][m][n], a finishing kernel adds them in order
+  int k_split;
+  float* slab;
+};
+
+// Bytes of slabs that a product may ask for, whatever its operands' alignment.
+size_t matmul_slab_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k);
+// Column ranges that PRODUCT_LSE may write: rows of `part`, whatever its operands' alignment.
+int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k);
+// Enqueues the product; m_a, n_b and k_b count as m, n and k where they are 0.  slab_bytes: what may be used at p.slab.  *ranges, of
+// PRODUCT_LSE: how many ranges have been written.
+hipError_t matmul(Product kind, int dtype, MatArgs p, size_t slab_bytes, hipStream_t s, int* ranges = nullptr);
+
+}  // namespace cmoe

@@ -1,0 +1,55 @@
+// Launches of the products' kernels (host code); one translation unit per group of products instantiates them.
+#pragma once
+#include "lds_limit.h"
+#include "matmul_device.h"
+
+namespace cmoe {
+
+// Tiles: rows, columns, columns of waves (the columns of a wave are a range of PRODUCT_LSE).
+enum Tile { ANY_128, ANY_32, TILES };
+struct TileShape {
+  int bm, bn, wgn;
+};
+constexpr TileShape kTiles[TILES] = {{128, 128, 2}, {32, 128, 4}};
+
+template <class KERNEL>
+hipError_t launch_tiles(KERNEL kernel, LdsLimit& limit, size_t lds, int bm, int bn, const MatArgs& p, int z, hipStream_t s) {
+  if (lds > 64 * 1024)
+    if (hipError_t e = limit.raise(reinterpret_cast<const void*>(kernel), lds)) return e;
+  const int64_t tiles = ((int64_t)p.m + bm - 1) / bm * (((int64_t)p.n + bn - 1) / bn);
+  hipLaunchKernelGGL(kernel, dim3(grid_of(tiles, p.k_split), z), dim3(256), lds, s, p);
+  return hipGetLastError();
+}
+
+template <int BM, int BN, int WGM, int WGN, bool ACOL, bool BCOL, class EPI>
+hipError_t launch_mat_any(const MatArgs& p, int z, hipStream_t s) {
+  static LdsLimit limit;
+  return launch_tiles(matmul_any<BM, BN, WGM, WGN, ACOL, BCOL, EPI>, limit, mat_any_bytes<typename EPI::type, BM, BN, WGM, WGN>(), BM, EPI::DUAL ? BN / 2 : BN, p, z, s);
+}
+
+template <bool ACOL, bool BCOL, class EPI>
+hipError_t launch_product(Tile tile, const MatArgs& p, hipStream_t s) {
+  const int z = EPI::PAIRED && p.c2 ? 2 : 1;
+  hipError_t e = hipErrorInvalidValue;
+  if (tile == ANY_128) e = launch_mat_any<128, 128, 2, 2, ACOL, BCOL, EPI>(p, z, s);
+  if (tile == ANY_32) e = launch_mat_any<32, 128, 1, 4, ACOL, BCOL, EPI>(p, z, s);
+  if (e != hipSuccess || p.k_split == 1) return e;
+  if constexpr (!EPI::RANGES) {
+    const int64_t threads = (int64_t)p.m * ((p.n + 7) / 8);
+    hipLaunchKernelGGL(matmul_finish<EPI>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, p);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+// By product and type; each in the translation unit of its group.
+hipError_t launch_gated(Tile, int dtype, const MatArgs&, hipStream_t);
+hipError_t launch_dgated(Tile, int dtype, const MatArgs&, hipStream_t);
+hipError_t launch_down(Tile, int dtype, const MatArgs&, hipStream_t);
+hipError_t launch_dx(Tile, int dtype, const MatArgs&, hipStream_t);
+hipError_t launch_dw(Tile, int dtype, const MatArgs&, hipStream_t);
+hipError_t launch_lse(Tile, int dtype, const MatArgs&, hipStream_t);
+hipError_t launch_dlogits(Tile, int dtype, const MatArgs&, hipStream_t);
+hipError_t launch_dhead(Tile, int dtype, const MatArgs&, hipStream_t);
+
+}  // namespace cmoe
