@@ -26,20 +26,21 @@ constexpr Shape shape_of(Product kind) {
 }
 
 // Relative time of a K step of 32 of a tile when the chip is full, and workgroups per CU.
-constexpr double kStep[TILES] = {2.6, 1.0};
-constexpr int kPerCu[TILES] = {2, 2};
+constexpr double kStep[TILES] = {1.0, 0.60, 0.42, 2.6, 1.0};
+constexpr int kPerCu[TILES] = {1, 2, 2, 2, 2};
 constexpr double kTileCost = 16;             // prologue and epilogue, in steps of the large tile
 
-Choice choose(Product kind, int64_t m, int64_t n, int64_t k, int pair, size_t slab_bytes) {
+Choice choose(Product kind, int dtype, bool ring, int64_t m, int64_t n, int64_t k, int pair, size_t slab_bytes) {
   const Shape sh = shape_of(kind);
   const int64_t steps = ((k + 31) / 32) * (sh.segments ? 2 : 1);
   const int64_t cols = sh.dual ? 2 * n : n;
   Choice best{ANY_128, 1};
   double best_cost = 1e300;
   const int forced_tile = tuning().mat_tile, forced_split = tuning().mat_split;
-  const int first = ANY_128, last = ANY_32;
+  const int first = ring ? RING_256 : ANY_128, last = ring ? RING_64 : ANY_32;
   for (int t = first; t <= last; ++t) {
-    if (forced_tile >= first && forced_tile <= last && forced_tile != t) continue;
+    if (sh.a_columns && t == RING_64) continue;
+    if (forced_tile >= first && forced_tile <= last && forced_tile != t && !(sh.a_columns && forced_tile == RING_64)) continue;
     const int64_t tiles = (m + kTiles[t].bm - 1) / kTiles[t].bm * ((cols + kTiles[t].bn - 1) / kTiles[t].bn) * pair;
     for (int split = 1; split <= 16; split *= 2) {
       if (split > 1 && (!sh.splits || pair > 1 || (size_t)split * m * cols * 4 > slab_bytes)) break;
@@ -54,6 +55,7 @@ Choice choose(Product kind, int64_t m, int64_t n, int64_t k, int pair, size_t sl
       if (cost < best_cost) best_cost = cost, best = {(Tile)t, split};
     }
   }
+  (void)dtype;
   return best;
 }
 
@@ -62,8 +64,9 @@ int64_t ranges_of(const Choice& c, int64_t n) { return (n + kTiles[c.tile].bn - 
 }  // namespace
 
 int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k) {
-  (void)dtype;
-  return ranges_of(choose(PRODUCT_LSE, m, n, k, 1, 0), n);
+  int64_t most = 0;
+  for (int ring = 0; ring <= (dtype == CMOE_BF16); ++ring) most = std::max(most, ranges_of(choose(PRODUCT_LSE, dtype, ring, m, n, k, 1, 0), n));
+  return most;
 }
 
 size_t matmul_slab_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k) {
@@ -71,11 +74,11 @@ size_t matmul_slab_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t 
   const size_t all = (size_t)1 << 40;
   const size_t one = (size_t)m * n * 4 * (shape_of(kind).dual ? 2 : 1);
   size_t most = 0;
-  (void)dtype;
-  for (int pair = 1; pair <= (kind == PRODUCT_DW ? 2 : 1); ++pair) {
-    const Choice c = choose(kind, m, n, k, pair, all);
-    if (c.k_split > 1) most = std::max(most, c.k_split * one);
-  }
+  for (int ring = 0; ring <= (dtype == CMOE_BF16); ++ring)
+    for (int pair = 1; pair <= (kind == PRODUCT_DW ? 2 : 1); ++pair) {
+      const Choice c = choose(kind, dtype, ring, m, n, k, pair, all);
+      if (c.k_split > 1) most = std::max(most, c.k_split * one);
+    }
   return most;
 }
 
@@ -84,7 +87,11 @@ hipError_t matmul(Product kind, int dtype, MatArgs p, size_t slab_bytes, hipStre
   if (!p.m_a) p.m_a = p.m;
   if (!p.n_b) p.n_b = p.n;
   if (!p.k_b) p.k_b = p.k;
-  const Choice c = choose(kind, p.m, p.n, p.k, kind == PRODUCT_DW && p.c2 ? 2 : 1, p.slab ? slab_bytes : 0);
+  const Shape sh = shape_of(kind);
+  auto wide = [](const void* q) { return ((uintptr_t)q & 15) == 0; };
+  const bool ring = dtype == CMOE_BF16 && wide(p.a) && wide(p.a2) && wide(p.b) && wide(p.b2) && p.lda % 8 == 0 && p.ldb % 8 == 0 &&
+                    (sh.a_columns ? p.m_a : p.k) % 8 == 0 && (sh.b_columns ? p.n_b : p.k) % 8 == 0;
+  const Choice c = choose(kind, dtype, ring, p.m, p.n, p.k, kind == PRODUCT_DW && p.c2 ? 2 : 1, p.slab ? slab_bytes : 0);
   p.k_split = c.k_split;
   if (ranges) *ranges = (int)ranges_of(c, p.n);
   switch (kind) {

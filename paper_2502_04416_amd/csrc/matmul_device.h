@@ -1,5 +1,17 @@
 // Kernels of the products in matmul.h.
 //
+// matmul_ring: bf16, both operands read 16 bytes at a time (widths that are multiples of 8, addresses of 16).  The ring of
+// gemm_bf16.hip with operands as they lie in a program's tensors: K steps of 32, global memory straight to LDS by buffer loads, STAGES
+// - 1 steps in flight, the fragments of the next step read from LDS while this one is multiplied out of registers.  A
+// stage holds an operand
+//   by rows     in blocks of 16 rows x 32 K (1 KB: one load instruction of a wave, one operand of an MFMA), or
+//   by columns  in panels of 32 K x 64 columns (4 KB: four load instructions of 8 K x 128 bytes): the 16 x 16 corners of an MFMA's
+//               operand are turned on the way out of LDS by ds_read_b64_tr_b16, whose 16 lanes read 4 rows of K of 16 columns
+//               (32 bytes each) and receive 4 K of one column each; two of them make an operand.
+// Both are XOR-swizzled on the global side so that the lanes of a read fall into different banks: 16-byte chunks of a block's row
+// with (row >> 2) & 3; 32-byte chunks of a panel's row k with bits 1 and 3 of k (bit 0 chooses the half of the 256-byte bank line,
+// bit 2 is the other read).
+//
 // matmul_any: both types, any alignment and size, operands through registers with every chunk's end checked.
 #pragma once
 #include <type_traits>
@@ -262,6 +274,214 @@ __device__ __forceinline__ bool find_tile(const MatArgs& p, int n_mt, int n_nt, 
   return true;
 }
 inline __host__ int grid_of(int64_t tiles, int k_split) { return (int)((tiles * k_split + 7) / 8 * 8); }
+
+// ---- the ring -------------------------------------------------------------------------------------------------------
+
+typedef short shortx4_t __attribute__((ext_vector_type(4)));
+
+// `__restrict__` is not for the programmer: inlined, it leaves the read with an alias scope, and the compiler then does not take it to wait for
+// every load into LDS that is under way (vmcnt(0) in front of each read, 0.4 of the rate; it takes ordinary reads so by their
+// type).  What they have to wait for is waited for by hand at the barrier of a step.
+__device__ __forceinline__ shortx4_t read_turned(const bf16_t* __restrict__ at) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4_t*)(at));
+#else
+  return shortx4_t{};
+#endif
+}
+
+constexpr int mat_ring_elems(int bm, int bn, int stages) { return stages * (bm + bn) * BK; }
+template <int BM, int BN, int STAGES, int WGM, int WGN>
+constexpr size_t mat_ring_bytes() {
+  const int strips = WGM * WGN * strip_floats<BM / WGM / 16, BN / WGN / 16>() * 4, ring = mat_ring_elems(BM, BN, STAGES) * 2;
+  return ring > strips ? ring : strips;
+}
+
+template <int BM, int BN, int STAGES, int WGM, int WGN, bool ACOL, bool BCOL, class EPI>
+__global__ __launch_bounds__(WGM* WGN * 64)
+__attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 1024 ? 2 : 1))) void matmul_ring(MatArgs p) {
+  constexpr int NW = WGM * WGN;
+  constexpr int TM = BM / WGM, TN = BN / WGN, MB = TM / 16, NB = TN / 16;
+  constexpr int A_CH = BM / 16 / NW, B_CH = BN / 16 / NW, LPT = A_CH + B_CH;   // load instructions per wave and step
+  constexpr int A_ELEMS = BM * BK, STAGE_ELEMS = (BM + BN) * BK;
+  static_assert(NW == 4 && BM % 64 == 0 && BN % 64 == 0, "a wave loads whole blocks and panels");
+  static_assert((!ACOL || TM % 64 == 0) && (!BCOL || EPI::DUAL || TN % 64 == 0), "panels belong to one wave column");
+  static_assert(!EPI::DUAL || (BCOL && BN % 128 == 0 && (TN / 2) % 32 == 0), "gate and up panels alternate");
+  static_assert(STAGES >= 3 && (STAGES - 1) * LPT < 64, "ring depth");
+  extern __shared__ __attribute__((aligned(16))) bf16_t smem[];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WGN, wn = wave % WGN;
+  const int r16 = lane & 15, kq = lane >> 4;
+
+  TileAt at;
+  constexpr int BNO = EPI::DUAL ? BN / 2 : BN;               // columns of the result in a tile
+  if (!find_tile(p, (p.m + BM - 1) / BM, (p.n + BNO - 1) / BNO, &at)) return;
+  const int z = blockIdx.y;
+  const int row_first = at.mt * BM, col_first = at.nt * BNO;
+  // steps of K: of one part (SEGMENTS: the second part's follow), and this workgroup's
+  const int seg_steps = (p.k + BK - 1) / BK;
+  const int all = EPI::SEGMENTS ? 2 * seg_steps : seg_steps;
+  const int per = (all + p.k_split - 1) / p.k_split;
+  const int k_begin = min(at.part * per, all), KT = min(per, all - k_begin);
+
+  // Lanes' offsets in bytes from the operand's place of a step; DMA_NONE: zeros.  By rows: load i of a wave is block wave + 4 i,
+  // lane l its row l / 4 and chunk (l % 4) ^ (row >> 2) & 3.  By columns: load i is a quarter of panel i, lane l row l / 8 of
+  // it and the 16-byte chunk that the swizzle puts at l % 8.
+  auto row_chunk = [&]() { return ((lane & 3) ^ ((lane >> 4) & 3)) << 3; };
+  const int coff = row_chunk();
+  const int pk = wave * 8 + (lane >> 3);                     // row of a panel
+  const int pcol = ((((lane & 7) >> 1) ^ (((pk >> 1) & 1) | (((pk >> 3) & 1) << 1))) << 4) + ((lane & 1) << 3);
+  uint32_t a_off[A_CH], b_off[B_CH];
+#pragma unroll
+  for (int i = 0; i < A_CH; ++i) {
+    if (ACOL) a_off[i] = row_first + i * 64 + pcol < p.m_a ? (uint32_t)((pk * p.lda + i * 64 + pcol) * 2) : DMA_NONE;
+    else a_off[i] = row_first + (wave + i * NW) * 16 + (lane >> 2) < p.m_a ? (uint32_t)((((wave + i * NW) * 16 + (lane >> 2)) * p.lda + coff) * 2) : DMA_NONE;
+  }
+#pragma unroll
+  for (int i = 0; i < B_CH; ++i) {
+    const int panel = EPI::DUAL ? i >> 1 : i;
+    if (BCOL) b_off[i] = col_first + panel * 64 + pcol < p.n_b ? (uint32_t)((pk * p.ldb + panel * 64 + pcol) * 2) : DMA_NONE;
+    else b_off[i] = col_first + (wave + i * NW) * 16 + (lane >> 2) < p.n_b ? (uint32_t)((((wave + i * NW) * 16 + (lane >> 2)) * p.ldb + coff) * 2) : DMA_NONE;
+  }
+  const bool k_past = (seg_steps - 1) * BK + coff >= p.k;    // of a part's last step, by rows
+  const bf16_t* const a1 = static_cast<const bf16_t*>(p.a) + (ACOL ? row_first : row_first * p.lda);
+  const bf16_t* const b1 = static_cast<const bf16_t*>(EPI::PAIRED && z ? p.b2 : p.b) + (BCOL ? col_first : col_first * p.ldb);
+  const bf16_t* const a2 = EPI::SEGMENTS ? static_cast<const bf16_t*>(p.a2) + row_first * p.lda : nullptr;
+  const bf16_t* const b2 = EPI::SEGMENTS ? static_cast<const bf16_t*>(p.b2) + col_first * p.ldb : EPI::DUAL ? static_cast<const bf16_t*>(p.b2) + col_first : nullptr;
+
+  // load i of step kt (counted from k_begin) of an operand; `left`: rows of it (by rows) or columns (by columns) from its place on
+  auto fetch = [&](auto col_tag, const bf16_t* base, const bf16_t* base2, int64_t ld, int left, int k, uint32_t off, int kt, bf16_t* dst) {
+    int s = kt + k_begin;
+    const bool there = kt < KT;
+    if (EPI::SEGMENTS && s >= seg_steps) {
+      s -= seg_steps;
+      base = base2;
+    }
+    if constexpr (decltype(col_tag)::value) {
+      // the 32 rows of a step are the buffer: K past its end lies past the buffer's
+      const int rows = there ? min(k - s * BK, BK) : 0;
+      const int64_t size = rows > 0 ? ((rows - 1) * ld + left) * 2 : 0;
+      dma16_buffer(uniform_ptr(base + (int64_t)s * BK * ld), __builtin_amdgcn_readfirstlane((uint32_t)min(size, (int64_t)DMA_NONE)), off, 0, dst);
+    } else {
+      const int64_t size = there ? ((left - 1) * ld + k) * 2 : 0;
+      dma16_buffer(uniform_ptr(base), __builtin_amdgcn_readfirstlane((uint32_t)min(size, (int64_t)DMA_NONE)), s == seg_steps - 1 && k_past ? DMA_NONE : off,
+                   (uint32_t)s * (BK * 2), dst);
+    }
+  };
+  auto issue = [&](int kt, int slot, int i) {
+    bf16_t* st = smem + slot * STAGE_ELEMS;
+    if (i < A_CH) {
+      fetch(std::bool_constant<ACOL>{}, a1, a2, p.lda, p.m_a - row_first, p.k, a_off[i], kt, st + (ACOL ? i * 2048 + wave * 512 : (wave + i * NW) * BLK));
+    } else {
+      const int j = i - A_CH;
+      fetch(std::bool_constant<BCOL>{}, EPI::DUAL && (j & 1) ? b2 : b1, b2, p.ldb, p.n_b - col_first, p.k_b, b_off[j], kt,
+            st + A_ELEMS + (BCOL ? j * 2048 + wave * 512 : (wave + j * NW) * BLK));
+    }
+  };
+
+  // fragments: of a block row r16, chunk kq; of a panel columns r16 of a block of 16, K kq * 8 .. + 7 in two reads
+  const int frag = r16 * BK + ((kq ^ (r16 >> 2)) << 3);
+  const int tj = r16 >> 2;                                   // K row of a read that the lane asks for
+  const int swz = ((tj >> 1) & 1) | ((kq & 1) << 1);
+  int turned[4];                                             // by block of 16 columns of a panel (DUAL, TN 64: from the wave's first on)
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int cb = (c + (EPI::DUAL ? wn * (TN / 32) : 0)) & 3;
+    turned[c] = (kq * 8 + tj) * 64 + ((cb ^ swz) << 4) + ((r16 & 3) << 2);
+  }
+  int turned_a[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) turned_a[c] = (kq * 8 + tj) * 64 + ((c ^ swz) << 4) + ((r16 & 3) << 2);
+
+  floatx4_t acc[MB][NB];
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[mb][nb][i] = 0.0f;
+
+  bf16x8_t af[2][MB], wf[2][NB];
+  auto read2 = [&](const bf16_t* from) {
+    union { shortx4_t h[2]; bf16x8_t v; } u;
+    u.h[0] = read_turned(from);
+    u.h[1] = read_turned(from + 4 * 64);
+    return u.v;
+  };
+  auto load_frag = [&](int slot, int f, int set) {           // B fragments first, then A
+    const bf16_t* st = smem + slot * STAGE_ELEMS;
+    if (f < NB) {
+      if constexpr (!BCOL) wf[set][f] = *reinterpret_cast<const bf16x8_t*>(st + A_ELEMS + (wn * NB + f) * BLK + frag);
+      else if constexpr (EPI::DUAL) {
+        const int which = f / (NB / 2), c = f % (NB / 2);    // panel of the wave's column block, in gate / up pairs
+        wf[set][f] = read2(st + A_ELEMS + ((wn * (NB / 2)) / 4 * 2 + which) * 2048 + turned[c]);
+      } else wf[set][f] = read2(st + A_ELEMS + (wn * (NB / 4) + f / 4) * 2048 + turned[f % 4]);
+    } else {
+      const int q = f - NB;
+      if constexpr (!ACOL) af[set][q] = *reinterpret_cast<const bf16x8_t*>(st + (wm * MB + q) * BLK + frag);
+      else af[set][q] = read2(st + (wm * (MB / 4) + q / 4) * 2048 + turned_a[q % 4]);
+    }
+  };
+  static_assert(!EPI::DUAL || NB / 2 <= 4, "a wave's gate columns lie in one panel");
+
+  constexpr int NM = MB * NB, NF = MB + NB, ND = LPT;
+  static_assert(ND <= NM, "at most one load instruction after an MFMA");
+#pragma unroll
+  for (int st = 0; st < STAGES; ++st)
+#pragma unroll
+    for (int i = 0; i < ND; ++i) issue(st, st, i);
+  wait_vmcnt<(STAGES - 1) * ND>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int f = 0; f < NF; ++f) load_frag(0, f, 0);
+
+  int slot = 0;
+  auto step = [&](int ks, auto set_tag, auto wait_tag) {
+    constexpr int SET = decltype(set_tag)::value;
+    constexpr bool WAIT = decltype(wait_tag)::value;
+    // this wave's loads of step ks + 1 have landed and its reads of step ks have returned: behind the barrier step ks + 1 may be
+    // read and the slot of step ks refilled (a bare barrier: __syncthreads() would drain every load)
+    wait_vmcnt<(STAGES - 2) * ND>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int next = slot + 1 == STAGES ? 0 : slot + 1;
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+      const int mb = m / NB, nb = m % NB;
+      __builtin_amdgcn_sched_barrier(0);
+      if (WAIT && m == NM - 1) mfma_acc<true>(acc[mb][nb], wf[SET][nb], af[SET][mb]);
+      else mfma_acc<false>(acc[mb][nb], wf[SET][nb], af[SET][mb]);
+      __builtin_amdgcn_sched_barrier(0);
+      // the fragments of the next step in the first three quarters of the MFMAs, the load instructions spread over all
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+        if (f * NM * 3 / (NF * 4) == m) load_frag(next, f, SET ^ 1);
+      const int i = ((m + 1) * ND + NM - 1) / NM - 1;
+      if (i < ND && (i + 1) * NM / ND - 1 == m) issue(ks + STAGES, slot, i);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    slot = next;
+  };
+  int ks = 0;
+  for (; ks + 1 < KT; ks += 2) {
+    step(ks, std::integral_constant<int, 0>{}, std::false_type{});
+    step(ks + 1, std::integral_constant<int, 1>{}, std::true_type{});
+  }
+  if (ks < KT) step(ks, std::integral_constant<int, 0>{}, std::true_type{});
+  __builtin_amdgcn_sched_barrier(0);
+  wait_vmcnt<0>();                                           // (no load into LDS may outlive the workgroup)
+  const int64_t row0 = row_first + wm * TM;
+  if constexpr (EPI::RANGES) {
+    put_ranges<MB, NB>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
+  } else {
+    __syncthreads();                                         // every wave has left the ring
+    put_tile<MB, NB, EPI>(p, acc, reinterpret_cast<float*>(smem) + wave * strip_floats<MB, NB>(), z, at.part, row0, col_first + wn * (EPI::DUAL ? TN / 2 : TN));
+  }
+}
 
 // ---- any size, alignment and type -----------------------------------------------------------------------------------
 

@@ -1,6 +1,7 @@
 """The feed-forward block, the head's loss and the clipping on the GPU against their definitions in 64 bits (training_oracle.py).
 
-Tensors lie in larger buffers of NaN at addresses of an element's alignment or of 16 bytes; tiles and K splits are forced in turn.
+Tensors lie in larger buffers of NaN: at addresses of an element's alignment, where the kernels that take any operand run, or of 16 bytes,
+where widths of multiples of 8 run on the ring, with every tile and K split forced in turn.
 """
 import pytest
 import torch
@@ -11,8 +12,9 @@ from test_gpu_operators import Arena, TYPES
 
 pytestmark = pytest.mark.gpu
 
-ANY = {"any 128": 0, "any 32": 1}
-TILES = {None: -1, **ANY}
+RING = {"ring 256": 0, "ring 128": 1, "ring 64": 2}
+ANY = {"any 128": 3, "any 32": 4}
+TILES = {None: -1, **RING, **ANY}
 
 
 @pytest.fixture(scope="module")
@@ -93,6 +95,14 @@ def test_ffn_of_any_size_and_address(B, dtype, t, d, f):
 def test_ffn_on_the_tiles_for_any_operand(B, forced, dtype, tile, split):
     forced(tile, split)
     run_ffn(B, Arena(split, shift=3), TYPES[dtype], 135, 139, 270, base=True)
+
+
+@pytest.mark.parametrize("tile", list(RING))
+@pytest.mark.parametrize("split", [1, 2, 8])
+@pytest.mark.parametrize("t,d,f", [(1, 8, 8), (64, 64, 64), (130, 200, 328), (300, 264, 520), (600, 520, 264), (77, 1032, 136), (1030, 72, 776)])
+def test_ffn_on_the_ring(B, forced, tile, split, t, d, f):
+    forced(tile, split)
+    run_ffn(B, Arena(t + split, shift=0), TYPES["bf16"], t, d, f, base=split == 2)
 
 
 @pytest.mark.parametrize("t,d,f", [(1, 4096, 1032), (24, 1032, 4096), (2048, 512, 768), (4100, 128, 264)])
@@ -198,7 +208,14 @@ def test_head_of_any_size_and_address(B, dtype, t, d, v):
     run_head(B, Arena(t + v, shift=1), TYPES[dtype], t, d, v, weighted=t % 2 == 1)
 
 
-@pytest.mark.parametrize("tile", list(ANY))
+@pytest.mark.parametrize("tile", list(RING))
+@pytest.mark.parametrize("t,d,v", [(1, 64, 40), (70, 136, 257), (300, 64, 1003), (257, 520, 130), (64, 32, 2050)])
+def test_head_on_the_ring(B, forced, tile, t, d, v):
+    forced(tile)
+    run_head(B, Arena(t + v, shift=0), TYPES["bf16"], t, d, v, weighted=t % 2 == 1)
+
+
+@pytest.mark.parametrize("tile", list(RING) + list(ANY))
 @pytest.mark.parametrize("split", [2, 16])
 def test_head_with_k_splits(B, forced, tile, split):
     forced(tile, split)

@@ -1,0 +1,42 @@
+"""The machine code that was built here for the training operators' ring kernels, on the CPU: the distances around the MFMAs that are written as
+assembly, and that nothing between them waits for the loads into LDS but the barrier of a K step, which leaves all but one step under way."""
+import os
+import subprocess
+
+import pytest
+
+from test_kernel_code_cpu import LIB, OBJDUMP, code_objects, parse, violations
+
+
+@pytest.fixture(scope="module")
+def kernels(tmp_path_factory):
+    if not os.path.exists(LIB):
+        import __graft_entry__
+        __graft_entry__.build()
+    found = {}
+    for i, obj in enumerate(code_objects(LIB)):
+        if b"matmul_ring" not in obj:
+            continue
+        path = tmp_path_factory.mktemp("code") / ("%d.o" % i)
+        path.write_bytes(obj)
+        listing = subprocess.run([OBJDUMP, "-d", str(path)], capture_output=True, text=True, check=True).stdout
+        found.update(parse(listing, "matmul_ring"))
+    return found
+
+
+def test_mfma_results_are_waited_for(kernels):
+    assert len(kernels) >= 23
+    bad = {name: violations(code) for name, code in kernels.items() if violations(code)}
+    assert not bad, bad
+
+
+def test_nothing_waits_for_the_loads_but_the_barrier(kernels):
+    # loads per wave and step times the steps that stay under way
+    left = {"Li256ELi256ELi5E": 3 * 8, "Li128ELi128ELi5E": 3 * 4, "Li64ELi128ELi6E": 4 * 3}
+    for name, code in kernels.items():
+        want = next(n for shape, n in left.items() if shape in name)
+        mfmas = [i for i, ins in enumerate(code) if ins[1] == "v_mfma_f32_16x16x32_bf16"]
+        loop = code[mfmas[0]:mfmas[-1]]
+        waits = {ins[2] for ins in loop if ins[1] == "s_waitcnt" and "vmcnt" in ins[2]}
+        assert waits == {"vmcnt(%d)" % want}, (name, waits)
+        assert not [ins for ins in loop if ins[1].startswith(("scratch_", "global_", "flat_", "buffer_store"))], name
