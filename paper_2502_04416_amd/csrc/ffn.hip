@@ -3,7 +3,7 @@
 //   backward   from G and U as they were stored: dH = dY Wd^T (never stored), with s = 1 / (1 + e^-G)
 //              dG = dH U s (1 + G (1 - s)), dU = dH G s, rounded; dX = dx_base + dG Wg^T + dU Wu^T;
 //              dWg = X^T dG, dWu = X^T dU, dWd = H^T dY
-// Two launches forward and four backward (and one for each product that splits K): both projections, the activation and the product in one,
+// Two launches forward and four backward (and one before each product whose operands are copied, one behind each that splits K): both projections, the activation and the product in one,
 // its gradient behind the product that makes dH, dX one product over twice the width, and the two gradients that share X
 // one launch.
 #include <algorithm>
@@ -26,11 +26,11 @@ int check_sizes(const char* what, int32_t dtype, int64_t tokens, int32_t d, int3
 }
 
 size_t forward_bytes(int dtype, int64_t t, int64_t d, int64_t f) {
-  return std::max(matmul_slab_bytes(PRODUCT_GATED, dtype, t, f, d), matmul_slab_bytes(PRODUCT_DOWN, dtype, t, d, f));
+  return std::max(matmul_workspace_bytes(PRODUCT_GATED, dtype, t, f, d), matmul_workspace_bytes(PRODUCT_DOWN, dtype, t, d, f));
 }
 size_t backward_bytes(int dtype, int64_t t, int64_t d, int64_t f) {
-  return std::max({matmul_slab_bytes(PRODUCT_DGATED, dtype, t, f, d), matmul_slab_bytes(PRODUCT_DX, dtype, t, d, f),
-                   matmul_slab_bytes(PRODUCT_DW, dtype, d, f, t), matmul_slab_bytes(PRODUCT_DW, dtype, f, d, t)});
+  return std::max({matmul_workspace_bytes(PRODUCT_DGATED, dtype, t, f, d), matmul_workspace_bytes(PRODUCT_DX, dtype, t, d, f),
+                   matmul_workspace_bytes(PRODUCT_DW, dtype, d, f, t), matmul_workspace_bytes(PRODUCT_DW, dtype, f, d, t)});
 }
 
 int check_workspace(const char* what, const void* ws, uint64_t have, size_t need) {
@@ -71,14 +71,12 @@ extern "C" int cmoe_ffn_forward(const cmoe_ffn_forward_args* args, void* hip_str
   p.a = a.x, p.lda = a.d, p.b = a.w_gate, p.b2 = a.w_up, p.ldb = a.d_ff;
   p.m = (int)a.tokens, p.n = a.d_ff, p.k = a.d;
   p.c = a.hidden, p.c2 = a.gate, p.c3 = a.up, p.ldc = a.d_ff;
-  p.slab = need ? static_cast<float*>(a.workspace) : nullptr;
-  if (hipError_t e = matmul(PRODUCT_GATED, a.dtype, p, need, s)) return launched(what, e);
+  if (hipError_t e = matmul(PRODUCT_GATED, a.dtype, p, a.workspace, need, s)) return launched(what, e);
   MatArgs q = {};
   q.a = a.hidden, q.lda = a.d_ff, q.b = a.w_down, q.ldb = a.d;
   q.m = (int)a.tokens, q.n = a.d, q.k = a.d_ff;
   q.c = a.y, q.e1 = a.base, q.ldc = a.d;
-  q.slab = p.slab;
-  return launched(what, matmul(PRODUCT_DOWN, a.dtype, q, need, s));
+  return launched(what, matmul(PRODUCT_DOWN, a.dtype, q, a.workspace, need, s));
 }
 
 extern "C" size_t cmoe_ffn_backward_workspace_bytes(int64_t tokens, int32_t d, int32_t d_ff, int32_t dtype) {
@@ -118,21 +116,18 @@ extern "C" int cmoe_ffn_backward(const cmoe_ffn_backward_args* args, void* hip_s
                               {{"dx", a.dx, td, es, true}}))
     return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  float* slab = need ? static_cast<float*>(a.workspace) : nullptr;
   if (a.tokens > 0) {
     MatArgs p = {};
     p.a = a.dy, p.lda = a.d, p.b = a.w_down, p.ldb = a.d;
     p.m = (int)a.tokens, p.n = a.d_ff, p.k = a.d;
     p.e1 = a.gate, p.e2 = a.up, p.c = a.dgate, p.c2 = a.dup, p.ldc = a.d_ff;
-    p.slab = slab;
-    if (hipError_t e = matmul(PRODUCT_DGATED, a.dtype, p, need, s)) return launched(what, e);
+    if (hipError_t e = matmul(PRODUCT_DGATED, a.dtype, p, a.workspace, need, s)) return launched(what, e);
     if (a.dx) {
       MatArgs q = {};
       q.a = a.dgate, q.a2 = a.dup, q.lda = a.d_ff, q.b = a.w_gate, q.b2 = a.w_up, q.ldb = a.d_ff;
       q.m = (int)a.tokens, q.n = a.d, q.k = a.d_ff;
       q.c = a.dx, q.e1 = a.dx_base, q.ldc = a.d;
-      q.slab = slab;
-      if (hipError_t e = matmul(PRODUCT_DX, a.dtype, q, need, s)) return launched(what, e);
+      if (hipError_t e = matmul(PRODUCT_DX, a.dtype, q, a.workspace, need, s)) return launched(what, e);
     }
   }
   auto weights = [&](const void* left, int m, const void* right, const void* right2, int n, void* c, void* c2) {
@@ -140,8 +135,7 @@ extern "C" int cmoe_ffn_backward(const cmoe_ffn_backward_args* args, void* hip_s
     q.a = left, q.lda = m, q.b = right, q.b2 = right2, q.ldb = n;
     q.m = m, q.n = n, q.k = (int)a.tokens;
     q.c = c, q.c2 = c2, q.ldc = n, q.alpha = 1.0f;
-    q.slab = slab;
-    return matmul(PRODUCT_DW, a.dtype, q, need, s);
+    return matmul(PRODUCT_DW, a.dtype, q, a.workspace, need, s);
   };
   if (a.dw_gate && a.dw_up) {
     if (hipError_t e = weights(a.x, a.d, a.dgate, a.dup, a.d_ff, a.dw_gate, a.dw_up)) return launched(what, e);

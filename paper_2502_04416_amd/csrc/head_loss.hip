@@ -1,9 +1,9 @@
 // Softmax cross entropy of a head over a vocabulary, without its logits in memory.
-//   forward    z = X W^T piece by piece in registers: every tile leaves the largest logit m of its columns of a row and the sum of
+//   forward    z = X W^T in registers: every tile leaves the largest logit m of its columns of a row and the sum of
 //              exp(z - m), and the target's logit; lse = log sum exp z over the ranges, loss = lse - z[target], 0 without a target
 //   backward   in pieces of the vocabulary: z once more, dZ = weight * (exp(z - lse) - [target]) of a piece in the type, then
 //              dX += dZ W (fp32 between the pieces) and dW = scale * dZ^T X, complete for the piece's rows
-// What a piece costs beside its products is dX's sums, read and written, so pieces are as wide as 128 MB of dZ (in bf16) allow:
+// What a piece costs beside its products is dX's sums, read and written, so pieces are as wide as 128 MB of dZ allow:
 // it is read twice soon after it is written, and this part's last cache holds 256 MB.
 // `scale` is applied to the sums in fp32, and not to dZ: what all tokens share would round the entries of all targets, which are all
 // close to -scale, to the same side.
@@ -18,7 +18,7 @@ namespace cmoe {
 namespace {
 
 constexpr int64_t MOST = 1 << 20;
-constexpr int64_t PIECE_ELEMS = 64 << 20;
+constexpr int64_t PIECE_BYTES = 128 << 20;
 constexpr int64_t PIECE_LEAST = 1024;
 
 int check_sizes(const char* what, int32_t dtype, int64_t tokens, int32_t d, int32_t vocab) {
@@ -30,29 +30,44 @@ int check_sizes(const char* what, int32_t dtype, int64_t tokens, int32_t d, int3
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
+// How many vocabulary entries a piece may have for the copies of their rows, where operands may be copied, to stay below 256 MB (up to a width of
+// 8192); all of them otherwise.
+int64_t copied_piece(Product kind, int dtype, int64_t t, int64_t d, int64_t vocab) {
+  if (!matmul_copies(kind, dtype, t, vocab, d)) return vocab;
+  return std::min(vocab, std::max<int64_t>(4096, ((int64_t)1 << (dtype == CMOE_F32 ? 25 : 27)) / d / 256 * 256));
+}
+
 struct ForwardSpace {
-  size_t part, picked, total;              // offsets of the ranges and of the targets' logits
+  int64_t piece, last;                     // entries of a piece, and of the last one
+  size_t picked, product, total;           // offsets of the targets' logits and of the products' workspace; the ranges at 0
   ForwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
-    part = 0;
-    picked = round16((size_t)lse_ranges(dtype, t, vocab, d) * t * sizeof(float2));
-    total = picked + round16((size_t)t * 4);
+    piece = copied_piece(PRODUCT_LSE, dtype, t, d, vocab);
+    const int64_t pieces = (vocab - 1) / piece;              // but the last
+    last = vocab - pieces * piece;
+    const int64_t ranges = pieces * lse_ranges(dtype, t, piece, d) + lse_ranges(dtype, t, last, d);
+    picked = round16((size_t)ranges * t * sizeof(float2));
+    product = picked + round16((size_t)t * 4);
+    total = product + std::max(matmul_workspace_bytes(PRODUCT_LSE, dtype, t, piece, d), matmul_workspace_bytes(PRODUCT_LSE, dtype, t, last, d));
   }
 };
 
 struct BackwardSpace {
   int64_t piece, ld;                       // vocabulary entries of a piece, elements of a row of dZ
-  size_t acc, slab, total, slab_bytes;     // dZ at 0
+  size_t acc, product, total;              // offsets of dX's sums and of the products' workspace; dZ at 0
   BackwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
-    piece = std::max(PIECE_LEAST, PIECE_ELEMS / std::max<int64_t>(t, 1) / 256 * 256);
-    piece = std::min(piece, vocab);
+    piece = std::max(PIECE_LEAST, PIECE_BYTES / (int64_t)elem_size(dtype) / std::max<int64_t>(t, 1) / 256 * 256);
+    piece = std::min(piece, copied_piece(PRODUCT_DLOGITS, dtype, t, d, vocab));
     ld = (piece + 7) / 8 * 8;
     acc = round16((size_t)t * ld * elem_size(dtype));
-    slab = acc + (piece < vocab ? (size_t)round16((size_t)t * d * 4) : 0);
-    slab_bytes = 0;
+    product = acc + (piece < vocab ? round16((size_t)t * d * 4) : 0);
+    size_t most = 0;
     const int64_t last = vocab - (vocab - 1) / piece * piece;
-    for (int64_t w : {piece, last})
-      slab_bytes = std::max({slab_bytes, matmul_slab_bytes(PRODUCT_DHEAD, dtype, t, d, (w + 7) / 8 * 8), matmul_slab_bytes(PRODUCT_DW, dtype, w, d, t)});
-    total = slab + slab_bytes;
+    for (int64_t w : {piece, last}) {
+      const int64_t padded = (w + 7) / 8 * 8;
+      most = std::max({most, matmul_workspace_bytes(PRODUCT_DLOGITS, dtype, t, padded, d), matmul_workspace_bytes(PRODUCT_DHEAD, dtype, t, d, padded),
+                       matmul_workspace_bytes(PRODUCT_DW, dtype, w, d, t)});
+    }
+    total = product + most;
   }
 };
 
@@ -115,16 +130,22 @@ extern "C" int cmoe_head_loss_forward(const cmoe_head_loss_forward_args* args, v
     return rc;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   char* base = static_cast<char*>(a.workspace);
-  MatArgs p = {};
-  p.a = a.x, p.lda = a.d, p.b = a.weight, p.ldb = a.d;
-  p.m = (int)a.tokens, p.n = a.vocab, p.k = a.d;
-  p.ids = a.ids, p.vocab = a.vocab;
-  p.part = reinterpret_cast<float2*>(base + ws.part), p.picked = reinterpret_cast<float*>(base + ws.picked);
+  float2* part = static_cast<float2*>(a.workspace);
+  float* picked = reinterpret_cast<float*>(base + ws.picked);
   int ranges = 0;
-  if (hipError_t e = matmul(PRODUCT_LSE, a.dtype, p, 0, s, &ranges)) return launched(what, e);
+  for (int64_t first = 0; first < a.vocab; first += ws.piece) {
+    MatArgs p = {};
+    p.a = a.x, p.lda = a.d, p.b = static_cast<const char*>(a.weight) + (size_t)first * a.d * es, p.ldb = a.d;
+    p.m = (int)a.tokens, p.n = (int)std::min(ws.piece, a.vocab - first), p.k = a.d;
+    p.ids = a.ids, p.vocab = a.vocab, p.col0 = (int)first;
+    p.part = part + (size_t)ranges * a.tokens, p.picked = picked;
+    int more = 0;
+    if (hipError_t e = matmul(PRODUCT_LSE, a.dtype, p, base + ws.product, ws.total - ws.product, s, &more)) return launched(what, e);
+    ranges += more;
+  }
   // few rows: all threads to a row; many: neighbouring threads read neighbouring rows
   auto finish = [&](auto kernel, int rows_of) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.tokens + rows_of - 1) / rows_of)), dim3(256), 0, s, p.part, ranges, p.picked, a.ids, a.vocab, a.tokens, a.loss, a.lse);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((a.tokens + rows_of - 1) / rows_of)), dim3(256), 0, s, part, ranges, picked, a.ids, a.vocab, a.tokens, a.loss, a.lse);
   };
   if (a.tokens <= 512) finish(head_finish<1>, 1);
   else if (a.tokens <= 2048) finish(head_finish<8>, 8);
@@ -152,7 +173,7 @@ extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args,
     if (!a.dweight) return CMOE_OK;
     if (int rc = check_operands(what, {}, {{"dweight", a.dweight, (uint64_t)a.vocab * a.d * es, es}})) return rc;
     w.m = a.vocab, w.lda = a.vocab, w.c = a.dweight;
-    return launched(what, matmul(PRODUCT_DW, a.dtype, w, 0, s));
+    return launched(what, matmul(PRODUCT_DW, a.dtype, w, nullptr, 0, s));
   }
   if (!a.x || !a.weight || !a.ids || !a.lse) return fail(CMOE_EINVAL, "%s: x, weight, ids or lse is null", what);
   const BackwardSpace ws(a.dtype, a.tokens, a.d, a.vocab);
@@ -162,7 +183,8 @@ extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args,
                               {{"dx", a.dx, td, es}, {"dweight", a.dweight, vd, es}, {"the workspace", a.workspace, ws.total, 16}}))
     return rc;
   char* base = static_cast<char*>(a.workspace);
-  float* slab = ws.slab_bytes ? reinterpret_cast<float*>(base + ws.slab) : nullptr;
+  void* const room = base + ws.product;
+  const size_t room_bytes = ws.total - ws.product;
   for (int64_t first = 0; first < a.vocab; first += ws.piece) {
     const int n = (int)std::min<int64_t>(ws.piece, a.vocab - first), padded = (n + 7) / 8 * 8;
     const char* rows_of_w = static_cast<const char*>(a.weight) + (size_t)first * a.d * es;
@@ -171,19 +193,19 @@ extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args,
     p.m = (int)a.tokens, p.n = padded, p.n_b = n, p.k = a.d;
     p.c = base, p.ldc = ws.ld;
     p.ids = a.ids, p.vocab = a.vocab, p.col0 = (int)first, p.lse = a.lse, p.dloss = a.dloss;
-    if (hipError_t e = matmul(PRODUCT_DLOGITS, a.dtype, p, 0, s)) return launched(what, e);
+    if (hipError_t e = matmul(PRODUCT_DLOGITS, a.dtype, p, room, room_bytes, s)) return launched(what, e);
     if (a.dx) {
       MatArgs q = {};
       q.a = base, q.lda = ws.ld, q.b = rows_of_w, q.ldb = a.d;
       q.m = (int)a.tokens, q.n = a.d, q.k = padded, q.k_b = n;
       q.acc = reinterpret_cast<float*>(base + ws.acc), q.first = first == 0, q.last = first + n == a.vocab;
-      q.c = a.dx, q.ldc = a.d, q.alpha = a.scale, q.slab = slab;
-      if (hipError_t e = matmul(PRODUCT_DHEAD, a.dtype, q, ws.slab_bytes, s)) return launched(what, e);
+      q.c = a.dx, q.ldc = a.d, q.alpha = a.scale;
+      if (hipError_t e = matmul(PRODUCT_DHEAD, a.dtype, q, room, room_bytes, s)) return launched(what, e);
     }
     if (a.dweight) {
       w.a = base, w.lda = ws.ld, w.m = n, w.m_a = padded;
-      w.c = static_cast<char*>(a.dweight) + (size_t)first * a.d * es, w.slab = slab;
-      if (hipError_t e = matmul(PRODUCT_DW, a.dtype, w, ws.slab_bytes, s)) return launched(what, e);
+      w.c = static_cast<char*>(a.dweight) + (size_t)first * a.d * es;
+      if (hipError_t e = matmul(PRODUCT_DW, a.dtype, w, room, room_bytes, s)) return launched(what, e);
     }
   }
   return CMOE_OK;

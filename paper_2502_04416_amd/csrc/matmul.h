@@ -26,6 +26,7 @@ struct MatArgs {
   // what of an operand may be read where that is more or less than its part in the result: rows or columns of A (m_a >= m: padding, in
   // any state), of B (n_b <= n: zeros behind it), and B's K (k_b <= k: zeros behind it; A has zeros there itself)
   int m_a, n_b, k_b;
+  int64_t a_plane, b_plane;  // elements from one plane of a copied fp32 operand to the next
   void *c, *c2, *c3;
   const void *e1, *e2;
   int64_t ldc;               // of c, c2, c3, e1 and e2
@@ -45,12 +46,14 @@ struct MatArgs {
   float* slab;
 };
 
-// Bytes of slabs that a product may ask for, whatever its operands' alignment.
-size_t matmul_slab_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k);
+// Bytes of workspace, for copies of operands and slabs of a K split, that a product may ask for, whatever its operands' alignment.
+size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k);
+// Whether the product of operands that the ring cannot read where they are copies them.
+bool matmul_copies(Product kind, int dtype, int64_t m, int64_t n, int64_t k);
 // Column ranges that PRODUCT_LSE may write: rows of `part`, whatever its operands' alignment.
 int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k);
-// Enqueues the product; m_a, n_b and k_b count as m, n and k where they are 0.  slab_bytes: what may be used at p.slab.  *ranges, of
-// PRODUCT_LSE: how many ranges have been written.
-hipError_t matmul(Product kind, int dtype, MatArgs p, size_t slab_bytes, hipStream_t s, int* ranges = nullptr);
+// Enqueues the product; m_a, n_b and k_b count as m, n and k where they are 0.  Workspace: 16-byte aligned.  *ranges, of PRODUCT_LSE: how many
+// ranges have been written.
+hipError_t matmul(Product kind, int dtype, MatArgs p, void* workspace, size_t workspace_bytes, hipStream_t s, int* ranges = nullptr);
 
 }  // namespace cmoe

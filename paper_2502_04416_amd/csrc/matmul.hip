@@ -1,4 +1,4 @@
-// Which kernel, tile and K split a product of matmul.h runs on.
+// Which kernel, tile and K split a product of matmul.h runs on, and whether its operands are copied for it.
 #include "matmul.h"
 
 #include <algorithm>
@@ -12,11 +12,6 @@ namespace {
 
 constexpr int CUS = 256;
 
-struct Choice {
-  Tile tile;
-  int k_split;
-};
-
 struct Shape {
   bool a_columns, b_columns, dual, segments, splits;
 };
@@ -25,74 +20,142 @@ constexpr Shape shape_of(Product kind) {
           kind == PRODUCT_DX, kind != PRODUCT_LSE && kind != PRODUCT_DLOGITS};
 }
 
-// Relative time of a K step of 32 of a tile when the chip is full, and workgroups per CU.
-constexpr double kStep[TILES] = {1.0, 0.60, 0.42, 2.6, 1.0};
-constexpr int kPerCu[TILES] = {1, 2, 2, 2, 2};
-constexpr double kTileCost = 16;             // prologue and epilogue, in steps of the large tile
+struct Choice {
+  Tile tile;
+  int k_split;
+  bool copies;
+};
 
-Choice choose(Product kind, int dtype, bool ring, int64_t m, int64_t n, int64_t k, int pair, size_t slab_bytes) {
+// Times in us, of a K step of 32 of a tile when the chip is full, of a tile's beginning and end, and workgroups per CU.
+constexpr double kStep[TILES] = {0.68, 0.41, 0.29, 1.8, 0.70, 0.70};
+constexpr double kStepFp32[TILES] = {0.68, 0.41, 0.29, 5.0, 2.6, 2.6};
+constexpr int kPerCu[TILES] = {1, 2, 2, 2, 4, 2};
+constexpr double kTile = 11, kLaunch = 4, kBytesPerUs = 4.5e6;
+
+int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
+
+// Bytes of the copies, and of what is read and written for them.
+size_t copy_bytes(const Shape& sh, int planes, int64_t m, int64_t n, int64_t k, bool second) {
+  const int64_t a = (sh.a_columns ? k * round8(m) : m * round8(k)) * (sh.segments ? 2 : 1);
+  const int64_t b = (sh.b_columns ? k * round8(n) : n * round8(k)) * (second ? 2 : 1);
+  return ((size_t)(a + b) * planes * 2 + 255) / 256 * 256;
+}
+
+// direct: bf16 operands that the ring can read where they are.  second: there is a second B.
+Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace) {
   const Shape sh = shape_of(kind);
-  const int64_t steps = ((k + 31) / 32) * (sh.segments ? 2 : 1);
+  const int pair = kind == PRODUCT_DW && second ? 2 : 1, planes = dtype == CMOE_F32 ? 3 : 1;
+  const int64_t steps1 = ((k + 31) / 32) * (sh.segments ? 2 : 1);
   const int64_t cols = sh.dual ? 2 * n : n;
-  Choice best{ANY_128, 1};
-  double best_cost = 1e300;
   const int forced_tile = tuning().mat_tile, forced_split = tuning().mat_split;
-  const int first = ring ? RING_256 : ANY_128, last = ring ? RING_64 : ANY_32;
-  for (int t = first; t <= last; ++t) {
+  const size_t copies = direct ? 0 : copy_bytes(sh, planes, m, n, k, second);
+  const double copy_time = direct ? 0 : kLaunch + (double)copies * (planes == 3 ? 10.0 / 6 : 2) / kBytesPerUs;
+  Choice best{ANY_64, 1, false};
+  double best_cost = 1e300;
+  for (int t = RING_256; t <= (direct ? RING_64 : ANY_32); ++t) {
+    const bool ring = t <= RING_64;
     if (sh.a_columns && t == RING_64) continue;
-    if (forced_tile >= first && forced_tile <= last && forced_tile != t && !(sh.a_columns && forced_tile == RING_64)) continue;
+    if (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && !(sh.a_columns && forced_tile == RING_64) && !(direct && forced_tile > RING_64)) continue;
+    const size_t room = ring ? copies : 0;
+    if (room > workspace) continue;
+    const int64_t steps = steps1 * (ring && planes == 3 ? PAIRS : 1);
     const int64_t tiles = (m + kTiles[t].bm - 1) / kTiles[t].bm * ((cols + kTiles[t].bn - 1) / kTiles[t].bn) * pair;
+    const double step = dtype == CMOE_F32 ? kStepFp32[t] : kStep[t];
     for (int split = 1; split <= 16; split *= 2) {
-      if (split > 1 && (!sh.splits || pair > 1 || (size_t)split * m * cols * 4 > slab_bytes)) break;
+      if (split > 1 && (!sh.splits || pair > 1 || room + (size_t)split * m * cols * 4 > workspace)) break;
       if (split > 1 && forced_split < 1 && steps / split < 8) break;
       if (forced_split >= 1 && split != forced_split && sh.splits && pair == 1) continue;
       const int64_t slots = (int64_t)CUS * kPerCu[t];
       const double rounds = (double)((tiles * split + slots - 1) / slots);
-      // a last round that does not fill the chip still takes a tile's time; with one workgroup on a CU of two it is somewhat shorter
-      const double fill = tiles * split <= CUS && kPerCu[t] == 2 ? 0.6 : 1.0;
-      double cost = rounds * fill * kStep[t] * ((double)(steps + split - 1) / split + kTileCost);
-      if (split > 1) cost += 8 + (double)split * m * cols * 8 / 4e12 / 0.68e-6;   // the slabs written and read, a launch
-      if (cost < best_cost) best_cost = cost, best = {(Tile)t, split};
+      // a last round that does not fill the chip still takes a tile's time; with one workgroup on a CU of several it is shorter
+      const double fill = tiles * split <= CUS && kPerCu[t] > 1 ? 0.6 : 1.0;
+      double cost = kLaunch + rounds * fill * step * ((double)(steps + split - 1) / split + kTile / 0.68);
+      if (ring) cost += copy_time;
+      if (split > 1) cost += kLaunch + (double)split * m * cols * 8 / kBytesPerUs;
+      if (cost < best_cost) best_cost = cost, best = {(Tile)t, split, ring && !direct};
     }
   }
-  (void)dtype;
   return best;
 }
 
 int64_t ranges_of(const Choice& c, int64_t n) { return (n + kTiles[c.tile].bn - 1) / kTiles[c.tile].bn * kTiles[c.tile].wgn; }
 
+constexpr size_t EVERYTHING = (size_t)1 << 60;
+
+bool has_second(Product kind) { return kind == PRODUCT_GATED || kind == PRODUCT_DX; }
+
+template <typename T>
+hipError_t prepare(const CopyArgs& args, uint32_t groups, hipStream_t s) {
+  hipLaunchKernelGGL(matmul_prepare<T>, dim3(groups), dim3(256), 0, s, args);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k) {
   int64_t most = 0;
-  for (int ring = 0; ring <= (dtype == CMOE_BF16); ++ring) most = std::max(most, ranges_of(choose(PRODUCT_LSE, dtype, ring, m, n, k, 1, 0), n));
+  for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct) most = std::max(most, ranges_of(choose(PRODUCT_LSE, dtype, direct, false, m, n, k, EVERYTHING), n));
   return most;
 }
 
-size_t matmul_slab_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k) {
-  if (!shape_of(kind).splits || m == 0 || n == 0) return 0;
-  const size_t all = (size_t)1 << 40;
-  const size_t one = (size_t)m * n * 4 * (shape_of(kind).dual ? 2 : 1);
+bool matmul_copies(Product kind, int dtype, int64_t m, int64_t n, int64_t k) {
+  return choose(kind, dtype, false, has_second(kind), m, n, k, EVERYTHING).copies;
+}
+
+size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k) {
+  if (m <= 0 || n <= 0) return 0;
+  const Shape sh = shape_of(kind);
   size_t most = 0;
-  for (int ring = 0; ring <= (dtype == CMOE_BF16); ++ring)
-    for (int pair = 1; pair <= (kind == PRODUCT_DW ? 2 : 1); ++pair) {
-      const Choice c = choose(kind, dtype, ring, m, n, k, pair, all);
-      if (c.k_split > 1) most = std::max(most, c.k_split * one);
+  for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct)
+    for (int second = has_second(kind); second <= (has_second(kind) || kind == PRODUCT_DW); ++second) {
+      const Choice c = choose(kind, dtype, direct, second, m, n, k, EVERYTHING);
+      most = std::max(most, (c.copies ? copy_bytes(sh, dtype == CMOE_F32 ? 3 : 1, m, n, k, second) : 0) + (c.k_split > 1 ? (size_t)c.k_split * m * n * 4 * (sh.dual ? 2 : 1) : 0));
     }
-  return most;
+  return (most + 15) / 16 * 16;
 }
 
-hipError_t matmul(Product kind, int dtype, MatArgs p, size_t slab_bytes, hipStream_t s, int* ranges) {
+hipError_t matmul(Product kind, int dtype, MatArgs p, void* workspace, size_t workspace_bytes, hipStream_t s, int* ranges) {
   if (p.m <= 0 || p.n <= 0) return hipSuccess;
   if (!p.m_a) p.m_a = p.m;
   if (!p.n_b) p.n_b = p.n;
   if (!p.k_b) p.k_b = p.k;
   const Shape sh = shape_of(kind);
+  const bool second = has_second(kind) || (kind == PRODUCT_DW && p.c2);
   auto wide = [](const void* q) { return ((uintptr_t)q & 15) == 0; };
-  const bool ring = dtype == CMOE_BF16 && wide(p.a) && wide(p.a2) && wide(p.b) && wide(p.b2) && p.lda % 8 == 0 && p.ldb % 8 == 0 &&
-                    (sh.a_columns ? p.m_a : p.k) % 8 == 0 && (sh.b_columns ? p.n_b : p.k) % 8 == 0;
-  const Choice c = choose(kind, dtype, ring, p.m, p.n, p.k, kind == PRODUCT_DW && p.c2 ? 2 : 1, p.slab ? slab_bytes : 0);
+  const bool direct = dtype == CMOE_BF16 && wide(p.a) && wide(p.a2) && wide(p.b) && wide(p.b2) && p.lda % 8 == 0 && p.ldb % 8 == 0 &&
+                      (sh.a_columns ? p.m_a : p.k) % 8 == 0 && (sh.b_columns ? p.n_b : p.k) % 8 == 0;
+  const Choice c = choose(kind, dtype, direct, second, p.m, p.n, p.k, workspace ? workspace_bytes : 0);
   p.k_split = c.k_split;
+  char* room = static_cast<char*>(workspace);
+  if (c.copies) {
+    const int planes = dtype == CMOE_F32 ? 3 : 1;
+    CopyArgs args = {};
+    uint32_t groups = 0;
+    auto copy = [&](const void* from, int64_t ld, int64_t rows, int cols) {
+      Copied& op = args.op[args.n++];
+      op.from = from, op.to = reinterpret_cast<bf16_t*>(room), op.ld = ld, op.rows = rows, op.cols = cols, op.pitch = (int)round8(cols), op.first = groups;
+      groups += (uint32_t)((rows * (op.pitch / 8) + 255) / 256);
+      room += (size_t)rows * op.pitch * planes * 2;
+      return op.to;
+    };
+    const int64_t a_rows = sh.a_columns ? p.k : p.m, b_rows = sh.b_columns ? p.k_b : p.n_b;
+    const int a_cols = sh.a_columns ? p.m : p.k, b_cols = sh.b_columns ? p.n_b : p.k_b;
+    p.a = copy(p.a, p.lda, a_rows, a_cols);
+    if (sh.segments) p.a2 = copy(p.a2, p.lda, a_rows, a_cols);
+    p.b = copy(p.b, p.ldb, b_rows, b_cols);
+    if (second) p.b2 = copy(p.b2, p.ldb, b_rows, b_cols);
+    p.lda = round8(a_cols), p.ldb = round8(b_cols);
+    p.a_plane = a_rows * p.lda, p.b_plane = b_rows * p.ldb;
+    // the zeros behind the columns are read
+    if (sh.a_columns) p.m_a = (int)p.lda;
+    else p.k = (int)p.lda;
+    if (sh.b_columns) p.n_b = (int)p.ldb;
+    else p.k_b = (int)p.ldb;
+    if (groups)
+      if (hipError_t e = dtype == CMOE_F32 ? prepare<float>(args, groups, s) : prepare<bf16_t>(args, groups, s)) return e;
+    room = static_cast<char*>(workspace) + (room - static_cast<char*>(workspace) + 255) / 256 * 256;
+  }
+  if (c.k_split > 1) p.slab = reinterpret_cast<float*>(room);
   if (ranges) *ranges = (int)ranges_of(c, p.n);
   switch (kind) {
     case PRODUCT_GATED: return launch_gated(c.tile, dtype, p, s);

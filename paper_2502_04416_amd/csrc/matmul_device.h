@@ -12,7 +12,13 @@
 // with (row >> 2) & 3; 32-byte chunks of a panel's row k with bits 1 and 3 of k (bit 0 chooses the half of the 256-byte bank line,
 // bit 2 is the other read).
 //
-// matmul_any: both types, any alignment and size, operands through registers with every chunk's end checked.
+// fp32 on the ring: an operand is copied into three planes of bf16 that hold the first, the second and the last eight of its 24 bits
+// (matmul_prepare; cut, not rounded, so that their sum is the value), and the six products of planes above 2^-24 are summed as parts of K, the
+// smallest first: the sums and their errors are those of fp32 products.  Infinities become NaN.  One such product runs at a sixth
+// of the bf16 rate, 200 TFLOP/s, where the fp32 matrix instructions have 157 at most.  bf16 operands at odd addresses or of
+// odd widths are copied into one plane.
+//
+// matmul_any: both types, any alignment and size, operands through registers with every chunk's end checked: what is too small to be worth copying.
 #pragma once
 #include <type_traits>
 
@@ -275,6 +281,56 @@ __device__ __forceinline__ bool find_tile(const MatArgs& p, int n_mt, int n_nt, 
 }
 inline __host__ int grid_of(int64_t tiles, int k_split) { return (int)((tiles * k_split + 7) / 8 * 8); }
 
+// ---- operands copied for the ring ---------------------------------------------------------------------------------------
+
+struct Copied {
+  const void* from;          // [rows, cols], rows `ld` apart
+  bf16_t* to;                // [planes][rows][pitch], zeros behind the columns
+  int64_t ld, rows;
+  int cols, pitch;
+  uint32_t first, unused;    // its first workgroup
+};
+struct CopyArgs {
+  Copied op[4];
+  int n;
+};
+
+// A thread per eight columns.  Bound by memory.
+template <typename T>
+__global__ __launch_bounds__(256) void matmul_prepare(CopyArgs args) {
+  int which = 0;
+  for (int i = 1; i < args.n; ++i)
+    if (args.op[i].first <= blockIdx.x) which = i;
+  const Copied& op = args.op[which];
+  const uint32_t per_row = (uint32_t)op.pitch >> 3;
+  const uint64_t chunk = (uint64_t)(blockIdx.x - op.first) * 256;
+  const uint64_t row0 = chunk / per_row;
+  const uint32_t c0 = (uint32_t)(chunk - row0 * per_row) + threadIdx.x;
+  const int64_t row = row0 + c0 / per_row;
+  if (row >= op.rows) return;
+  const int col = (int)(c0 % per_row) * 8, n = op.cols - col;
+  float v[8] = {};
+  if (n > 0) load8(static_cast<const T*>(op.from) + row * op.ld + col, n, v);
+  bf16_t* to = op.to + row * op.pitch + col;
+  if constexpr (sizeof(T) == 2) {
+    store8(to, 8, v);
+  } else {
+    float top[8], mid[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      top[e] = __uint_as_float(__float_as_uint(v[e]) & 0xffff0000u);
+      // (an infinity or NaN is passed on as NaN: its rest is NaN)
+      const float rest = v[e] - top[e];
+      mid[e] = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+      v[e] = rest - mid[e];
+    }
+    const int64_t plane = op.rows * op.pitch;
+    store8(to, 8, top);
+    store8(to + plane, 8, mid);
+    store8(to + 2 * plane, 8, v);
+  }
+}
+
 // ---- the ring -------------------------------------------------------------------------------------------------------
 
 typedef short shortx4_t __attribute__((ext_vector_type(4)));
@@ -290,12 +346,23 @@ __device__ __forceinline__ shortx4_t read_turned(const bf16_t* __restrict__ at) 
 #endif
 }
 
+// Eight K of a column: two reads, the second `further` elements on.
+__device__ __forceinline__ bf16x8_t read_turned2(const bf16_t* at, int further) {
+  union { shortx4_t h[2]; bf16x8_t v; } u;
+  u.h[0] = read_turned(at);
+  u.h[1] = read_turned(at + further);
+  return u.v;
+}
+
 constexpr int mat_ring_elems(int bm, int bn, int stages) { return stages * (bm + bn) * BK; }
 template <int BM, int BN, int STAGES, int WGM, int WGN>
 constexpr size_t mat_ring_bytes() {
   const int strips = WGM * WGN * strip_floats<BM / WGM / 16, BN / WGN / 16>() * 4, ring = mat_ring_elems(BM, BN, STAGES) * 2;
   return ring > strips ? ring : strips;
 }
+
+// The pairs of planes of two fp32 operands whose products count, smallest first: plane of A and of B, two bits each.
+constexpr int PAIRS = 6, PAIRS_A = 0 | 1 << 2 | 2 << 4 | 0 << 6 | 1 << 8 | 0 << 10, PAIRS_B = 2 | 1 << 2 | 0 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
 
 template <int BM, int BN, int STAGES, int WGM, int WGN, bool ACOL, bool BCOL, class EPI>
 __global__ __launch_bounds__(WGM* WGN * 64)
@@ -304,6 +371,8 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   constexpr int TM = BM / WGM, TN = BN / WGN, MB = TM / 16, NB = TN / 16;
   constexpr int A_CH = BM / 16 / NW, B_CH = BN / 16 / NW, LPT = A_CH + B_CH;   // load instructions per wave and step
   constexpr int A_ELEMS = BM * BK, STAGE_ELEMS = (BM + BN) * BK;
+  constexpr bool PLANES = sizeof(typename EPI::type) == 4;
+  constexpr int SEGS = (PLANES ? PAIRS : 1) * (EPI::SEGMENTS ? 2 : 1);         // parts of K one after the other
   static_assert(NW == 4 && BM % 64 == 0 && BN % 64 == 0, "a wave loads whole blocks and panels");
   static_assert((!ACOL || TM % 64 == 0) && (!BCOL || EPI::DUAL || TN % 64 == 0), "panels belong to one wave column");
   static_assert(!EPI::DUAL || (BCOL && BN % 128 == 0 && (TN / 2) % 32 == 0), "gate and up panels alternate");
@@ -320,17 +389,15 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   if (!find_tile(p, (p.m + BM - 1) / BM, (p.n + BNO - 1) / BNO, &at)) return;
   const int z = blockIdx.y;
   const int row_first = at.mt * BM, col_first = at.nt * BNO;
-  // steps of K: of one part (SEGMENTS: the second part's follow), and this workgroup's
-  const int seg_steps = (p.k + BK - 1) / BK;
-  const int all = EPI::SEGMENTS ? 2 * seg_steps : seg_steps;
+  const int seg_steps = (p.k + BK - 1) / BK;                 // steps of a part of K
+  const int all = SEGS * seg_steps;
   const int per = (all + p.k_split - 1) / p.k_split;
   const int k_begin = min(at.part * per, all), KT = min(per, all - k_begin);
 
   // Lanes' offsets in bytes from the operand's place of a step; DMA_NONE: zeros.  By rows: load i of a wave is block wave + 4 i,
   // lane l its row l / 4 and chunk (l % 4) ^ (row >> 2) & 3.  By columns: load i is a quarter of panel i, lane l row l / 8 of
   // it and the 16-byte chunk that the swizzle puts at l % 8.
-  auto row_chunk = [&]() { return ((lane & 3) ^ ((lane >> 4) & 3)) << 3; };
-  const int coff = row_chunk();
+  const int coff = ((lane & 3) ^ ((lane >> 4) & 3)) << 3;
   const int pk = wave * 8 + (lane >> 3);                     // row of a panel
   const int pcol = ((((lane & 7) >> 1) ^ (((pk >> 1) & 1) | (((pk >> 3) & 1) << 1))) << 4) + ((lane & 1) << 3);
   uint32_t a_off[A_CH], b_off[B_CH];
@@ -346,38 +413,52 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
     else b_off[i] = col_first + (wave + i * NW) * 16 + (lane >> 2) < p.n_b ? (uint32_t)((((wave + i * NW) * 16 + (lane >> 2)) * p.ldb + coff) * 2) : DMA_NONE;
   }
   const bool k_past = (seg_steps - 1) * BK + coff >= p.k;    // of a part's last step, by rows
-  const bf16_t* const a1 = static_cast<const bf16_t*>(p.a) + (ACOL ? row_first : row_first * p.lda);
-  const bf16_t* const b1 = static_cast<const bf16_t*>(EPI::PAIRED && z ? p.b2 : p.b) + (BCOL ? col_first : col_first * p.ldb);
-  const bf16_t* const a2 = EPI::SEGMENTS ? static_cast<const bf16_t*>(p.a2) + row_first * p.lda : nullptr;
-  const bf16_t* const b2 = EPI::SEGMENTS ? static_cast<const bf16_t*>(p.b2) + col_first * p.ldb : EPI::DUAL ? static_cast<const bf16_t*>(p.b2) + col_first : nullptr;
 
-  // load i of step kt (counted from k_begin) of an operand; `left`: rows of it (by rows) or columns (by columns) from its place on
-  auto fetch = [&](auto col_tag, const bf16_t* base, const bf16_t* base2, int64_t ld, int left, int k, uint32_t off, int kt, bf16_t* dst) {
-    int s = kt + k_begin;
-    const bool there = kt < KT;
-    if (EPI::SEGMENTS && s >= seg_steps) {
-      s -= seg_steps;
-      base = base2;
-    }
-    if constexpr (decltype(col_tag)::value) {
-      // the 32 rows of a step are the buffer: K past its end lies past the buffer's
-      const int rows = there ? min(k - s * BK, BK) : 0;
-      const int64_t size = rows > 0 ? ((rows - 1) * ld + left) * 2 : 0;
-      dma16_buffer(uniform_ptr(base + (int64_t)s * BK * ld), __builtin_amdgcn_readfirstlane((uint32_t)min(size, (int64_t)DMA_NONE)), off, 0, dst);
+  // The step that is fetched next: part of K, step in it, and where its operands lie.
+  int f_left = KT, f_seg = SEGS > 1 && seg_steps > 0 ? k_begin / seg_steps : 0, f_step = k_begin - f_seg * seg_steps;
+  const bf16_t *f_a, *f_b, *f_b2 = nullptr;
+  auto place_of = [&]() {
+    const int part = EPI::SEGMENTS ? f_seg / (SEGS / 2) : 0, pair = f_seg - part * (EPI::SEGMENTS ? SEGS / 2 : 0);
+    const bf16_t* a = static_cast<const bf16_t*>(EPI::SEGMENTS && part ? p.a2 : p.a);
+    const bf16_t* b = static_cast<const bf16_t*>((EPI::SEGMENTS && part) || (EPI::PAIRED && z) ? p.b2 : p.b);
+    const int64_t at_a = (ACOL ? row_first + f_step * BK * p.lda : row_first * p.lda + f_step * BK) + (PLANES ? (PAIRS_A >> (2 * pair) & 3) * p.a_plane : 0);
+    const int64_t at_b = (BCOL ? col_first + f_step * BK * p.ldb : col_first * p.ldb + f_step * BK) + (PLANES ? (PAIRS_B >> (2 * pair) & 3) * p.b_plane : 0);
+    f_a = uniform_ptr(a + at_a);
+    f_b = uniform_ptr(b + at_b);
+    if (EPI::DUAL) f_b2 = uniform_ptr(static_cast<const bf16_t*>(p.b2) + at_b);
+  };
+  place_of();
+  auto advance = [&]() {
+    --f_left;
+    if (++f_step == seg_steps && SEGS > 1) {
+      f_step = 0;
+      f_seg = f_seg + 1 < SEGS ? f_seg + 1 : 0;              // (behind the last part nothing is read)
+      place_of();
     } else {
-      const int64_t size = there ? ((left - 1) * ld + k) * 2 : 0;
-      dma16_buffer(uniform_ptr(base), __builtin_amdgcn_readfirstlane((uint32_t)min(size, (int64_t)DMA_NONE)), s == seg_steps - 1 && k_past ? DMA_NONE : off,
-                   (uint32_t)s * (BK * 2), dst);
+      f_a += ACOL ? BK * p.lda : BK;
+      f_b += BCOL ? BK * p.ldb : BK;
+      if (EPI::DUAL) f_b2 += BK * p.ldb;
     }
   };
-  auto issue = [&](int kt, int slot, int i) {
+  // Lanes outside of an operand ask for nothing; the buffer's size is what the rows of a step by columns hold, so that K past its end is
+  // zeros, and nothing behind the last step.
+  auto fetch = [&](auto col_tag, const bf16_t* base, int64_t ld, int k, uint32_t off, bf16_t* dst) {
+    uint32_t size = DMA_NONE;
+    if constexpr (decltype(col_tag)::value) {
+      const int rows = min(k - f_step * BK, BK);
+      size = rows > 0 ? (uint32_t)(rows * ld * 2) : 0;
+    } else {
+      off = f_step == seg_steps - 1 && k_past ? DMA_NONE : off;
+    }
+    dma16_buffer(base, __builtin_amdgcn_readfirstlane(f_left > 0 ? size : 0), off, 0, dst);
+  };
+  auto issue = [&](int slot, int i) {                        // load i of the step fetched next
     bf16_t* st = smem + slot * STAGE_ELEMS;
     if (i < A_CH) {
-      fetch(std::bool_constant<ACOL>{}, a1, a2, p.lda, p.m_a - row_first, p.k, a_off[i], kt, st + (ACOL ? i * 2048 + wave * 512 : (wave + i * NW) * BLK));
+      fetch(std::bool_constant<ACOL>{}, f_a, p.lda, p.k, a_off[i], st + (ACOL ? i * 2048 + wave * 512 : (wave + i * NW) * BLK));
     } else {
       const int j = i - A_CH;
-      fetch(std::bool_constant<BCOL>{}, EPI::DUAL && (j & 1) ? b2 : b1, b2, p.ldb, p.n_b - col_first, p.k_b, b_off[j], kt,
-            st + A_ELEMS + (BCOL ? j * 2048 + wave * 512 : (wave + j * NW) * BLK));
+      fetch(std::bool_constant<BCOL>{}, EPI::DUAL && (j & 1) ? f_b2 : f_b, p.ldb, p.k_b, b_off[j], st + A_ELEMS + (BCOL ? j * 2048 + wave * 512 : (wave + j * NW) * BLK));
     }
   };
 
@@ -404,24 +485,18 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
       for (int i = 0; i < 4; ++i) acc[mb][nb][i] = 0.0f;
 
   bf16x8_t af[2][MB], wf[2][NB];
-  auto read2 = [&](const bf16_t* from) {
-    union { shortx4_t h[2]; bf16x8_t v; } u;
-    u.h[0] = read_turned(from);
-    u.h[1] = read_turned(from + 4 * 64);
-    return u.v;
-  };
   auto load_frag = [&](int slot, int f, int set) {           // B fragments first, then A
     const bf16_t* st = smem + slot * STAGE_ELEMS;
     if (f < NB) {
       if constexpr (!BCOL) wf[set][f] = *reinterpret_cast<const bf16x8_t*>(st + A_ELEMS + (wn * NB + f) * BLK + frag);
       else if constexpr (EPI::DUAL) {
         const int which = f / (NB / 2), c = f % (NB / 2);    // panel of the wave's column block, in gate / up pairs
-        wf[set][f] = read2(st + A_ELEMS + ((wn * (NB / 2)) / 4 * 2 + which) * 2048 + turned[c]);
-      } else wf[set][f] = read2(st + A_ELEMS + (wn * (NB / 4) + f / 4) * 2048 + turned[f % 4]);
+        wf[set][f] = read_turned2(st + A_ELEMS + ((wn * (NB / 2)) / 4 * 2 + which) * 2048 + turned[c], 4 * 64);
+      } else wf[set][f] = read_turned2(st + A_ELEMS + (wn * (NB / 4) + f / 4) * 2048 + turned[f % 4], 4 * 64);
     } else {
       const int q = f - NB;
       if constexpr (!ACOL) af[set][q] = *reinterpret_cast<const bf16x8_t*>(st + (wm * MB + q) * BLK + frag);
-      else af[set][q] = read2(st + (wm * (MB / 4) + q / 4) * 2048 + turned_a[q % 4]);
+      else af[set][q] = read_turned2(st + (wm * (MB / 4) + q / 4) * 2048 + turned_a[q % 4], 4 * 64);
     }
   };
   static_assert(!EPI::DUAL || NB / 2 <= 4, "a wave's gate columns lie in one panel");
@@ -429,9 +504,11 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   constexpr int NM = MB * NB, NF = MB + NB, ND = LPT;
   static_assert(ND <= NM, "at most one load instruction after an MFMA");
 #pragma unroll
-  for (int st = 0; st < STAGES; ++st)
+  for (int st = 0; st < STAGES; ++st) {
 #pragma unroll
-    for (int i = 0; i < ND; ++i) issue(st, st, i);
+    for (int i = 0; i < ND; ++i) issue(st, i);
+    advance();
+  }
   wait_vmcnt<(STAGES - 1) * ND>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -439,11 +516,11 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   for (int f = 0; f < NF; ++f) load_frag(0, f, 0);
 
   int slot = 0;
-  auto step = [&](int ks, auto set_tag, auto wait_tag) {
+  auto step = [&](auto set_tag, auto wait_tag) {
     constexpr int SET = decltype(set_tag)::value;
     constexpr bool WAIT = decltype(wait_tag)::value;
-    // this wave's loads of step ks + 1 have landed and its reads of step ks have returned: behind the barrier step ks + 1 may be
-    // read and the slot of step ks refilled (a bare barrier: __syncthreads() would drain every load)
+    // this wave's loads of the next step have landed and its reads of this one have returned: behind the barrier the next step may be
+    // read and this one's slot refilled (a bare barrier: __syncthreads() would drain every load)
     wait_vmcnt<(STAGES - 2) * ND>();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -461,17 +538,18 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
       for (int f = 0; f < NF; ++f)
         if (f * NM * 3 / (NF * 4) == m) load_frag(next, f, SET ^ 1);
       const int i = ((m + 1) * ND + NM - 1) / NM - 1;
-      if (i < ND && (i + 1) * NM / ND - 1 == m) issue(ks + STAGES, slot, i);
+      if (i < ND && (i + 1) * NM / ND - 1 == m) issue(slot, i);
     }
+    advance();
     __builtin_amdgcn_sched_barrier(0);
     slot = next;
   };
   int ks = 0;
   for (; ks + 1 < KT; ks += 2) {
-    step(ks, std::integral_constant<int, 0>{}, std::false_type{});
-    step(ks + 1, std::integral_constant<int, 1>{}, std::true_type{});
+    step(std::integral_constant<int, 0>{}, std::false_type{});
+    step(std::integral_constant<int, 1>{}, std::true_type{});
   }
-  if (ks < KT) step(ks, std::integral_constant<int, 0>{}, std::true_type{});
+  if (ks < KT) step(std::integral_constant<int, 0>{}, std::true_type{});
   __builtin_amdgcn_sched_barrier(0);
   wait_vmcnt<0>();                                           // (no load into LDS may outlive the workgroup)
   const int64_t row0 = row_first + wm * TM;
@@ -485,19 +563,25 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
 
 // ---- any size, alignment and type -----------------------------------------------------------------------------------
 
-// Operands go through registers into LDS in rows of 64 bytes of K, whichever way they lie in memory, padded by 16 bytes: the 16 rows of
-// a read then fall into different banks.  One K step is loaded while the one before it is multiplied.
-template <typename T> struct AnyStep;
-template <> struct AnyStep<float> { static constexpr int K = 16, E = 4, LD = 20; };
-template <> struct AnyStep<bf16_t> { static constexpr int K = 32, E = 8, LD = 40; };
+// Steps of 128 bytes of K, through registers: two steps are under way while a third is multiplied out of LDS, since a step is shorter than the
+// memory's latency.  An operand by rows lies in LDS in rows of 128 bytes padded by 16 (16 rows of a ds_read_b128 in different banks);
+// by columns as in memory, a row per K, and an MFMA's operand is taken down a column: in fp32 one value per K (rows padded so that four
+// K apart is a quarter of the banks apart), in bf16 turned by ds_read_b64_tr_b16 (four K at eight banks from one another).
+template <typename T>
+struct Any {
+  static constexpr int E = 16 / sizeof(T), K = 128 / sizeof(T), KC = 8;      // values of a chunk, K of a step, chunks of a row
+  static constexpr int ROW = K + E;                                          // pitch of an operand by rows
+  static constexpr int pitch(int cols) { return sizeof(T) == 4 ? cols + 4 : cols + 16; }
+  static constexpr int elems(bool columns, int size) { return columns ? K * pitch(size) : size * ROW; }
+};
 
 template <typename T>
 struct Chunk {
-  T v[AnyStep<T>::E];
+  T v[Any<T>::E];
 };
 template <typename T>
 __device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
-  constexpr int E = AnyStep<T>::E;
+  constexpr int E = Any<T>::E;
   if (n >= E) return __builtin_bit_cast(Chunk<T>, *reinterpret_cast<const Bytes16<T>*>(p));
   Chunk<T> c;
 #pragma unroll
@@ -505,19 +589,22 @@ __device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
   return c;
 }
 
-template <typename T, int BM, int BN, int WGM, int WGN>
+template <typename T, int BM, int BN, int WGM, int WGN, bool ACOL, bool BCOL>
 constexpr size_t mat_any_bytes() {
-  const size_t strips = (size_t)WGM * WGN * strip_floats<BM / WGM / 16, BN / WGN / 16>() * 4, tiles = 2 * (size_t)(BM + BN) * AnyStep<T>::LD * sizeof(T);
+  const size_t strips = (size_t)WGM * WGN * strip_floats<BM / WGM / 16, BN / WGN / 16>() * 4;
+  const size_t tiles = 2 * (size_t)(Any<T>::elems(ACOL, BM) + Any<T>::elems(BCOL, BN)) * sizeof(T);
   return strips > tiles ? strips : tiles;
 }
 
 template <int BM, int BN, int WGM, int WGN, bool ACOL, bool BCOL, class EPI>
 __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
   typedef typename EPI::type T;
-  constexpr int NT = WGM * WGN * 64, K = AnyStep<T>::K, E = AnyStep<T>::E, LD = AnyStep<T>::LD, KC = K / E;
+  typedef Any<T> S;
+  constexpr int NT = WGM * WGN * 64, K = S::K, E = S::E, KC = S::KC;
   constexpr int TM = BM / WGM, TN = BN / WGN, MB = TM / 16, NB = TN / 16;
-  constexpr int A_N = (BM * KC + NT - 1) / NT, B_N = (BN * KC + NT - 1) / NT;   // chunks per thread and step
-  static_assert(BM % 16 == 0 && BN % 64 == 0 && (BM * KC) % 64 == 0, "whole waves load");
+  constexpr int A_N = BM * KC / NT, B_N = BN * KC / NT;                      // chunks per thread and step
+  constexpr int A_ELEMS = S::elems(ACOL, BM), STAGE = A_ELEMS + S::elems(BCOL, BN);
+  static_assert(BM * KC % NT == 0 && BN * KC % NT == 0, "every thread loads");
   extern __shared__ __attribute__((aligned(16))) char any_smem[];
   T* const tiles = reinterpret_cast<T*>(any_smem);
 
@@ -533,59 +620,58 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
   const int per = (all + p.k_split - 1) / p.k_split;
   const int k_begin = min(at.part * per, all), k_end = min(k_begin + per, all);
 
-  Chunk<T> ra[A_N], rb[B_N];
-  auto fetch = [&](auto col_tag, int c, int rows, const T* base, int64_t ld, int first, int size, int k_size, int k0) {
+  Chunk<T> ra[2][A_N], rb[2][B_N];
+  // chunk c of a step: by columns K row c / (size / E) and E columns of it, by rows row c / KC and E of its K
+  auto fetch = [&](auto col_tag, int c, int size, const T* base, int64_t ld, int first, int there, int k_there, int k0) {
     Chunk<T> out = {};
-    if constexpr (decltype(col_tag)::value) {                // chunk c: K row c / (rows / E), E columns
-      const int kr = c / (rows / E), col = first + c % (rows / E) * E;
-      if (k0 + kr < k_size && col < size) out = load_chunk<T>(base + (int64_t)(k0 + kr) * ld + col, size - col);
+    if constexpr (decltype(col_tag)::value) {
+      const int k = k0 + c / (size / E), col = first + c % (size / E) * E;
+      if (k < k_there && col < there) out = load_chunk<T>(base + (int64_t)k * ld + col, there - col);
     } else {
       const int row = first + c / KC, k = k0 + c % KC * E;
-      if (row < size && k < k_size) out = load_chunk<T>(base + (int64_t)row * ld + k, k_size - k);
+      if (row < there && k < k_there) out = load_chunk<T>(base + (int64_t)row * ld + k, k_there - k);
     }
     return out;
   };
-  auto load = [&](int s) {
+  auto load = [&](int s, int set) {
+    if (s >= k_end) return;
     const bool second = EPI::SEGMENTS && s >= seg_steps;
     const int k0 = (second ? s - seg_steps : s) * K;
     const T* a = static_cast<const T*>(second ? p.a2 : p.a);
     const T* b = static_cast<const T*>(second || (EPI::PAIRED && z) ? p.b2 : p.b);
 #pragma unroll
-    for (int i = 0; i < A_N; ++i)
-      if (BM * KC >= NT || tid < BM * KC) ra[i] = fetch(std::bool_constant<ACOL>{}, tid + i * NT, BM, a, p.lda, row_first, p.m_a, p.k, k0);
+    for (int i = 0; i < A_N; ++i) ra[set][i] = fetch(std::bool_constant<ACOL>{}, tid + i * NT, BM, a, p.lda, row_first, p.m_a, p.k, k0);
 #pragma unroll
     for (int i = 0; i < B_N; ++i) {
       int c = tid + i * NT;
       const T* from = b;
-      // DUAL: the tile's first half from B, its second from B2, the same columns of both
+      // DUAL: the first half of the chunks from B, the second from B2, the same columns of both
       if (EPI::DUAL && c >= BN * KC / 2) {
         c -= BN * KC / 2;
         from = static_cast<const T*>(p.b2);
       }
-      rb[i] = fetch(std::bool_constant<BCOL>{}, c, EPI::DUAL ? BN / 2 : BN, from, p.ldb, col_first, p.n_b, p.k_b, k0);
+      rb[set][i] = fetch(std::bool_constant<BCOL>{}, c, BNO, from, p.ldb, col_first, p.n_b, p.k_b, k0);
     }
   };
-  auto place = [&](auto col_tag, const Chunk<T>& v, int c, int rows, T* to) {
-    if constexpr (decltype(col_tag)::value) {
-      const int kr = c / (rows / E), col = c % (rows / E) * E;
-#pragma unroll
-      for (int e = 0; e < E; ++e) to[(col + e) * LD + kr] = v.v[e];
-    } else {
-      *reinterpret_cast<Chunk<T>*>(__builtin_assume_aligned(to + (c / KC) * LD + c % KC * E, 16)) = v;
-    }
+  auto place = [&](auto col_tag, const Chunk<T>& v, int c, int size, int pitch, T* to) {
+    to += decltype(col_tag)::value ? c / (size / E) * pitch + c % (size / E) * E : c / KC * S::ROW + c % KC * E;
+    *reinterpret_cast<Chunk<T>*>(__builtin_assume_aligned(to, 16)) = v;
   };
-  auto store = [&](int buf) {
-    T* ta = tiles + buf * (BM + BN) * LD;
-    T* tb = ta + BM * LD;
+  auto store = [&](int buf, int set) {
+    T* ta = tiles + buf * STAGE;
+    T* tb = ta + A_ELEMS;
 #pragma unroll
-    for (int i = 0; i < A_N; ++i)
-      if (BM * KC >= NT || tid < BM * KC) place(std::bool_constant<ACOL>{}, ra[i], tid + i * NT, BM, ta);
+    for (int i = 0; i < A_N; ++i) place(std::bool_constant<ACOL>{}, ra[set][i], tid + i * NT, BM, S::pitch(BM), ta);
 #pragma unroll
     for (int i = 0; i < B_N; ++i) {
       const int c = tid + i * NT;
       const bool up = EPI::DUAL && c >= BN * KC / 2;
-      place(std::bool_constant<BCOL>{}, rb[i], up ? c - BN * KC / 2 : c, EPI::DUAL ? BN / 2 : BN, up ? tb + BN / 2 * LD : tb);
+      place(std::bool_constant<BCOL>{}, rb[set][i], up ? c - BN * KC / 2 : c, BNO, S::pitch(BN), up ? tb + (BCOL ? BNO : BNO * S::ROW) : tb);
     }
+  };
+  auto b_first = [&](int nb) {                               // first column, in the tile, of a wave's block
+    if (!EPI::DUAL) return wn * TN + nb * 16;
+    return (nb / (NB / 2)) * BNO + wn * (TN / 2) + nb % (NB / 2) * 16;
   };
 
   floatx4_t acc[MB][NB];
@@ -593,43 +679,67 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
   for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  auto b_row = [&](int nb) {
-    if (!EPI::DUAL) return wn * TN + nb * 16;
-    return (nb / (NB / 2)) * (BN / 2) + wn * (TN / 2) + nb % (NB / 2) * 16;
-  };
-  if (k_begin < k_end) load(k_begin);
-  int buf = 0;
-  for (int s = k_begin; s < k_end; ++s) {
-    store(buf);
-    __syncthreads();                                         // (the reads of this buffer, two steps ago, lie before the last barrier)
-    if (s + 1 < k_end) load(s + 1);
-    const T* ta = tiles + buf * (BM + BN) * LD;
-    const T* tb = ta + BM * LD;
+  auto multiply = [&](int buf) {
+    const T* ta = tiles + buf * STAGE;
+    const T* tb = ta + A_ELEMS;
     if constexpr (sizeof(T) == 4) {
-      // K in the order of the reads: MFMA i takes elements 4 kq + i of both operands
-      floatx4_t fa[MB], fb[NB];
+      // 16 of K at a time: MFMA i takes K 4 kq + i of both operands
+      auto four = [&](auto col_tag, const T* t, int first, int pitch, int k) {
+        floatx4_t v;
+        if constexpr (decltype(col_tag)::value) {
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) fa[mb] = *reinterpret_cast<const floatx4_t*>(ta + (wm * TM + mb * 16 + r16) * LD + kq * 4);
+          for (int i = 0; i < 4; ++i) v[i] = t[(k + kq * 4 + i) * pitch + first + r16];
+        } else {
+          v = *reinterpret_cast<const floatx4_t*>(t + (first + r16) * S::ROW + k + kq * 4);
+        }
+        return v;
+      };
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) fb[nb] = *reinterpret_cast<const floatx4_t*>(tb + (b_row(nb) + r16) * LD + kq * 4);
+      for (int k = 0; k < K; k += 16) {
+        floatx4_t fa[MB], fb[NB];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int mb = 0; mb < MB; ++mb) fa[mb] = four(std::bool_constant<ACOL>{}, ta, wm * TM + mb * 16, S::pitch(BM), k);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) fb[nb] = four(std::bool_constant<BCOL>{}, tb, b_first(nb), S::pitch(BN), k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[nb][i], fa[mb][i], acc[mb][nb], 0, 0, 0);
+      }
+    } else {
+      auto eight = [&](auto col_tag, const T* t, int first, int pitch, int k) {
+        if constexpr (decltype(col_tag)::value) return read_turned2(t + (k + kq * 8 + (r16 >> 2)) * pitch + first + (r16 & 3) * 4, 4 * pitch);
+        else return *reinterpret_cast<const bf16x8_t*>(t + (first + r16) * S::ROW + k + kq * 8);
+      };
+#pragma unroll
+      for (int k = 0; k < K; k += 32) {
+        bf16x8_t fa[MB], fb[NB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) fa[mb] = eight(std::bool_constant<ACOL>{}, ta, wm * TM + mb * 16, S::pitch(BM), k);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) fb[nb] = eight(std::bool_constant<BCOL>{}, tb, b_first(nb), S::pitch(BN), k);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[nb][i], fa[mb][i], acc[mb][nb], 0, 0, 0);
-    } else {
-      bf16x8_t fa[MB], fb[NB];
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb) fa[mb] = *reinterpret_cast<const bf16x8_t*>(ta + (wm * TM + mb * 16 + r16) * LD + kq * 8);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) fb[nb] = *reinterpret_cast<const bf16x8_t*>(tb + (b_row(nb) + r16) * LD + kq * 8);
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[nb], fa[mb], acc[mb][nb], 0, 0, 0);
+          for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[nb], fa[mb], acc[mb][nb], 0, 0, 0);
+      }
     }
-    buf ^= 1;
+  };
+  load(k_begin, 0);
+  load(k_begin + 1, 1);
+  for (int s = k_begin; s < k_end; s += 2) {
+    store(0, 0);
+    __syncthreads();                                         // (a buffer's reads lie before the barrier of the step between)
+    load(s + 2, 0);
+    multiply(0);
+    if (s + 1 < k_end) {
+      store(1, 1);
+      __syncthreads();
+      load(s + 3, 1);
+      multiply(1);
+    }
   }
   const int64_t row0 = row_first + wm * TM;
   if constexpr (EPI::RANGES) {

@@ -6,11 +6,11 @@
 namespace cmoe {
 
 // Tiles: rows, columns, columns of waves (the columns of a wave are a range of PRODUCT_LSE).
-enum Tile { RING_256, RING_128, RING_64, ANY_128, ANY_32, TILES };
+enum Tile { RING_256, RING_128, RING_64, ANY_128, ANY_64, ANY_32, TILES };
 struct TileShape {
   int bm, bn, wgn;
 };
-constexpr TileShape kTiles[TILES] = {{256, 256, 2}, {128, 128, 2}, {64, 128, 2}, {128, 128, 2}, {32, 128, 4}};
+constexpr TileShape kTiles[TILES] = {{256, 256, 2}, {128, 128, 2}, {64, 128, 2}, {128, 128, 2}, {64, 64, 2}, {32, 128, 4}};
 
 template <class KERNEL>
 hipError_t launch_tiles(KERNEL kernel, LdsLimit& limit, size_t lds, int bm, int bn, const MatArgs& p, int z, hipStream_t s) {
@@ -29,21 +29,20 @@ hipError_t launch_mat_ring(const MatArgs& p, int z, hipStream_t s) {
 template <int BM, int BN, int WGM, int WGN, bool ACOL, bool BCOL, class EPI>
 hipError_t launch_mat_any(const MatArgs& p, int z, hipStream_t s) {
   static LdsLimit limit;
-  return launch_tiles(matmul_any<BM, BN, WGM, WGN, ACOL, BCOL, EPI>, limit, mat_any_bytes<typename EPI::type, BM, BN, WGM, WGN>(), BM, EPI::DUAL ? BN / 2 : BN, p, z, s);
+  return launch_tiles(matmul_any<BM, BN, WGM, WGN, ACOL, BCOL, EPI>, limit, mat_any_bytes<typename EPI::type, BM, BN, WGM, WGN, ACOL, BCOL>(), BM, EPI::DUAL ? BN / 2 : BN, p, z, s);
 }
 
 template <bool ACOL, bool BCOL, class EPI>
 hipError_t launch_product(Tile tile, const MatArgs& p, hipStream_t s) {
   const int z = EPI::PAIRED && p.c2 ? 2 : 1;
   hipError_t e = hipErrorInvalidValue;
-  if constexpr (sizeof(typename EPI::type) == 2) {
-    if (tile == RING_256) e = launch_mat_ring<256, 256, 5, ACOL, BCOL, EPI>(p, z, s);
-    if (tile == RING_128) e = launch_mat_ring<128, 128, 5, ACOL, BCOL, EPI>(p, z, s);
-    if constexpr (!ACOL) {
-      if (tile == RING_64) e = launch_mat_ring<64, 128, 6, ACOL, BCOL, EPI>(p, z, s);
-    }
+  if (tile == RING_256) e = launch_mat_ring<256, 256, 5, ACOL, BCOL, EPI>(p, z, s);
+  if (tile == RING_128) e = launch_mat_ring<128, 128, 5, ACOL, BCOL, EPI>(p, z, s);
+  if constexpr (!ACOL) {
+    if (tile == RING_64) e = launch_mat_ring<64, 128, 6, ACOL, BCOL, EPI>(p, z, s);
   }
   if (tile == ANY_128) e = launch_mat_any<128, 128, 2, 2, ACOL, BCOL, EPI>(p, z, s);
+  if (tile == ANY_64) e = launch_mat_any<64, 64, 2, 2, ACOL, BCOL, EPI>(p, z, s);
   if (tile == ANY_32) e = launch_mat_any<32, 128, 1, 4, ACOL, BCOL, EPI>(p, z, s);
   if (e != hipSuccess || p.k_split == 1) return e;
   if constexpr (!EPI::RANGES) {

@@ -13,7 +13,7 @@ from test_gpu_operators import Arena, TYPES
 pytestmark = pytest.mark.gpu
 
 RING = {"ring 256": 0, "ring 128": 1, "ring 64": 2}
-ANY = {"any 128": 3, "any 32": 4}
+ANY = {"any 128": 3, "any 64": 4, "any 32": 5}
 TILES = {None: -1, **RING, **ANY}
 
 
@@ -95,6 +95,15 @@ def test_ffn_of_any_size_and_address(B, dtype, t, d, f):
 def test_ffn_on_the_tiles_for_any_operand(B, forced, dtype, tile, split):
     forced(tile, split)
     run_ffn(B, Arena(split, shift=3), TYPES[dtype], 135, 139, 270, base=True)
+
+
+@pytest.mark.parametrize("dtype,shift", [("bf16", 1), ("fp32", 0), ("fp32", 1)])
+@pytest.mark.parametrize("tile", list(RING))
+@pytest.mark.parametrize("split", [1, 4])
+@pytest.mark.parametrize("t,d,f", [(1, 1, 1), (3, 33, 70), (130, 67, 131), (300, 515, 264)])
+def test_ffn_on_the_ring_from_copies(B, forced, dtype, shift, tile, split, t, d, f):
+    forced(tile, split)
+    run_ffn(B, Arena(t + split, shift=shift), TYPES[dtype], t, d, f, base=split == 1)
 
 
 @pytest.mark.parametrize("tile", list(RING))
@@ -213,6 +222,21 @@ def test_head_of_any_size_and_address(B, dtype, t, d, v):
 def test_head_on_the_ring(B, forced, tile, t, d, v):
     forced(tile)
     run_head(B, Arena(t + v, shift=0), TYPES["bf16"], t, d, v, weighted=t % 2 == 1)
+
+
+@pytest.mark.parametrize("dtype,shift", [("bf16", 1), ("fp32", 0), ("fp32", 1)])
+@pytest.mark.parametrize("tile", list(RING))
+@pytest.mark.parametrize("t,d,v", [(1, 9, 3), (70, 67, 257), (300, 64, 1003)])
+def test_head_on_the_ring_from_copies(B, forced, dtype, shift, tile, t, d, v):
+    forced(tile)
+    run_head(B, Arena(t + v, shift=shift), TYPES[dtype], t, d, v, weighted=t % 2 == 1)
+
+
+def test_head_forward_in_pieces(B, forced):
+    """Rows so wide that the forward pass takes the vocabulary in pieces too, from copies and in place."""
+    run_head(B, Arena(8, shift=0), torch.bfloat16, 5, 40000, 4100)
+    forced("ring 128")
+    run_head(B, Arena(8, shift=1), torch.float32, 3, 32771, 4097)
 
 
 @pytest.mark.parametrize("tile", list(RING) + list(ANY))
