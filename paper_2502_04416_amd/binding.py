@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+from itertools import chain
 from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
@@ -691,7 +692,7 @@ def head_loss_backward(x, weight, ids, lse, *, dx=None, dweight=None, dloss=None
 def clip_gradients(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6) -> None:
     """norm[0] = the norm of all tensors of the list together; each scaled by min(1, max_norm / (norm + eps)), in place or into out's.
 
-    grads, out: lists of contiguous tensors of any shapes, bfloat16 or float32 each; norm: [1] fp32.  max_norm = inf: the norm alone (out's
+    grads, out: lists of contiguous tensors of any shapes, bfloat16 or float32 each, out's of the sizes and types of grads; norm: [1] fp32.  max_norm = inf: the norm alone (out's
     tensors are then copies)."""
     if not max_norm >= 0.0 or not 0.0 <= eps <= 3e38:
         raise CmoeError("clip_gradients: max_norm and eps must not be negative, eps finite")
@@ -701,17 +702,25 @@ def clip_gradients(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6)
         out = grads
     elif len(out) != len(grads):
         raise CmoeError("clip_gradients: out must have a tensor for each of grads")
-    dev, stream = _place("norm", norm)
     import torch
-    to = _operand("norm", norm, torch.float32, (1,), dev)
-    listed, code = [], {torch.bfloat16: CMOE_BF16, torch.float32: CMOE_F32}
-    for g, o in zip(grads, out):
-        dtype = g.dtype
-        if dtype not in code:
-            raise CmoeError("grads must be bfloat16 or float32, not %s" % dtype)
-        at = _operand("grads", g, dtype, g.shape, dev)
-        listed.append(_GRADIENT.pack(at, at if o is g else _operand("out", o, dtype, g.shape, dev), g.numel(), code[dtype], 0))
-    packed, n = b"".join(listed), len(listed)
+    dev, stream = _place("norm", norm)
+    to, n, tensor = _operand("norm", norm, torch.float32, (1,), dev), len(grads), torch.Tensor
+    # a call's time is the host's where tensors are many and small: columns of the list at once, not tensor by tensor
+    sizes = [*map(tensor.numel, grads)]
+    dtypes = [g.dtype for g in grads]
+    lists = (("grads", grads),) if out is grads else (("grads", grads), ("out", out))
+    for name, ts in lists:
+        if not all(map(tensor.is_contiguous, ts)):
+            raise CmoeError("%s must be contiguous tensors" % name)
+        if {*map(tensor.get_device, ts)} - {dev}:
+            raise CmoeError("%s must be on the current HIP device" % name)
+    if out is not grads and ([*map(tensor.numel, out)] != sizes or [o.dtype for o in out] != dtypes):
+        raise CmoeError("out must have the sizes and types of grads")
+    code = {torch.bfloat16: CMOE_BF16, torch.float32: CMOE_F32}
+    if not code.keys() >= {*dtypes}:
+        raise CmoeError("grads must be bfloat16 or float32")
+    at = [*map(tensor.data_ptr, grads)]
+    packed = struct.pack("=" + "QQqq" * n, *chain.from_iterable(zip(at, at if out is grads else map(tensor.data_ptr, out), sizes, [code[t] for t in dtypes])))
     lib = load()
     nbytes = lib.cmoe_clip_gradients_workspace_bytes(packed, n)
     ws = _workspace(nbytes) if nbytes else None

@@ -41,8 +41,9 @@ struct MatArgs {
   const float* dloss;        // [m] or null
   float2* part;              // [column ranges][m]
   float* picked;             // [m]
-  // K split: part s of a tile stores its sums to slab [k_split][m][n], a finishing kernel adds them in order
-  int k_split;
+  // Tiles are numbered over both results (zs of them); from tile `full` on, each is split into k_split parts of K, whose sums go to slab
+  // [tile][part][bm][bn] (both halves of a gated tile side by side), and a finishing kernel adds them in order.
+  int zs, full, k_split, bm, bn;
   float* slab;
 };
 

@@ -17,20 +17,24 @@ struct Shape {
 };
 constexpr Shape shape_of(Product kind) {
   return {kind == PRODUCT_DW, kind == PRODUCT_GATED || kind == PRODUCT_DOWN || kind == PRODUCT_DW || kind == PRODUCT_DHEAD, kind == PRODUCT_GATED,
-          kind == PRODUCT_DX, kind != PRODUCT_LSE && kind != PRODUCT_DLOGITS};
+          kind == PRODUCT_DX, kind != PRODUCT_LSE};
 }
 
 struct Choice {
   Tile tile;
-  int k_split;
+  int full, k_split;
   bool copies;
+  size_t slab;               // bytes
 };
 
-// Times in us, of a K step of 32 of a tile when the chip is full, of a tile's beginning and end, and workgroups per CU.
-constexpr double kStep[TILES] = {0.68, 0.41, 0.29, 1.8, 0.70, 0.70};
-constexpr double kStepFp32[TILES] = {0.68, 0.41, 0.29, 5.0, 2.6, 2.6};
-constexpr int kPerCu[TILES] = {1, 2, 2, 2, 4, 2};
-constexpr double kTile = 11, kLaunch = 4, kBytesPerUs = 4.5e6;
+// What a tile takes, in us: a K step of 32 where a CU is full of such tiles, and where it has one alone; its beginning and end; tiles to a CU.
+struct Cost {
+  double step, alone, ends;
+  int per_cu;
+};
+constexpr Cost kBf16[TILES] = {{0.69, 0.62, 14, 1}, {0.41, 0.265, 6, 2}, {0.30, 0.20, 5, 2}, {1.2, 1.0, 6, 2}, {0.70, 0.45, 5, 4}, {0.70, 0.45, 5, 2}};
+constexpr Cost kFp32[TILES] = {{0.69, 0.62, 14, 1}, {0.41, 0.265, 6, 2}, {0.30, 0.20, 5, 2}, {5.0, 4.0, 8, 2}, {3.3, 1.3, 6, 4}, {3.0, 1.6, 6, 2}};
+constexpr double kLaunch = 4, kBytesPerUs = 4.5e6;
 
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
 
@@ -42,6 +46,7 @@ size_t copy_bytes(const Shape& sh, int planes, int64_t m, int64_t n, int64_t k, 
 }
 
 // direct: bf16 operands that the ring can read where they are.  second: there is a second B.
+// The tiles that fill the chip a whole number of times are left whole; the rest, if that is shorter, is split.
 Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace) {
   const Shape sh = shape_of(kind);
   const int pair = kind == PRODUCT_DW && second ? 2 : 1, planes = dtype == CMOE_F32 ? 3 : 1;
@@ -50,7 +55,9 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
   const int forced_tile = tuning().mat_tile, forced_split = tuning().mat_split;
   const size_t copies = direct ? 0 : copy_bytes(sh, planes, m, n, k, second);
   const double copy_time = direct ? 0 : kLaunch + (double)copies * (planes == 3 ? 10.0 / 6 : 2) / kBytesPerUs;
-  Choice best{ANY_64, 1, false};
+  // the operands once, at the rate at which they arrive
+  const double arrive = (double)(m * steps1 * 32 + cols * steps1 * 32) * (planes == 3 ? 4 : 2) / kBytesPerUs;
+  Choice best{ANY_64, 0, 1, false, 0};
   double best_cost = 1e300;
   for (int t = RING_256; t <= (direct ? RING_64 : ANY_32); ++t) {
     const bool ring = t <= RING_64;
@@ -60,19 +67,20 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
     if (room > workspace) continue;
     const int64_t steps = steps1 * (ring && planes == 3 ? PAIRS : 1);
     const int64_t tiles = (m + kTiles[t].bm - 1) / kTiles[t].bm * ((cols + kTiles[t].bn - 1) / kTiles[t].bn) * pair;
-    const double step = dtype == CMOE_F32 ? kStepFp32[t] : kStep[t];
-    for (int split = 1; split <= 16; split *= 2) {
-      if (split > 1 && (!sh.splits || pair > 1 || room + (size_t)split * m * cols * 4 > workspace)) break;
-      if (split > 1 && forced_split < 1 && steps / split < 8) break;
-      if (forced_split >= 1 && split != forced_split && sh.splits && pair == 1) continue;
-      const int64_t slots = (int64_t)CUS * kPerCu[t];
-      const double rounds = (double)((tiles * split + slots - 1) / slots);
-      // a last round that does not fill the chip still takes a tile's time; with one workgroup on a CU of several it is shorter
-      const double fill = tiles * split <= CUS && kPerCu[t] > 1 ? 0.6 : 1.0;
-      double cost = kLaunch + rounds * fill * step * ((double)(steps + split - 1) / split + kTile / 0.68);
+    const Cost& c = (dtype == CMOE_F32 ? kFp32 : kBf16)[t];
+    const int64_t slots = (int64_t)CUS * c.per_cu, full = sh.splits ? tiles / slots * slots : 0, rest = tiles - full;
+    for (int split = 1; split <= 32; ++split) {
+      const size_t slab = split > 1 ? (size_t)rest * split * kTiles[t].bm * kTiles[t].bn * 4 : 0;
+      if (split > 1 && (!sh.splits || rest == 0 || room + slab > workspace)) break;
+      if (split > 1 && forced_split < 1 && (steps / split < 6 || rest * (split - 1) >= slots)) break;
+      if (forced_split >= 1 && split != forced_split && sh.splits && rest > 0) continue;
+      const double part = (double)((steps + split - 1) / split);
+      double cost = kLaunch + (double)(full / slots) * (steps * c.step + c.ends);
+      for (int64_t left = rest * split; left > 0; left -= slots) cost += part * (left <= CUS ? c.alone : c.step) + c.ends;
+      cost = std::max(cost, kLaunch + arrive);
       if (ring) cost += copy_time;
-      if (split > 1) cost += kLaunch + (double)split * m * cols * 8 / kBytesPerUs;
-      if (cost < best_cost) best_cost = cost, best = {(Tile)t, split, ring && !direct};
+      if (split > 1) cost += kLaunch + (double)slab * 2 / kBytesPerUs;
+      if (cost < best_cost) best_cost = cost, best = {(Tile)t, split > 1 ? (int)full : (int)(tiles / 8 * 8), split, ring && !direct, slab};
     }
   }
   return best;
@@ -109,7 +117,7 @@ size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int
   for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct)
     for (int second = has_second(kind); second <= (has_second(kind) || kind == PRODUCT_DW); ++second) {
       const Choice c = choose(kind, dtype, direct, second, m, n, k, EVERYTHING);
-      most = std::max(most, (c.copies ? copy_bytes(sh, dtype == CMOE_F32 ? 3 : 1, m, n, k, second) : 0) + (c.k_split > 1 ? (size_t)c.k_split * m * n * 4 * (sh.dual ? 2 : 1) : 0));
+      most = std::max(most, (c.copies ? copy_bytes(sh, dtype == CMOE_F32 ? 3 : 1, m, n, k, second) : 0) + c.slab);
     }
   return (most + 15) / 16 * 16;
 }
@@ -125,7 +133,8 @@ hipError_t matmul(Product kind, int dtype, MatArgs p, void* workspace, size_t wo
   const bool direct = dtype == CMOE_BF16 && wide(p.a) && wide(p.a2) && wide(p.b) && wide(p.b2) && p.lda % 8 == 0 && p.ldb % 8 == 0 &&
                       (sh.a_columns ? p.m_a : p.k) % 8 == 0 && (sh.b_columns ? p.n_b : p.k) % 8 == 0;
   const Choice c = choose(kind, dtype, direct, second, p.m, p.n, p.k, workspace ? workspace_bytes : 0);
-  p.k_split = c.k_split;
+  p.zs = kind == PRODUCT_DW && second ? 2 : 1;
+  p.full = c.full, p.k_split = c.k_split, p.bm = kTiles[c.tile].bm, p.bn = kTiles[c.tile].bn;
   char* room = static_cast<char*>(workspace);
   if (c.copies) {
     const int planes = dtype == CMOE_F32 ? 3 : 1;

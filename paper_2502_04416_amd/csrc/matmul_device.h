@@ -36,32 +36,66 @@ template <> __device__ __forceinline__ float exp_of<bf16_t>(float x) { return __
 template <typename T> __device__ __forceinline__ float sigmoid_of(float x) { return 1.0f / (1.0f + exp_of<T>(-x)); }
 
 // ---- what happens to eight consecutive columns of a row of the result ---------------------------------------------
-// put: n of them exist; v, and for DUAL w, hold the sums.
+// hold: what it reads of global memory for them (n of them exist); put: with v, and for DUAL w, the sums.
+
+// Eight values as they lie in memory.
+template <typename T>
+struct Raw8 {
+  uint32_t w[2 * sizeof(T)];
+};
+template <typename T>
+__device__ __forceinline__ void hold8(const T* p, int n, Raw8<T>& r) {
+  if (n >= 8) {
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+      const Bytes16<T> b = *reinterpret_cast<const Bytes16<T>*>(p + 16 / sizeof(T) * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.w[4 * h + e] = b.w[e];
+    }
+  } else {
+    float v[8];
+    load8(p, n, v);
+#pragma unroll
+    for (int e = 0; e < 2 * (int)sizeof(T); ++e) r.w[e] = sizeof(T) == 4 ? __float_as_uint(v[e]) : pack_bf16(v[2 * (e & 3)], v[2 * (e & 3) + 1]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float held(const Raw8<T>& r, int e) {
+  if (sizeof(T) == 4) return __uint_as_float(r.w[e & (2 * sizeof(T) - 1)]);
+  return __uint_as_float(e & 1 ? r.w[e >> 1] & 0xffff0000u : r.w[e >> 1] << 16);
+}
 
 template <typename T, bool SEGS, bool PAIR>
 struct EpiStore {                                             // PRODUCT_DOWN, PRODUCT_DX, PRODUCT_DW
   static constexpr bool DUAL = false, SEGMENTS = SEGS, PAIRED = PAIR, RANGES = false;
   typedef T type;
-  static __device__ __forceinline__ void put(const MatArgs& p, int z, int64_t row, int col, int n, float (&v)[8], float (&)[8]) {
-    const int64_t at = row * p.ldc + col;
+  struct Held {
+    Raw8<T> base;
+  };
+  static __device__ __forceinline__ void hold(const MatArgs& p, int64_t row, int col, int n, Held& h) {
+    if (!PAIR && p.e1) hold8(static_cast<const T*>(p.e1) + row * p.ldc + col, n, h.base);
+  }
+  static __device__ __forceinline__ void put(const MatArgs& p, int z, int64_t row, int col, int n, float (&v)[8], float (&)[8], const Held& h) {
     if (PAIR) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= p.alpha;
     } else if (p.e1) {
-      float base[8];
-      load8(static_cast<const T*>(p.e1) + at, n, base);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += base[e];
+      for (int e = 0; e < 8; ++e) v[e] += held(h.base, e);
     }
-    store8(static_cast<T*>(PAIR && z ? p.c2 : p.c) + at, n, v);
+    store8(static_cast<T*>(PAIR && z ? p.c2 : p.c) + row * p.ldc + col, n, v);
   }
 };
+
+struct HeldNothing {};
 
 template <typename T>
 struct EpiGated {
   static constexpr bool DUAL = true, SEGMENTS = false, PAIRED = false, RANGES = false;
   typedef T type;
-  static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&w)[8]) {
+  typedef HeldNothing Held;
+  static __device__ __forceinline__ void hold(const MatArgs&, int64_t, int, int, Held&) {}
+  static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&w)[8], const Held&) {
     const int64_t at = row * p.ldc + col;
     if (p.c2) {
       store8(static_cast<T*>(p.c2) + at, n, v);
@@ -77,19 +111,25 @@ template <typename T>
 struct EpiDGated {
   static constexpr bool DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
   typedef T type;
-  static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&)[8]) {
+  struct Held {
+    Raw8<T> gate, up;
+  };
+  static __device__ __forceinline__ void hold(const MatArgs& p, int64_t row, int col, int n, Held& h) {
     const int64_t at = row * p.ldc + col;
-    float g[8], u[8];
-    load8(static_cast<const T*>(p.e1) + at, n, g);
-    load8(static_cast<const T*>(p.e2) + at, n, u);
+    hold8(static_cast<const T*>(p.e1) + at, n, h.gate);
+    hold8(static_cast<const T*>(p.e2) + at, n, h.up);
+  }
+  static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&)[8], const Held& h) {
+    const int64_t at = row * p.ldc + col;
+    float dg[8], du[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float s = sigmoid_of<T>(g[e]);
-      u[e] *= v[e] * s * (1.0f + g[e] * (1.0f - s));
-      g[e] *= v[e] * s;
+      const float g = held(h.gate, e), s = sigmoid_of<T>(g);
+      dg[e] = held(h.up, e) * v[e] * s * (1.0f + g * (1.0f - s));
+      du[e] = g * v[e] * s;
     }
-    store8(static_cast<T*>(p.c) + at, n, u);
-    store8(static_cast<T*>(p.c2) + at, n, g);
+    store8(static_cast<T*>(p.c) + at, n, dg);
+    store8(static_cast<T*>(p.c2) + at, n, du);
   }
 };
 
@@ -97,14 +137,21 @@ template <typename T>
 struct EpiDLogits {
   static constexpr bool DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
   typedef T type;
-  static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&)[8]) {
-    const int id = p.ids[row];
-    const float lse = p.lse[row], weight = p.dloss ? p.dloss[row] : 1.0f;
-    const bool has = (unsigned)id < (unsigned)p.vocab;
+  struct Held {
+    int id;
+    float lse, weight;
+  };
+  static __device__ __forceinline__ void hold(const MatArgs& p, int64_t row, int, int, Held& h) {
+    h.id = p.ids[row];
+    h.lse = p.lse[row];
+    h.weight = p.dloss ? p.dloss[row] : 1.0f;
+  }
+  static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&)[8], const Held& h) {
+    const bool has = (unsigned)h.id < (unsigned)p.vocab;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float d = exp_of<T>(v[e] - lse) - (id == p.col0 + col + e ? 1.0f : 0.0f);
-      v[e] = has && col + e < p.n_b ? d * weight : 0.0f;     // (columns behind the vocabulary are zeros)
+      const float d = exp_of<T>(v[e] - h.lse) - (h.id == p.col0 + col + e ? 1.0f : 0.0f);
+      v[e] = has && col + e < p.n_b ? d * h.weight : 0.0f;   // (columns behind the vocabulary are zeros)
     }
     store8(static_cast<T*>(p.c) + row * p.ldc + col, n, v);
   }
@@ -114,20 +161,23 @@ template <typename T>
 struct EpiDHead {
   static constexpr bool DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
   typedef T type;
-  static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&)[8]) {
-    float* acc = p.acc + row * p.n + col;
+  struct Held {
+    Raw8<float> before;
+  };
+  static __device__ __forceinline__ void hold(const MatArgs& p, int64_t row, int col, int n, Held& h) {
+    if (!p.first) hold8(p.acc + row * p.n + col, n, h.before);
+  }
+  static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&)[8], const Held& h) {
     if (!p.first) {
-      float before[8];
-      load8(acc, n, before);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += before[e];
+      for (int e = 0; e < 8; ++e) v[e] += held(h.before, e);
     }
     if (p.last) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= p.alpha;
       store8(static_cast<T*>(p.c) + row * p.ldc + col, n, v);
     } else {
-      store8(acc, n, v);
+      store8(p.acc + row * p.n + col, n, v);
     }
   }
 };
@@ -136,7 +186,6 @@ template <typename T>
 struct EpiLse {
   static constexpr bool DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = true;
   typedef T type;
-  static __device__ __forceinline__ void put(const MatArgs&, int, int64_t, int, int, float (&)[8], float (&)[8]) {}
 };
 
 // The largest of two, and the exponentials summed below it.  An empty range is (-inf, 0).
@@ -182,104 +231,158 @@ __device__ __forceinline__ void put_ranges(const MatArgs& p, const floatx4_t (&a
   }
 }
 
+// Which tile a workgroup has.  Workgroup b runs on XCD b % 8, each of which works through a run of the list, so that tiles that share
+// an operand meet in one L2; inside the list the row tile runs fastest in bands of eight.  The last p.full .. tiles, which would not fill the
+// chip, are given to p.k_split workgroups each, a range of K to every one: behind the parts of one range come those of the next.
+struct TileAt {
+  int mt, nt, z;
+  int part;                  // of p.k_split
+  int slot;                  // among the tiles that are split; -1: this one is not
+};
+__device__ __forceinline__ void tile_of(const MatArgs& p, int tile, int n_mt, int n_nt, TileAt* at) {
+  const int each = n_mt * n_nt;
+  at->z = tile >= each;
+  const int local = tile - at->z * each;
+  constexpr int BAND = 8;
+  const int band = local / (BAND * n_nt), rem = local - band * (BAND * n_nt);
+  const int rows = min(n_mt - band * BAND, BAND);
+  at->mt = band * BAND + rem % rows;
+  at->nt = rem / rows;
+}
+__device__ __forceinline__ bool find_tile(const MatArgs& p, int n_mt, int n_nt, TileAt* at) {
+  const int b = blockIdx.x;
+  int tile;
+  at->part = 0;
+  at->slot = -1;
+  if (b < p.full) {
+    tile = (b & 7) * (p.full >> 3) + (b >> 3);
+  } else {
+    const int rest = n_mt * n_nt * p.zs - p.full, items = rest * p.k_split, chunk = (items + 7) >> 3;
+    const int item = (b & 7) * chunk + ((b - p.full) >> 3);
+    if (((b - p.full) >> 3) >= chunk || item >= items) return false;
+    at->part = item / rest;
+    const int slot = item - at->part * rest;
+    if (p.k_split > 1) at->slot = slot;
+    tile = p.full + slot;
+  }
+  tile_of(p, tile, n_mt, n_nt, at);
+  return true;
+}
+
 // A wave's tile [MB * 16][NB * 16] from its accumulators to eight columns of a row per lane, 32 rows at a time through a strip of LDS
 // that is the wave's own.
 template <int MB, int NB>
 constexpr int strip_floats() { return (MB > 1 ? 32 : 16) * (NB * 16 + 4); }
 
 template <int MB, int NB, class EPI>
-__device__ __forceinline__ void put_tile(const MatArgs& p, const floatx4_t (&acc)[MB][NB], float* strip, int z, int part, int64_t row0, int col0) {
+__device__ __forceinline__ void put_tile(const MatArgs& p, const floatx4_t (&acc)[MB][NB], float* strip, const TileAt& at, int wave_row, int wave_col, int64_t row0,
+                                         int col0) {
   constexpr int RB = MB > 1 ? 2 : 1, TN = NB * 16, LD = TN + 4;
-  constexpr int OUT = EPI::DUAL ? TN / 2 : TN, CH = OUT / 8;
-  static_assert(MB % RB == 0, "rows of a strip");
+  constexpr int OUT = EPI::DUAL ? TN / 2 : TN, CH = OUT / 8, TURNS = RB * 16 * CH / 64;
+  static_assert(MB % RB == 0 && RB * 16 * CH % 64 == 0, "rows of a strip");
   const int lane = threadIdx.x & 63, r16 = lane & 15, kq = lane >> 4;
-  float* slab = p.k_split > 1 ? p.slab + ((int64_t)part * p.m) * (EPI::DUAL ? 2 * p.n : p.n) : nullptr;
+  if (at.slot >= 0) {
+    // a part of a tile: its sums as they are, the tile's rows one after the other
+    float* slab = p.slab + ((int64_t)(at.slot * p.k_split + at.part) * p.bm + wave_row) * p.bn;
 #pragma unroll
-  for (int mb = 0; mb < MB; mb += RB) {
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const int col = EPI::DUAL ? nb / (NB / 2) * (p.bn / 2) + wave_col + nb % (NB / 2) * 16 : wave_col + nb * 16;
+        *reinterpret_cast<floatx4_t*>(slab + (mb * 16 + r16) * p.bn + col + kq * 4) = acc[mb][nb];
+      }
+    return;
+  }
+  auto stage = [&](int mb) {
 #pragma unroll
     for (int r = 0; r < RB; ++r)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) *reinterpret_cast<floatx4_t*>(strip + (r * 16 + r16) * LD + nb * 16 + kq * 4) = acc[mb + r][nb];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 2
+  };
+  auto take = [&](int rr, int cc, float (&v)[8], float (&w)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const floatx4_t f = *reinterpret_cast<const floatx4_t*>(strip + rr * LD + cc + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * h + e] = f[e];
+      if (EPI::DUAL) {
+        const floatx4_t g = *reinterpret_cast<const floatx4_t*>(strip + rr * LD + OUT + cc + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * h + e] = g[e];
+      }
+    }
+  };
+  if (row0 + MB * 16 <= p.m && col0 + OUT <= p.n) {
+    // A tile that is whole: nothing has to be asked for every row, and what the rows of a strip read is under way before the strip is written.
+    typename EPI::Held held[TURNS];
+    const int rr0 = lane / CH, cc = lane % CH * 8;
+#pragma unroll
+    for (int mb = 0; mb < MB; mb += RB) {
+#pragma unroll
+      for (int t = 0; t < TURNS; ++t) EPI::hold(p, row0 + mb * 16 + rr0 + t * (64 / CH), col0 + cc, 8, held[t]);
+      stage(mb);
+#pragma unroll
+      for (int t = 0; t < TURNS; ++t) {
+        float v[8], w[8];
+        take(rr0 + t * (64 / CH), cc, v, w);
+        EPI::put(p, at.z, row0 + mb * 16 + rr0 + t * (64 / CH), col0 + cc, 8, v, w, held[t]);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    return;
+  }
+#pragma unroll
+  for (int mb = 0; mb < MB; mb += RB) {
+    stage(mb);
+#pragma unroll 1
     for (int q = lane; q < RB * 16 * CH; q += 64) {
       const int rr = q / CH, cc = q % CH * 8;
       const int64_t row = row0 + mb * 16 + rr;
       const int col = col0 + cc;
       float v[8], w[8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const floatx4_t f = *reinterpret_cast<const floatx4_t*>(strip + rr * LD + cc + 4 * h);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * h + e] = f[e];
-        if (EPI::DUAL) {
-          const floatx4_t g = *reinterpret_cast<const floatx4_t*>(strip + rr * LD + OUT + cc + 4 * h);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[4 * h + e] = g[e];
-        }
-      }
+      take(rr, cc, v, w);
       if (row >= p.m || col >= p.n) continue;
-      const int n = p.n - col;
-      if (slab) {
-        float* to = slab + row * (EPI::DUAL ? 2 * p.n : p.n) + col;
-        store8(to, n, v);
-        if (EPI::DUAL) store8(to + p.n, n, w);
-      } else {
-        EPI::put(p, z, row, col, n, v, w);
-      }
+      typename EPI::Held held;
+      EPI::hold(p, row, col, p.n - col, held);
+      EPI::put(p, at.z, row, col, p.n - col, v, w, held);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
-// The parts of a K split, added in order.
+// The parts of the tiles that are split, added in order: a thread per eight columns, gridDim.y parts of a tile.
 template <class EPI>
 __global__ __launch_bounds__(256) void matmul_finish(MatArgs p) {
-  const int per_row = (p.n + 7) >> 3;
-  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = q / per_row;
-  if (row >= p.m) return;
-  const int col = (int)(q - row * per_row) * 8, n = p.n - col;
-  const int64_t cols = EPI::DUAL ? 2 * (int64_t)p.n : p.n;
-  const float* from = p.slab + row * cols + col;
+  const int bno = EPI::DUAL ? p.bn / 2 : p.bn, per_row = bno >> 3;
+  const int q = blockIdx.y * 256 + threadIdx.x, rr = q / per_row, cc = q % per_row * 8;
+  TileAt at;
+  tile_of(p, p.full + blockIdx.x, (p.m + p.bm - 1) / p.bm, (p.n + bno - 1) / bno, &at);
+  const int64_t row = (int64_t)at.mt * p.bm + rr;
+  const int col = at.nt * bno + cc, n = p.n - col;
+  if (rr >= p.bm || row >= p.m || col >= p.n) return;
+  const int64_t each = (int64_t)p.bm * p.bn;
+  const float* from = p.slab + blockIdx.x * p.k_split * each + rr * p.bn + cc;
   float v[8], w[8];
-  load8(from, n, v);
-  if (EPI::DUAL) load8(from + p.n, n, w);
+  typename EPI::Held held;
+  EPI::hold(p, row, col, n, held);
+  load8(from, 8, v);
+  if (EPI::DUAL) load8(from + bno, 8, w);
+#pragma unroll 2
   for (int s = 1; s < p.k_split; ++s) {
     float t[8];
-    from += p.m * cols;
-    load8(from, n, t);
+    from += each;
+    load8(from, 8, t);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += t[e];
     if (EPI::DUAL) {
-      load8(from + p.n, n, t);
+      load8(from + bno, 8, t);
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[e] += t[e];
     }
   }
-  EPI::put(p, 0, row, col, n, v, w);
+  EPI::put(p, at.z, row, col, n, v, w, held);
 }
-
-// Which tile a workgroup has.  Workgroup b runs on XCD b % 8, each of which works through a run of the list, so that tiles that share
-// an operand meet in one L2; inside the list the row tile runs fastest in bands of eight.  Behind the tiles of one part of K come those of the next.
-struct TileAt {
-  int mt, nt, part;
-};
-__device__ __forceinline__ bool find_tile(const MatArgs& p, int n_mt, int n_nt, TileAt* at) {
-  const int tiles = n_mt * n_nt, total = tiles * p.k_split;
-  const int chunk = (total + 7) >> 3;
-  const int item = (blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= chunk || item >= total) return false;
-  at->part = item / tiles;
-  const int local = item - at->part * tiles;
-  constexpr int BAND = 8;
-  const int band = local / (BAND * n_nt), rem = local - band * (BAND * n_nt);
-  const int rows = min(n_mt - band * BAND, BAND);
-  at->mt = band * BAND + rem % rows;
-  at->nt = rem / rows;
-  return true;
-}
-inline __host__ int grid_of(int64_t tiles, int k_split) { return (int)((tiles * k_split + 7) / 8 * 8); }
 
 // ---- operands copied for the ring ---------------------------------------------------------------------------------------
 
@@ -387,11 +490,11 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   TileAt at;
   constexpr int BNO = EPI::DUAL ? BN / 2 : BN;               // columns of the result in a tile
   if (!find_tile(p, (p.m + BM - 1) / BM, (p.n + BNO - 1) / BNO, &at)) return;
-  const int z = blockIdx.y;
+  const int z = at.z;
   const int row_first = at.mt * BM, col_first = at.nt * BNO;
   const int seg_steps = (p.k + BK - 1) / BK;                 // steps of a part of K
   const int all = SEGS * seg_steps;
-  const int per = (all + p.k_split - 1) / p.k_split;
+  const int per = at.slot < 0 ? all : (all + p.k_split - 1) / p.k_split;
   const int k_begin = min(at.part * per, all), KT = min(per, all - k_begin);
 
   // Lanes' offsets in bytes from the operand's place of a step; DMA_NONE: zeros.  By rows: load i of a wave is block wave + 4 i,
@@ -557,7 +660,8 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
     put_ranges<MB, NB>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
   } else {
     __syncthreads();                                         // every wave has left the ring
-    put_tile<MB, NB, EPI>(p, acc, reinterpret_cast<float*>(smem) + wave * strip_floats<MB, NB>(), z, at.part, row0, col_first + wn * (EPI::DUAL ? TN / 2 : TN));
+    put_tile<MB, NB, EPI>(p, acc, reinterpret_cast<float*>(smem) + wave * strip_floats<MB, NB>(), at, wm * TM, wn * (EPI::DUAL ? TN / 2 : TN), row0,
+                          col_first + wn * (EPI::DUAL ? TN / 2 : TN));
   }
 }
 
@@ -613,11 +717,11 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
   TileAt at;
   constexpr int BNO = EPI::DUAL ? BN / 2 : BN;
   if (!find_tile(p, (p.m + BM - 1) / BM, (p.n + BNO - 1) / BNO, &at)) return;
-  const int z = blockIdx.y;
+  const int z = at.z;
   const int row_first = at.mt * BM, col_first = at.nt * BNO;
   const int seg_steps = (p.k + K - 1) / K;
   const int all = EPI::SEGMENTS ? 2 * seg_steps : seg_steps;
-  const int per = (all + p.k_split - 1) / p.k_split;
+  const int per = at.slot < 0 ? all : (all + p.k_split - 1) / p.k_split;
   const int k_begin = min(at.part * per, all), k_end = min(k_begin + per, all);
 
   Chunk<T> ra[2][A_N], rb[2][B_N];
@@ -746,7 +850,8 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
     put_ranges<MB, NB>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
   } else {
     __syncthreads();
-    put_tile<MB, NB, EPI>(p, acc, reinterpret_cast<float*>(any_smem) + wave * strip_floats<MB, NB>(), z, at.part, row0, col_first + wn * (EPI::DUAL ? TN / 2 : TN));
+    put_tile<MB, NB, EPI>(p, acc, reinterpret_cast<float*>(any_smem) + wave * strip_floats<MB, NB>(), at, wm * TM, wn * (EPI::DUAL ? TN / 2 : TN), row0,
+                          col_first + wn * (EPI::DUAL ? TN / 2 : TN));
   }
 }
 

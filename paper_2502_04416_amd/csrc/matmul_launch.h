@@ -5,7 +5,7 @@
 
 namespace cmoe {
 
-// Tiles: rows, columns, columns of waves (the columns of a wave are a range of PRODUCT_LSE).
+// The ring's tiles and those of the kernel for any operand: rows, columns, columns of waves (the columns of a wave are a range of PRODUCT_LSE).
 enum Tile { RING_256, RING_128, RING_64, ANY_128, ANY_64, ANY_32, TILES };
 struct TileShape {
   int bm, bn, wgn;
@@ -13,41 +13,41 @@ struct TileShape {
 constexpr TileShape kTiles[TILES] = {{256, 256, 2}, {128, 128, 2}, {64, 128, 2}, {128, 128, 2}, {64, 64, 2}, {32, 128, 4}};
 
 template <class KERNEL>
-hipError_t launch_tiles(KERNEL kernel, LdsLimit& limit, size_t lds, int bm, int bn, const MatArgs& p, int z, hipStream_t s) {
+hipError_t launch_tiles(KERNEL kernel, LdsLimit& limit, size_t lds, const MatArgs& p, int bno, hipStream_t s) {
   if (lds > 64 * 1024)
     if (hipError_t e = limit.raise(reinterpret_cast<const void*>(kernel), lds)) return e;
-  const int64_t tiles = ((int64_t)p.m + bm - 1) / bm * (((int64_t)p.n + bn - 1) / bn);
-  hipLaunchKernelGGL(kernel, dim3(grid_of(tiles, p.k_split), z), dim3(256), lds, s, p);
+  const int64_t tiles = ((int64_t)p.m + p.bm - 1) / p.bm * (((int64_t)p.n + bno - 1) / bno) * p.zs;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.full + ((tiles - p.full) * p.k_split + 7) / 8 * 8)), dim3(256), lds, s, p);
   return hipGetLastError();
 }
 
 template <int BM, int BN, int STAGES, bool ACOL, bool BCOL, class EPI>
-hipError_t launch_mat_ring(const MatArgs& p, int z, hipStream_t s) {
+hipError_t launch_mat_ring(const MatArgs& p, hipStream_t s) {
   static LdsLimit limit;
-  return launch_tiles(matmul_ring<BM, BN, STAGES, 2, 2, ACOL, BCOL, EPI>, limit, mat_ring_bytes<BM, BN, STAGES, 2, 2>(), BM, EPI::DUAL ? BN / 2 : BN, p, z, s);
+  return launch_tiles(matmul_ring<BM, BN, STAGES, 2, 2, ACOL, BCOL, EPI>, limit, mat_ring_bytes<BM, BN, STAGES, 2, 2>(), p, EPI::DUAL ? BN / 2 : BN, s);
 }
 template <int BM, int BN, int WGM, int WGN, bool ACOL, bool BCOL, class EPI>
-hipError_t launch_mat_any(const MatArgs& p, int z, hipStream_t s) {
+hipError_t launch_mat_any(const MatArgs& p, hipStream_t s) {
   static LdsLimit limit;
-  return launch_tiles(matmul_any<BM, BN, WGM, WGN, ACOL, BCOL, EPI>, limit, mat_any_bytes<typename EPI::type, BM, BN, WGM, WGN, ACOL, BCOL>(), BM, EPI::DUAL ? BN / 2 : BN, p, z, s);
+  return launch_tiles(matmul_any<BM, BN, WGM, WGN, ACOL, BCOL, EPI>, limit, mat_any_bytes<typename EPI::type, BM, BN, WGM, WGN, ACOL, BCOL>(), p, EPI::DUAL ? BN / 2 : BN, s);
 }
 
 template <bool ACOL, bool BCOL, class EPI>
 hipError_t launch_product(Tile tile, const MatArgs& p, hipStream_t s) {
-  const int z = EPI::PAIRED && p.c2 ? 2 : 1;
   hipError_t e = hipErrorInvalidValue;
-  if (tile == RING_256) e = launch_mat_ring<256, 256, 5, ACOL, BCOL, EPI>(p, z, s);
-  if (tile == RING_128) e = launch_mat_ring<128, 128, 5, ACOL, BCOL, EPI>(p, z, s);
+  if (tile == RING_256) e = launch_mat_ring<256, 256, 5, ACOL, BCOL, EPI>(p, s);
+  if (tile == RING_128) e = launch_mat_ring<128, 128, 5, ACOL, BCOL, EPI>(p, s);
   if constexpr (!ACOL) {
-    if (tile == RING_64) e = launch_mat_ring<64, 128, 6, ACOL, BCOL, EPI>(p, z, s);
+    if (tile == RING_64) e = launch_mat_ring<64, 128, 6, ACOL, BCOL, EPI>(p, s);
   }
-  if (tile == ANY_128) e = launch_mat_any<128, 128, 2, 2, ACOL, BCOL, EPI>(p, z, s);
-  if (tile == ANY_64) e = launch_mat_any<64, 64, 2, 2, ACOL, BCOL, EPI>(p, z, s);
-  if (tile == ANY_32) e = launch_mat_any<32, 128, 1, 4, ACOL, BCOL, EPI>(p, z, s);
+  if (tile == ANY_128) e = launch_mat_any<128, 128, 2, 2, ACOL, BCOL, EPI>(p, s);
+  if (tile == ANY_64) e = launch_mat_any<64, 64, 2, 2, ACOL, BCOL, EPI>(p, s);
+  if (tile == ANY_32) e = launch_mat_any<32, 128, 1, 4, ACOL, BCOL, EPI>(p, s);
   if (e != hipSuccess || p.k_split == 1) return e;
   if constexpr (!EPI::RANGES) {
-    const int64_t threads = (int64_t)p.m * ((p.n + 7) / 8);
-    hipLaunchKernelGGL(matmul_finish<EPI>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, p);
+    const int bno = EPI::DUAL ? p.bn / 2 : p.bn;
+    const int64_t tiles = ((int64_t)p.m + p.bm - 1) / p.bm * (((int64_t)p.n + bno - 1) / bno) * p.zs;
+    hipLaunchKernelGGL(matmul_finish<EPI>, dim3((unsigned)(tiles - p.full), (p.bm * bno / 8 + 255) / 256), dim3(256), 0, s, p);
     e = hipGetLastError();
   }
   return e;
