@@ -27,13 +27,14 @@ struct Choice {
   size_t slab;               // bytes
 };
 
-// What a tile takes, in us: a K step of 32 where a CU is full of such tiles, and where it has one alone; its beginning and end; tiles to a CU.
+// What a tile takes, in us: a K step of 32 where it has a CU alone, and its share of one with others; its beginning and end; tiles to a CU.
+// The ring's small tiles are bound by what a CU takes in, 62 KB a us, with two on it as with one.
 struct Cost {
-  double step, alone, ends;
+  double alone, share, ends;
   int per_cu;
 };
-constexpr Cost kBf16[TILES] = {{0.69, 0.62, 14, 1}, {0.41, 0.265, 6, 2}, {0.30, 0.20, 5, 2}, {1.2, 1.0, 6, 2}, {0.70, 0.45, 5, 4}, {0.70, 0.45, 5, 2}};
-constexpr Cost kFp32[TILES] = {{0.69, 0.62, 14, 1}, {0.41, 0.265, 6, 2}, {0.30, 0.20, 5, 2}, {5.0, 4.0, 8, 2}, {3.3, 1.3, 6, 4}, {3.0, 1.6, 6, 2}};
+constexpr Cost kBf16[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {0.7, 0.7, 6, 2}, {0.4, 0.25, 5, 4}, {0.4, 0.3, 5, 2}};
+constexpr Cost kFp32[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {3.0, 2.6, 8, 2}, {1.2, 0.82, 6, 4}, {1.2, 0.9, 6, 2}};
 constexpr double kLaunch = 4, kBytesPerUs = 4.5e6;
 
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -57,12 +58,15 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
   const double copy_time = direct ? 0 : kLaunch + (double)copies * (planes == 3 ? 10.0 / 6 : 2) / kBytesPerUs;
   // the operands once, at the rate at which they arrive
   const double arrive = (double)(m * steps1 * 32 + cols * steps1 * 32) * (planes == 3 ? 4 : 2) / kBytesPerUs;
-  Choice best{ANY_64, 0, 1, false, 0};
+  // (the kernel for any operand loads 16 bytes at a time: operands that have not so many are copied too.  B may be up to 7 rows or K short of n and k)
+  const bool any = m * k >= 8 && std::max<int64_t>(n - 7, 1) * std::max<int64_t>(k - 7, 1) >= 8;
+  Choice best{RING_128, 0, 1, !direct, 0};
   double best_cost = 1e300;
   for (int t = RING_256; t <= (direct ? RING_64 : ANY_32); ++t) {
     const bool ring = t <= RING_64;
     if (sh.a_columns && t == RING_64) continue;
-    if (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && !(sh.a_columns && forced_tile == RING_64) && !(direct && forced_tile > RING_64)) continue;
+    if (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && (any || forced_tile <= RING_64) && !(sh.a_columns && forced_tile == RING_64) && !(direct && forced_tile > RING_64)) continue;
+    if (!ring && !any) continue;
     const size_t room = ring ? copies : 0;
     if (room > workspace) continue;
     const int64_t steps = steps1 * (ring && planes == 3 ? PAIRS : 1);
@@ -75,8 +79,10 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
       if (split > 1 && forced_split < 1 && (steps / split < 6 || rest * (split - 1) >= slots)) break;
       if (forced_split >= 1 && split != forced_split && sh.splits && rest > 0) continue;
       const double part = (double)((steps + split - 1) / split);
-      double cost = kLaunch + (double)(full / slots) * (steps * c.step + c.ends);
-      for (int64_t left = rest * split; left > 0; left -= slots) cost += part * (left <= CUS ? c.alone : c.step) + c.ends;
+      auto round = [&](double steps_of, int64_t on_a_cu) { return steps_of * std::max(c.alone, c.share * on_a_cu) + c.ends; };
+      double cost = kLaunch + (double)(full / slots) * round((double)steps, c.per_cu);
+      const int64_t parts = rest * split;
+      cost += (double)(parts / slots) * round(part, c.per_cu) + (parts % slots ? round(part, (parts % slots + CUS - 1) / CUS) : 0);
       cost = std::max(cost, kLaunch + arrive);
       if (ring) cost += copy_time;
       if (split > 1) cost += kLaunch + (double)slab * 2 / kBytesPerUs;

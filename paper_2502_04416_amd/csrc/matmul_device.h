@@ -679,18 +679,30 @@ struct Any {
   static constexpr int elems(bool columns, int size) { return columns ? K * pitch(size) : size * ROW; }
 };
 
+// A chunk's 16 bytes, loaded from where they all lie in the operand (which has at least that many), up to E - 1 elements before the chunk's
+// place at the operand's end; and what of it counts, moved into place.  The loads have no branch around them: one would wait for each.
 template <typename T>
 struct Chunk {
-  T v[Any<T>::E];
+  uint32_t w[4];
 };
 template <typename T>
-__device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
-  constexpr int E = Any<T>::E;
-  if (n >= E) return __builtin_bit_cast(Chunk<T>, *reinterpret_cast<const Bytes16<T>*>(p));
-  Chunk<T> c;
+__device__ __forceinline__ void keep(Chunk<T>& c, int shift, int n) {
+  if constexpr (sizeof(T) == 4) {
+    if (shift & 2) c.w[0] = c.w[2], c.w[1] = c.w[3];
+    if (shift & 1) c.w[0] = c.w[1], c.w[1] = c.w[2], c.w[2] = c.w[3];
 #pragma unroll
-  for (int e = 0; e < E; ++e) c.v[e] = e < n ? p[e] : (T)0;
-  return c;
+    for (int e = 0; e < 4; ++e) c.w[e] = e < n ? c.w[e] : 0;
+  } else {
+    if (shift & 4) c.w[0] = c.w[2], c.w[1] = c.w[3];
+    if (shift & 2) c.w[0] = c.w[1], c.w[1] = c.w[2], c.w[2] = c.w[3];
+    if (shift & 1) {
+#pragma unroll
+      for (int e = 0; e < 3; ++e) c.w[e] = c.w[e] >> 16 | c.w[e + 1] << 16;
+      c.w[3] >>= 16;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c.w[e] = n >= 2 * e + 2 ? c.w[e] : n == 2 * e + 1 ? c.w[e] & 0xffffu : 0;
+  }
 }
 
 template <typename T, int BM, int BN, int WGM, int WGN, bool ACOL, bool BCOL>
@@ -724,53 +736,67 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
   const int per = at.slot < 0 ? all : (all + p.k_split - 1) / p.k_split;
   const int k_begin = min(at.part * per, all), k_end = min(k_begin + per, all);
 
+  static_assert(!EPI::DUAL || BN * KC / 2 % NT == 0, "a thread's chunk is of one of the two");
   Chunk<T> ra[2][A_N], rb[2][B_N];
-  // chunk c of a step: by columns K row c / (size / E) and E columns of it, by rows row c / KC and E of its K
-  auto fetch = [&](auto col_tag, int c, int size, const T* base, int64_t ld, int first, int there, int k_there, int k0) {
-    Chunk<T> out = {};
-    if constexpr (decltype(col_tag)::value) {
-      const int k = k0 + c / (size / E), col = first + c % (size / E) * E;
-      if (k < k_there && col < there) out = load_chunk<T>(base + (int64_t)k * ld + col, there - col);
-    } else {
-      const int row = first + c / KC, k = k0 + c % KC * E;
-      if (row < there && k < k_there) out = load_chunk<T>(base + (int64_t)row * ld + k, k_there - k);
-    }
-    return out;
+  // An operand's step: by columns its chunk c is K row c / (size / E) and E columns of it, by rows row c / KC and E of its K.  `off`: the
+  // chunk from the step's place on; `last`: where the operand's last 16 bytes begin from there (before it, where a step ends with the operand).
+  struct Place {
+    int64_t at;
+    int last;
+  };
+  auto place_of = [&](auto col_tag, int64_t ld, int first, int there, int k_there, int k0) {
+    constexpr bool COL = decltype(col_tag)::value;
+    const int64_t at = COL ? k0 * ld + first : first * ld + k0, total = COL ? (k_there - 1) * ld + there : (there - 1) * ld + k_there;
+    return Place{at, (int)min(total - E - at, (int64_t)0x3fffffff)};
+  };
+  auto off_of = [&](auto col_tag, int c, int size, int64_t ld) {
+    return decltype(col_tag)::value ? c / (size / E) * (int)ld + c % (size / E) * E : c / KC * (int)ld + c % KC * E;
+  };
+  auto fetch = [&](const T* base, int off, const Place& at) {
+    const Bytes16<T> b = *reinterpret_cast<const Bytes16<T>*>(base + at.at + min(off, at.last));
+    return Chunk<T>{{b.w[0], b.w[1], b.w[2], b.w[3]}};
+  };
+  auto k_of = [&](int s, bool* second) {
+    *second = EPI::SEGMENTS && s >= seg_steps;
+    return (*second ? s - seg_steps : s) * K;
   };
   auto load = [&](int s, int set) {
     if (s >= k_end) return;
-    const bool second = EPI::SEGMENTS && s >= seg_steps;
-    const int k0 = (second ? s - seg_steps : s) * K;
+    bool second;
+    const int k0 = k_of(s, &second);
     const T* a = static_cast<const T*>(second ? p.a2 : p.a);
     const T* b = static_cast<const T*>(second || (EPI::PAIRED && z) ? p.b2 : p.b);
+    const Place pa = place_of(std::bool_constant<ACOL>{}, p.lda, row_first, p.m_a, p.k, k0), pb = place_of(std::bool_constant<BCOL>{}, p.ldb, col_first, p.n_b, p.k_b, k0);
 #pragma unroll
-    for (int i = 0; i < A_N; ++i) ra[set][i] = fetch(std::bool_constant<ACOL>{}, tid + i * NT, BM, a, p.lda, row_first, p.m_a, p.k, k0);
+    for (int i = 0; i < A_N; ++i) ra[set][i] = fetch(a, off_of(std::bool_constant<ACOL>{}, tid + i * NT, BM, p.lda), pa);
 #pragma unroll
     for (int i = 0; i < B_N; ++i) {
-      int c = tid + i * NT;
-      const T* from = b;
-      // DUAL: the first half of the chunks from B, the second from B2, the same columns of both
-      if (EPI::DUAL && c >= BN * KC / 2) {
-        c -= BN * KC / 2;
-        from = static_cast<const T*>(p.b2);
-      }
-      rb[set][i] = fetch(std::bool_constant<BCOL>{}, c, BNO, from, p.ldb, col_first, p.n_b, p.k_b, k0);
+      const bool up = EPI::DUAL && i * NT >= BN * KC / 2;    // DUAL: the first half of the chunks from B, the second from B2, the same columns of both
+      rb[set][i] = fetch(up ? static_cast<const T*>(p.b2) : b, off_of(std::bool_constant<BCOL>{}, tid + (up ? i * NT - BN * KC / 2 : i * NT), BNO, p.ldb), pb);
     }
   };
-  auto place = [&](auto col_tag, const Chunk<T>& v, int c, int size, int pitch, T* to) {
-    to += decltype(col_tag)::value ? c / (size / E) * pitch + c % (size / E) * E : c / KC * S::ROW + c % KC * E;
-    *reinterpret_cast<Chunk<T>*>(__builtin_assume_aligned(to, 16)) = v;
+  auto place = [&](auto col_tag, Chunk<T> v, int c, int size, int pitch, int64_t ld, const Place& at, int left, int k_left, T* to) {
+    constexpr bool COL = decltype(col_tag)::value;
+    const int r = COL ? c / (size / E) : c / KC, e = COL ? c % (size / E) * E : c % KC * E;
+    if (left < size || k_left < K) {                         // (uniform) the step reaches past the operand: what of the chunk counts
+      const int off = r * (int)ld + e;
+      keep(v, max(off - at.last, 0), r < (COL ? k_left : left) ? (COL ? left : k_left) - e : 0);
+    }
+    *reinterpret_cast<Chunk<T>*>(__builtin_assume_aligned(to + (COL ? r * pitch + e : r * S::ROW + e), 16)) = v;
   };
-  auto store = [&](int buf, int set) {
+  auto store = [&](int s, int buf, int set) {
     T* ta = tiles + buf * STAGE;
     T* tb = ta + A_ELEMS;
+    bool second;
+    const int k0 = k_of(s, &second);
+    const Place pa = place_of(std::bool_constant<ACOL>{}, p.lda, row_first, p.m_a, p.k, k0), pb = place_of(std::bool_constant<BCOL>{}, p.ldb, col_first, p.n_b, p.k_b, k0);
 #pragma unroll
-    for (int i = 0; i < A_N; ++i) place(std::bool_constant<ACOL>{}, ra[set][i], tid + i * NT, BM, S::pitch(BM), ta);
+    for (int i = 0; i < A_N; ++i) place(std::bool_constant<ACOL>{}, ra[set][i], tid + i * NT, BM, S::pitch(BM), p.lda, pa, p.m_a - row_first, p.k - k0, ta);
 #pragma unroll
     for (int i = 0; i < B_N; ++i) {
-      const int c = tid + i * NT;
-      const bool up = EPI::DUAL && c >= BN * KC / 2;
-      place(std::bool_constant<BCOL>{}, rb[set][i], up ? c - BN * KC / 2 : c, BNO, S::pitch(BN), up ? tb + (BCOL ? BNO : BNO * S::ROW) : tb);
+      const bool up = EPI::DUAL && i * NT >= BN * KC / 2;
+      place(std::bool_constant<BCOL>{}, rb[set][i], tid + (up ? i * NT - BN * KC / 2 : i * NT), BNO, S::pitch(BN), p.ldb, pb, p.n_b - col_first, p.k_b - k0,
+            up ? tb + (BCOL ? BNO : BNO * S::ROW) : tb);
     }
   };
   auto b_first = [&](int nb) {                               // first column, in the tile, of a wave's block
@@ -834,12 +860,12 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
   load(k_begin, 0);
   load(k_begin + 1, 1);
   for (int s = k_begin; s < k_end; s += 2) {
-    store(0, 0);
+    store(s, 0, 0);
     __syncthreads();                                         // (a buffer's reads lie before the barrier of the step between)
     load(s + 2, 0);
     multiply(0);
     if (s + 1 < k_end) {
-      store(1, 1);
+      store(s + 1, 1, 1);
       __syncthreads();
       load(s + 3, 1);
       multiply(1);
