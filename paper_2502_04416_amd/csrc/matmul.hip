@@ -65,7 +65,9 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
   for (int t = RING_256; t <= (direct ? RING_64 : ANY_32); ++t) {
     const bool ring = t <= RING_64;
     if (sh.a_columns && t == RING_64) continue;
-    if (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && (any || forced_tile <= RING_64) && !(sh.a_columns && forced_tile == RING_64) && !(direct && forced_tile > RING_64)) continue;
+    if (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && (any || forced_tile <= RING_64) && !(sh.a_columns && forced_tile == RING_64) &&
+        !(direct && forced_tile > RING_64))
+      continue;
     if (!ring && !any) continue;
     const size_t room = ring ? copies : 0;
     if (room > workspace) continue;

@@ -517,8 +517,12 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   }
   const bool k_past = (seg_steps - 1) * BK + coff >= p.k;    // of a part's last step, by rows
 
-  // The step that is fetched next: part of K, step in it, and where its operands lie.
-  int f_left = KT, f_seg = SEGS > 1 && seg_steps > 0 ? k_begin / seg_steps : 0, f_step = k_begin - f_seg * seg_steps;
+  // The step that is fetched next: part of K, step in it, and where its operands lie.  Where a tile's rows are all there is, the columns' tiles
+  // share nothing, and each begins K at a place of its own: rows of B a power of two apart would otherwise ask the same few channels of the
+  // memory at the same time.
+  constexpr bool TURNS = !ACOL && !BCOL && SEGS == 1;
+  const int turn = TURNS && p.m <= BM && KT > 0 ? at.nt * 5 % KT : 0;
+  int f_left = KT, f_seg = SEGS > 1 && seg_steps > 0 ? k_begin / seg_steps : 0, f_step = k_begin - f_seg * seg_steps + turn;
   const bf16_t *f_a, *f_b, *f_b2 = nullptr;
   auto place_of = [&]() {
     const int part = EPI::SEGMENTS ? f_seg / (SEGS / 2) : 0, pair = f_seg - part * (EPI::SEGMENTS ? SEGS / 2 : 0);
@@ -536,6 +540,9 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
     if (++f_step == seg_steps && SEGS > 1) {
       f_step = 0;
       f_seg = f_seg + 1 < SEGS ? f_seg + 1 : 0;              // (behind the last part nothing is read)
+      place_of();
+    } else if (TURNS && f_step == k_begin + KT) {
+      f_step = k_begin;
       place_of();
     } else {
       f_a += ACOL ? BK * p.lda : BK;
@@ -594,7 +601,7 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
       if constexpr (!BCOL) wf[set][f] = *reinterpret_cast<const bf16x8_t*>(st + A_ELEMS + (wn * NB + f) * BLK + frag);
       else if constexpr (EPI::DUAL) {
         const int which = f / (NB / 2), c = f % (NB / 2);    // panel of the wave's column block, in gate / up pairs
-        wf[set][f] = read_turned2(st + A_ELEMS + ((wn * (NB / 2)) / 4 * 2 + which) * 2048 + turned[c], 4 * 64);
+        wf[set][f] = read_turned2(st + A_ELEMS + ((wn * (NB / 2) / 4 + c / 4) * 2 + which) * 2048 + turned[c % 4], 4 * 64);
       } else wf[set][f] = read_turned2(st + A_ELEMS + (wn * (NB / 4) + f / 4) * 2048 + turned[f % 4], 4 * 64);
     } else {
       const int q = f - NB;
@@ -602,7 +609,7 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
       else af[set][q] = read_turned2(st + (wm * (MB / 4) + q / 4) * 2048 + turned_a[q % 4], 4 * 64);
     }
   };
-  static_assert(!EPI::DUAL || NB / 2 <= 4, "a wave's gate columns lie in one panel");
+  static_assert(!EPI::DUAL || NB / 2 == 2 || NB / 2 % 4 == 0, "a wave's gate columns are whole panels, or half of one");
 
   constexpr int NM = MB * NB, NF = MB + NB, ND = LPT;
   static_assert(ND <= NM, "at most one load instruction after an MFMA");
