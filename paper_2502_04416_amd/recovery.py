@@ -4,8 +4,8 @@ A block is what a transformer has there:
 
     out = norm(residual + drop(ffn(x) + adapters(drop(x)))) * weight
 
-`Block.step` trains the adapters and the norm's weight towards given outputs, by the package's own forward and backward operators; the
-feed-forward layer is frozen.  `Block.serve` runs the block for a batch of requests, each token with an adapter of the bank or none.
+`Block.step` trains the adapters and the norm's weight towards given outputs, `Block.step_tokens` towards given tokens under a head, by the
+package's own forward and backward operators; the feed-forward layer is frozen (finetune.Dense trains it before it is restructured).  `Block.serve` runs the block for a batch of requests, each token with an adapter of the bank or none.
 
     python -m paper_2502_04416_amd.recovery        # on an MI355X: a small layer, the distance to its dense form before and after
 """
@@ -54,27 +54,50 @@ class Block:
         binding.norm_forward(z, out, self.weight, form=self.form, eps=self.eps, residual=residual, sum_out=z)
         return out, z
 
-    def gradients(self, x, residual, target, ids=None):
-        """(mean squared distance of the block's outputs to the target, gradients of a, b and weight)."""
+    def _forward(self, x, residual, ids):
+        """(out, what the backward pass needs)."""
         import torch
-        t, d = x.shape
+        t = x.shape[0]
         f32 = dict(dtype=torch.float32, device="cuda")
         before, after = (binding.Dropout(self.p, self.seed, 2 * self.steps + i) for i in (0, 1))
-        z, s, out, dz = (torch.empty_like(x) for _ in range(4))
+        z, s, out = (torch.empty_like(x) for _ in range(3))
         u, mean, rstd = torch.empty(t, self.a.shape[1], **f32), torch.empty(t, **f32), torch.empty(t, **f32)
         self.layer.forward_device(x, z)
         binding.adapters_forward(x, z, self.a, self.b, self.scale, ids=ids, base=z, dropout=before, u=u)
         binding.norm_forward(z, out, self.weight, form=self.form, eps=self.eps, residual=residual, dropout=after, sum_out=s, mean=mean, rstd=rstd)
-        off = out.float() - target.float()
-        dy = (off * (2.0 / off.numel())).to(self.dtype)
-        grads = {k: torch.empty_like(v) for k, v in self.params.items()}
+        return out, (x, ids, s, u, mean, rstd, before, after)
+
+    def _backward(self, dy, saved):
+        """Gradients of a, b and weight from that of the outputs."""
+        import torch
+        x, ids, s, u, mean, rstd, before, after = saved
+        grads, dz = {k: torch.empty_like(v) for k, v in self.params.items()}, torch.empty_like(x)
         binding.norm_backward(dy, s, dz, mean, rstd, self.weight, form=self.form, dropout=after, dweight=grads["weight"])
         binding.adapters_backward(dz, x, u, self.a, self.b, self.scale, ids=ids, dropout=before, da=grads["a"], db=grads["b"])
-        return (off * off).mean(), grads
+        return grads
 
-    def step(self, x, residual, target, ids=None, lr: float = 1e-3, betas=(0.9, 0.95)):
-        """One step of Adam; the loss before it (on the device)."""
-        loss, grads = self.gradients(x, residual, target, ids)
+    def gradients(self, x, residual, target, ids=None):
+        """(mean squared distance of the block's outputs to the target, gradients of a, b and weight)."""
+        out, saved = self._forward(x, residual, ids)
+        off = out.float() - target.float()
+        dy = (off * (2.0 / off.numel())).to(self.dtype)
+        return (off * off).mean(), self._backward(dy, saved)
+
+    def token_gradients(self, x, residual, targets, head, ids=None):
+        """(mean loss of the targets under a frozen finetune.Head on the block's outputs, gradients of a, b and weight).
+
+        targets: [tokens] int32, no loss where it is not in the vocabulary."""
+        out, saved = self._forward(x, residual, ids)
+        loss, dy, _ = head.loss(out, targets, train=False)
+        return loss, self._backward(dy, saved)
+
+    def _update(self, grads, lr, betas, max_norm):
+        """One step of Adam on gradients that are first clipped, together, to max_norm; their norm before it if they are."""
+        import torch
+        norm = None
+        if max_norm is not None:
+            norm = torch.empty(1, dtype=torch.float32, device="cuda")
+            binding.clip_gradients(list(grads.values()), norm, max_norm)
         self.steps += 1
         for k, g in grads.items():
             m, v = self.moments[k]
@@ -82,6 +105,18 @@ class Block:
             v.lerp_(g * g, 1 - betas[1])
             self.params[k] -= lr * (m / (1 - betas[0] ** self.steps)) / ((v / (1 - betas[1] ** self.steps)).sqrt() + 1e-12)
         self._cast()
+        return norm
+
+    def step(self, x, residual, target, ids=None, lr: float = 1e-3, betas=(0.9, 0.95), max_norm: Optional[float] = None):
+        """One step of Adam towards given outputs; the loss before it (on the device)."""
+        loss, grads = self.gradients(x, residual, target, ids)
+        self._update(grads, lr, betas, max_norm)
+        return loss
+
+    def step_tokens(self, x, residual, targets, head, ids=None, lr: float = 1e-3, betas=(0.9, 0.95), max_norm: Optional[float] = 1.0):
+        """One step of Adam towards given tokens; the loss before it (on the device)."""
+        loss, grads = self.token_gradients(x, residual, targets, head, ids)
+        self._update(grads, lr, betas, max_norm)
         return loss
 
 
