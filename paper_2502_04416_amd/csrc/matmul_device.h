@@ -29,11 +29,15 @@
 
 namespace cmoe {
 
-template <typename T> __device__ __forceinline__ float exp_of(float x);
-template <> __device__ __forceinline__ float exp_of<float>(float x) { return expf(x); }
-// The hardware exponential: the error, |x| 2^-24 relative, is far below the rounding to bf16 that follows.
-template <> __device__ __forceinline__ float exp_of<bf16_t>(float x) { return __expf(x); }
-template <typename T> __device__ __forceinline__ float sigmoid_of(float x) { return 1.0f / (1.0f + exp_of<T>(-x)); }
+constexpr float LOG2E = 1.44269504088896341f;
+// exp(x - from).  What is rounded to bf16, and sums of 2^-24 |x| relative error at most, take the hardware's power of two of one fused product.
+template <typename T> __device__ __forceinline__ float exp_from(float x, float from);
+template <> __device__ __forceinline__ float exp_from<float>(float x, float from) { return expf(x - from); }
+template <> __device__ __forceinline__ float exp_from<bf16_t>(float x, float from) { return __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -from * LOG2E)); }
+template <typename T> __device__ __forceinline__ float sigmoid_of(float x);
+template <> __device__ __forceinline__ float sigmoid_of<float>(float x) { return 1.0f / (1.0f + expf(-x)); }
+// (the hardware's reciprocal: one unit in the last place of fp32, and the result is rounded to bf16; a division is ten instructions)
+template <> __device__ __forceinline__ float sigmoid_of<bf16_t>(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-x * LOG2E)); }
 
 // ---- what happens to eight consecutive columns of a row of the result ---------------------------------------------
 // hold: what it reads of global memory for them (n of them exist); put: with v, and for DUAL w, the sums.
@@ -148,10 +152,18 @@ struct EpiDLogits {
   }
   static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&)[8], const Held& h) {
     const bool has = (unsigned)h.id < (unsigned)p.vocab;
+    const unsigned at = (unsigned)(h.id - p.col0 - col);     // of the target among the eight
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float d = exp_of<T>(v[e] - h.lse) - (h.id == p.col0 + col + e ? 1.0f : 0.0f);
-      v[e] = has && col + e < p.n_b ? d * h.weight : 0.0f;   // (columns behind the vocabulary are zeros)
+    for (int e = 0; e < 8; ++e) v[e] = exp_from<T>(v[e], h.lse);
+    if (at < 8u) {                                           // (few waves have one)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] -= at == (unsigned)e ? 1.0f : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = has ? v[e] * h.weight : 0.0f;
+    if (col + 8 > p.n_b) {                                   // columns behind the vocabulary are zeros
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = col + e < p.n_b ? v[e] : 0.0f;
     }
     store8(static_cast<T*>(p.c) + row * p.ldc + col, n, v);
   }
@@ -196,24 +208,29 @@ __device__ __forceinline__ float2 join_ranges(float2 a, float2 b) {
 }
 
 // Rows of a wave's tile, reduced over its columns where they are: a lane holds columns kq * 4 .. + 3 of every block of 16 in row r16.
-// A NaN among the logits makes the sum NaN (fmaxf passes it over).
-template <int MB, int NB>
-__device__ __forceinline__ void put_ranges(const MatArgs& p, const floatx4_t (&acc)[MB][NB], int64_t row0, int col0, int range) {
+// A NaN among the logits makes the sum NaN (fmaxf passes it over).  The vector units' time for this is a CU's own, nothing else runs beside it: whole
+// tiles look for no edge, and rows whose target is in other columns for no target.
+template <typename T, bool WHOLE, int MB, int NB>
+__device__ __forceinline__ void put_rows(const MatArgs& p, const floatx4_t (&acc)[MB][NB], int64_t row0, int col0, int range) {
   const int lane = threadIdx.x & 63, r16 = lane & 15, kq = lane >> 4;
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb) {
     const int64_t row = row0 + mb * 16 + r16;
-    const bool in = row < p.m;
+    const bool in = WHOLE || row < p.m;
     const int want = (int)((uint32_t)(in ? p.ids[row] : -1) - (uint32_t)(p.col0 + col0 + kq * 4));
+    if ((unsigned)want < (unsigned)(NB * 16)) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (want == nb * 16 + i && (WHOLE || col0 + nb * 16 + kq * 4 + i < p.n)) p.picked[row] = acc[mb][nb][i];
+    }
+    auto there = [&](int nb, int i) { return WHOLE || col0 + nb * 16 + kq * 4 + i < p.n; };
     float top = -INFINITY;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool there = col0 + nb * 16 + kq * 4 + i < p.n;
-        if (there) top = fmaxf(top, acc[mb][nb][i]);
-        if (there && want == nb * 16 + i) p.picked[row] = acc[mb][nb][i];
-      }
+      for (int i = 0; i < 4; ++i) top = there(nb, i) ? fmaxf(top, acc[mb][nb][i]) : top;
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     const float from = top == -INFINITY ? 0.0f : top;
@@ -222,13 +239,18 @@ __device__ __forceinline__ void put_ranges(const MatArgs& p, const floatx4_t (&a
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float e = __expf(acc[mb][nb][i] - from);
-        sum += col0 + nb * 16 + kq * 4 + i < p.n ? e : 0.0f;
+        const float e = exp_from<T>(acc[mb][nb][i], from);
+        sum += there(nb, i) ? e : 0.0f;
       }
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (in && kq == 0) p.part[(int64_t)range * p.m + row] = float2{top, sum};
   }
+}
+template <typename T, int MB, int NB>
+__device__ __forceinline__ void put_ranges(const MatArgs& p, const floatx4_t (&acc)[MB][NB], int64_t row0, int col0, int range) {
+  if (row0 + MB * 16 <= p.m && col0 + NB * 16 <= p.n) put_rows<T, true>(p, acc, row0, col0, range);
+  else put_rows<T, false>(p, acc, row0, col0, range);
 }
 
 // Which tile a workgroup has.  Workgroup b runs on XCD b % 8, each of which works through a run of the list, so that tiles that share
@@ -664,7 +686,7 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   wait_vmcnt<0>();                                           // (no load into LDS may outlive the workgroup)
   const int64_t row0 = row_first + wm * TM;
   if constexpr (EPI::RANGES) {
-    put_ranges<MB, NB>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
+    put_ranges<typename EPI::type>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
   } else {
     __syncthreads();                                         // every wave has left the ring
     put_tile<MB, NB, EPI>(p, acc, reinterpret_cast<float*>(smem) + wave * strip_floats<MB, NB>(), at, wm * TM, wn * (EPI::DUAL ? TN / 2 : TN), row0,
@@ -880,7 +902,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
   }
   const int64_t row0 = row_first + wm * TM;
   if constexpr (EPI::RANGES) {
-    put_ranges<MB, NB>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
+    put_ranges<typename EPI::type>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
   } else {
     __syncthreads();
     put_tile<MB, NB, EPI>(p, acc, reinterpret_cast<float*>(any_smem) + wave * strip_floats<MB, NB>(), at, wm * TM, wn * (EPI::DUAL ? TN / 2 : TN), row0,
