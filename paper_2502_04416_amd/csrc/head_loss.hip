@@ -30,10 +30,13 @@ int check_sizes(const char* what, int32_t dtype, int64_t tokens, int32_t d, int3
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
+// Whether both passes take their logits from operands where they are: of the sizes alone, so that they agree (see MatArgs::no_copies).
+bool logits_in_place(int dtype, int64_t t, int64_t d, int64_t vocab) { return !matmul_copies(PRODUCT_LSE, dtype, t, vocab, d); }
+
 // How many vocabulary entries a piece may have for the copies of their rows, where operands may be copied, to stay below 256 MB (up to a width of
 // 8192); all of them otherwise.
-int64_t copied_piece(Product kind, int dtype, int64_t t, int64_t d, int64_t vocab) {
-  if (!matmul_copies(kind, dtype, t, vocab, d)) return vocab;
+int64_t copied_piece(int dtype, int64_t t, int64_t d, int64_t vocab) {
+  if (logits_in_place(dtype, t, d, vocab)) return vocab;
   return std::min(vocab, std::max<int64_t>(4096, ((int64_t)1 << (dtype == CMOE_F32 ? 25 : 27)) / d / 256 * 256));
 }
 
@@ -41,13 +44,14 @@ struct ForwardSpace {
   int64_t piece, last;                     // entries of a piece, and of the last one
   size_t picked, product, total;           // offsets of the targets' logits and of the products' workspace; the ranges at 0
   ForwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
-    piece = copied_piece(PRODUCT_LSE, dtype, t, d, vocab);
+    piece = copied_piece(dtype, t, d, vocab);
+    const bool in_place = logits_in_place(dtype, t, d, vocab);
     const int64_t pieces = (vocab - 1) / piece;              // but the last
     last = vocab - pieces * piece;
-    const int64_t ranges = pieces * lse_ranges(dtype, t, piece, d) + lse_ranges(dtype, t, last, d);
+    const int64_t ranges = pieces * lse_ranges(dtype, t, piece, d, in_place) + lse_ranges(dtype, t, last, d, in_place);
     picked = round16((size_t)ranges * t * sizeof(float2));
     product = picked + round16((size_t)t * 4);
-    total = product + std::max(matmul_workspace_bytes(PRODUCT_LSE, dtype, t, piece, d), matmul_workspace_bytes(PRODUCT_LSE, dtype, t, last, d));
+    total = product + std::max(matmul_workspace_bytes(PRODUCT_LSE, dtype, t, piece, d, in_place), matmul_workspace_bytes(PRODUCT_LSE, dtype, t, last, d, in_place));
   }
 };
 
@@ -56,7 +60,7 @@ struct BackwardSpace {
   size_t acc, product, total;              // offsets of dX's sums and of the products' workspace; dZ at 0
   BackwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
     piece = std::max(PIECE_LEAST, PIECE_BYTES / (int64_t)elem_size(dtype) / std::max<int64_t>(t, 1) / 256 * 256);
-    piece = std::min(piece, copied_piece(PRODUCT_DLOGITS, dtype, t, d, vocab));
+    piece = std::min(piece, copied_piece(dtype, t, d, vocab));
     ld = (piece + 7) / 8 * 8;
     acc = round16((size_t)t * ld * elem_size(dtype));
     product = acc + (piece < vocab ? round16((size_t)t * d * 4) : 0);
@@ -64,7 +68,7 @@ struct BackwardSpace {
     const int64_t last = vocab - (vocab - 1) / piece * piece;
     for (int64_t w : {piece, last}) {
       const int64_t padded = (w + 7) / 8 * 8;
-      most = std::max({most, matmul_workspace_bytes(PRODUCT_DLOGITS, dtype, t, padded, d), matmul_workspace_bytes(PRODUCT_DHEAD, dtype, t, d, padded),
+      most = std::max({most, matmul_workspace_bytes(PRODUCT_DLOGITS, dtype, t, padded, d, logits_in_place(dtype, t, d, vocab)), matmul_workspace_bytes(PRODUCT_DHEAD, dtype, t, d, padded),
                        matmul_workspace_bytes(PRODUCT_DW, dtype, w, d, t)});
     }
     total = product + most;
@@ -90,9 +94,10 @@ __global__ __launch_bounds__(256) void head_finish(const float2* part, int range
     if (g < half) joined[threadIdx.x] = mine = join_ranges(mine, joined[threadIdx.x + half * ROWS]);
   }
   if (g == 0 && row < tokens) {
-    const float l = mine.x + logf(mine.y);
-    if (lse) lse[row] = l;
-    if (loss) loss[row] = (uint32_t)ids[row] < (uint32_t)vocab ? l - picked[row] : 0.0f;
+    const float rest = logf(mine.y);
+    if (lse) lse[row] = mine.x + rest;
+    // (not lse - picked: a target that is nearly certain has a loss far below the rounding of lse)
+    if (loss) loss[row] = (uint32_t)ids[row] < (uint32_t)vocab ? (mine.x - picked[row]) + rest : 0.0f;
   }
 }
 
@@ -138,6 +143,7 @@ extern "C" int cmoe_head_loss_forward(const cmoe_head_loss_forward_args* args, v
     p.a = a.x, p.lda = a.d, p.b = static_cast<const char*>(a.weight) + (size_t)first * a.d * es, p.ldb = a.d;
     p.m = (int)a.tokens, p.n = (int)std::min(ws.piece, a.vocab - first), p.k = a.d;
     p.ids = a.ids, p.vocab = a.vocab, p.col0 = (int)first;
+    p.no_copies = logits_in_place(a.dtype, a.tokens, a.d, a.vocab);
     p.part = part + (size_t)ranges * a.tokens, p.picked = picked;
     int more = 0;
     if (hipError_t e = matmul(PRODUCT_LSE, a.dtype, p, base + ws.product, ws.total - ws.product, s, &more)) return launched(what, e);
@@ -192,6 +198,7 @@ extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args,
     p.m = (int)a.tokens, p.n = padded, p.n_b = n, p.k = a.d;
     p.c = base, p.ldc = ws.ld;
     p.ids = a.ids, p.vocab = a.vocab, p.col0 = (int)first, p.lse = a.lse, p.dloss = a.dloss;
+    p.no_copies = logits_in_place(a.dtype, a.tokens, a.d, a.vocab);
     if (hipError_t e = matmul(PRODUCT_DLOGITS, a.dtype, p, room, room_bytes, s)) return launched(what, e);
     if (a.dx) {
       MatArgs q = {};

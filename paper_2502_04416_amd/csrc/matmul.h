@@ -39,6 +39,9 @@ struct MatArgs {
   const int32_t* ids;        // [m]
   const float* lse;          // [m]
   const float* dloss;        // [m] or null
+  // PRODUCT_LSE and PRODUCT_DLOGITS have to agree to the bit: 1 - p of a likely target is a difference of both.  The ring's tiles sum in one
+  // order, those for any operand in another: both passes say which, for operands that the ring cannot read where they are.
+  bool no_copies;
   float2* part;              // [column ranges][m]
   float* picked;             // [m]
   // Tiles are numbered over both results (zs of them); from tile `full` on, each is split into k_split parts of K, whose sums go to slab
@@ -48,11 +51,11 @@ struct MatArgs {
 };
 
 // Bytes of workspace, for copies of operands and slabs of a K split, that a product may ask for, whatever its operands' alignment.
-size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k);
+size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k, bool no_copies = false);
 // Whether the product of operands that the ring cannot read where they are copies them.
 bool matmul_copies(Product kind, int dtype, int64_t m, int64_t n, int64_t k);
 // Column ranges that PRODUCT_LSE may write: rows of `part`, whatever its operands' alignment.
-int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k);
+int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k, bool no_copies);
 // Enqueues the product; m_a, n_b and k_b count as m, n and k where they are 0.  Workspace: 16-byte aligned.  *ranges, of PRODUCT_LSE: how many
 // ranges have been written.
 hipError_t matmul(Product kind, int dtype, MatArgs p, void* workspace, size_t workspace_bytes, hipStream_t s, int* ranges = nullptr);

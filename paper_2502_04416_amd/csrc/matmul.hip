@@ -17,7 +17,7 @@ struct Shape {
 };
 constexpr Shape shape_of(Product kind) {
   return {kind == PRODUCT_DW, kind == PRODUCT_GATED || kind == PRODUCT_DOWN || kind == PRODUCT_DW || kind == PRODUCT_DHEAD, kind == PRODUCT_GATED,
-          kind == PRODUCT_DX, kind != PRODUCT_LSE};
+          kind == PRODUCT_DX, kind != PRODUCT_LSE && kind != PRODUCT_DLOGITS};
 }
 
 struct Choice {
@@ -33,8 +33,8 @@ struct Cost {
   double alone, share, ends;
   int per_cu;
 };
-constexpr Cost kBf16[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {0.7, 0.7, 6, 2}, {0.4, 0.25, 5, 4}, {0.4, 0.3, 5, 2}};
-constexpr Cost kFp32[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {3.0, 2.6, 8, 2}, {1.2, 0.82, 6, 4}, {1.2, 0.9, 6, 2}};
+constexpr Cost kBf16[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {0.4, 0.25, 5, 4}, {0.4, 0.3, 5, 2}};
+constexpr Cost kFp32[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {1.2, 0.82, 6, 4}, {1.2, 0.9, 6, 2}};
 constexpr double kLaunch = 4, kBytesPerUs = 4.5e6;
 
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -46,9 +46,10 @@ size_t copy_bytes(const Shape& sh, int planes, int64_t m, int64_t n, int64_t k, 
   return ((size_t)(a + b) * planes * 2 + 255) / 256 * 256;
 }
 
-// direct: bf16 operands that the ring can read where they are.  second: there is a second B.
+// direct: bf16 operands that the ring can read where they are.  second: there is a second B.  logits: of logits of other operands, 1 on the kernel for any,
+// 0 on the ring, where that is settled.
 // The tiles that fill the chip a whole number of times are left whole; the rest, if that is shorter, is split.
-Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace) {
+Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace, int logits = -1) {
   const Shape sh = shape_of(kind);
   const int pair = kind == PRODUCT_DW && second ? 2 : 1, planes = dtype == CMOE_F32 ? 3 : 1;
   const int64_t steps1 = ((k + 31) / 32) * (sh.segments ? 2 : 1);
@@ -69,6 +70,9 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
         !(direct && forced_tile > RING_64))
       continue;
     if (!ring && !any) continue;
+    // logits have the bits of one order of sums in both passes: see MatArgs::no_copies
+    if (logits >= 0 && !direct && any && ring == (logits == 1)) continue;
+    if ((kind == PRODUCT_LSE || kind == PRODUCT_DLOGITS) && t == RING_256 && m <= FEW_ROWS) continue;
     const size_t room = ring ? copies : 0;
     if (room > workspace) continue;
     const int64_t steps = steps1 * (ring && planes == 3 ? PAIRS : 1);
@@ -108,9 +112,9 @@ hipError_t prepare(const CopyArgs& args, uint32_t groups, hipStream_t s) {
 
 }  // namespace
 
-int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k) {
+int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k, bool no_copies) {
   int64_t most = 0;
-  for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct) most = std::max(most, ranges_of(choose(PRODUCT_LSE, dtype, direct, false, m, n, k, EVERYTHING), n));
+  for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct) most = std::max(most, ranges_of(choose(PRODUCT_LSE, dtype, direct, false, m, n, k, EVERYTHING, no_copies), n));
   return most;
 }
 
@@ -118,13 +122,14 @@ bool matmul_copies(Product kind, int dtype, int64_t m, int64_t n, int64_t k) {
   return choose(kind, dtype, false, has_second(kind), m, n, k, EVERYTHING).copies;
 }
 
-size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k) {
+size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k, bool no_copies) {
+  const int logits = kind == PRODUCT_LSE || kind == PRODUCT_DLOGITS ? no_copies : -1;
   if (m <= 0 || n <= 0) return 0;
   const Shape sh = shape_of(kind);
   size_t most = 0;
   for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct)
     for (int second = has_second(kind); second <= (has_second(kind) || kind == PRODUCT_DW); ++second) {
-      const Choice c = choose(kind, dtype, direct, second, m, n, k, EVERYTHING);
+      const Choice c = choose(kind, dtype, direct, second, m, n, k, EVERYTHING, logits);
       most = std::max(most, (c.copies ? copy_bytes(sh, dtype == CMOE_F32 ? 3 : 1, m, n, k, second) : 0) + c.slab);
     }
   return (most + 15) / 16 * 16;
@@ -140,7 +145,8 @@ hipError_t matmul(Product kind, int dtype, MatArgs p, void* workspace, size_t wo
   auto wide = [](const void* q) { return ((uintptr_t)q & 15) == 0; };
   const bool direct = dtype == CMOE_BF16 && wide(p.a) && wide(p.a2) && wide(p.b) && wide(p.b2) && p.lda % 8 == 0 && p.ldb % 8 == 0 &&
                       (sh.a_columns ? p.m_a : p.k) % 8 == 0 && (sh.b_columns ? p.n_b : p.k) % 8 == 0;
-  const Choice c = choose(kind, dtype, direct, second, p.m, p.n, p.k, workspace ? workspace_bytes : 0);
+  const Choice c = choose(kind, dtype, direct, second, p.m, p.n, p.k, workspace ? workspace_bytes : 0,
+                          kind == PRODUCT_LSE || kind == PRODUCT_DLOGITS ? p.no_copies : -1);
   p.zs = kind == PRODUCT_DW && second ? 2 : 1;
   p.full = c.full, p.k_split = c.k_split, p.bm = kTiles[c.tile].bm, p.bn = kTiles[c.tile].bn;
   char* room = static_cast<char*>(workspace);

@@ -30,10 +30,11 @@
 namespace cmoe {
 
 constexpr float LOG2E = 1.44269504088896341f;
-// exp(x - from).  What is rounded to bf16, and sums of 2^-24 |x| relative error at most, take the hardware's power of two of one fused product.
+// exp(x - from), 1 where they are equal: the difference is taken first, or the product's rounding would be an error of every exponential of a row.
 template <typename T> __device__ __forceinline__ float exp_from(float x, float from);
 template <> __device__ __forceinline__ float exp_from<float>(float x, float from) { return expf(x - from); }
-template <> __device__ __forceinline__ float exp_from<bf16_t>(float x, float from) { return __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -from * LOG2E)); }
+// (the hardware's power of two: 2^-24 |x - from| relative)
+template <> __device__ __forceinline__ float exp_from<bf16_t>(float x, float from) { return __builtin_amdgcn_exp2f((x - from) * LOG2E); }
 template <typename T> __device__ __forceinline__ float sigmoid_of(float x);
 template <> __device__ __forceinline__ float sigmoid_of<float>(float x) { return 1.0f / (1.0f + expf(-x)); }
 // (the hardware's reciprocal: one unit in the last place of fp32, and the result is rounded to bf16; a division is ten instructions)
@@ -71,7 +72,7 @@ __device__ __forceinline__ float held(const Raw8<T>& r, int e) {
 
 template <typename T, bool SEGS, bool PAIR>
 struct EpiStore {                                             // PRODUCT_DOWN, PRODUCT_DX, PRODUCT_DW
-  static constexpr bool DUAL = false, SEGMENTS = SEGS, PAIRED = PAIR, RANGES = false;
+  static constexpr bool LOGITS = false, DUAL = false, SEGMENTS = SEGS, PAIRED = PAIR, RANGES = false;
   typedef T type;
   struct Held {
     Raw8<T> base;
@@ -95,7 +96,7 @@ struct HeldNothing {};
 
 template <typename T>
 struct EpiGated {
-  static constexpr bool DUAL = true, SEGMENTS = false, PAIRED = false, RANGES = false;
+  static constexpr bool LOGITS = false, DUAL = true, SEGMENTS = false, PAIRED = false, RANGES = false;
   typedef T type;
   typedef HeldNothing Held;
   static __device__ __forceinline__ void hold(const MatArgs&, int64_t, int, int, Held&) {}
@@ -113,7 +114,7 @@ struct EpiGated {
 
 template <typename T>
 struct EpiDGated {
-  static constexpr bool DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
+  static constexpr bool LOGITS = false, DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
   typedef T type;
   struct Held {
     Raw8<T> gate, up;
@@ -139,7 +140,7 @@ struct EpiDGated {
 
 template <typename T>
 struct EpiDLogits {
-  static constexpr bool DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
+  static constexpr bool LOGITS = true, DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
   typedef T type;
   struct Held {
     int id;
@@ -171,7 +172,7 @@ struct EpiDLogits {
 
 template <typename T>
 struct EpiDHead {
-  static constexpr bool DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
+  static constexpr bool LOGITS = false, DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = false;
   typedef T type;
   struct Held {
     Raw8<float> before;
@@ -196,7 +197,7 @@ struct EpiDHead {
 
 template <typename T>
 struct EpiLse {
-  static constexpr bool DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = true;
+  static constexpr bool LOGITS = true, DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = true;
   typedef T type;
 };
 
@@ -486,6 +487,8 @@ constexpr size_t mat_ring_bytes() {
   return ring > strips ? ring : strips;
 }
 
+constexpr int FEW_ROWS = 64;                                 // whose products are bound by the other operand's way out of memory
+
 // The pairs of planes of two fp32 operands whose products count, smallest first: plane of A and of B, two bits each.
 constexpr int PAIRS = 6, PAIRS_A = 0 | 1 << 2 | 2 << 4 | 0 << 6 | 1 << 8 | 0 << 10, PAIRS_B = 2 | 1 << 2 | 0 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
 
@@ -539,11 +542,11 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   }
   const bool k_past = (seg_steps - 1) * BK + coff >= p.k;    // of a part's last step, by rows
 
-  // The step that is fetched next: part of K, step in it, and where its operands lie.  Where a tile's rows are all there is, the columns' tiles
-  // share nothing, and each begins K at a place of its own: rows of B a power of two apart would otherwise ask the same few channels of the
-  // memory at the same time.
+  // The step that is fetched next: part of K, step in it, and where its operands lie.  Where there are few rows the columns' tiles share
+  // next to nothing, and each 256 columns begin K at a place of their own: rows of B a power of two apart would otherwise ask the same few
+  // channels of the memory at the same time.  (By the column and not the tile: a logit has the same bits in the forward and in the backward pass.)
   constexpr bool TURNS = !ACOL && !BCOL && SEGS == 1;
-  const int turn = TURNS && p.m <= BM && KT > 0 ? at.nt * 5 % KT : 0;
+  const int turn = TURNS && p.m <= FEW_ROWS && KT > 0 ? (p.col0 + col_first) / 256 * 5 % KT : 0;
   int f_left = KT, f_seg = SEGS > 1 && seg_steps > 0 ? k_begin / seg_steps : 0, f_step = k_begin - f_seg * seg_steps + turn;
   const bf16_t *f_a, *f_b, *f_b2 = nullptr;
   auto place_of = [&]() {
@@ -676,12 +679,36 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
     __builtin_amdgcn_sched_barrier(0);
     slot = next;
   };
+  // Logits of few rows, which one token's loss hangs on: sums of 512 K each, added up beside, have a third of the rounding of one chain (4096 K:
+  // 3e-6 of a logit of 16 or so before).  Smaller tiles have the registers for it, larger ones are not taken for few rows.
+  constexpr bool BESIDE = EPI::LOGITS && !PLANES && BM * BN <= 128 * 128;
+  floatx4_t beside[BESIDE ? MB : 1][BESIDE ? NB : 1] = {};
+  const bool few = BESIDE && p.m <= FEW_ROWS;
   int ks = 0;
   for (; ks + 1 < KT; ks += 2) {
     step(std::integral_constant<int, 0>{}, std::false_type{});
     step(std::integral_constant<int, 1>{}, std::true_type{});
+    if constexpr (BESIDE) {
+      if (few && (ks & 14) == 14) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            beside[mb][nb] += acc[mb][nb];
+            acc[mb][nb] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+          }
+      }
+    }
   }
   if (ks < KT) step(std::integral_constant<int, 0>{}, std::true_type{});
+  if constexpr (BESIDE) {
+    if (few) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) acc[mb][nb] += beside[mb][nb];
+    }
+  }
   __builtin_amdgcn_sched_barrier(0);
   wait_vmcnt<0>();                                           // (no load into LDS may outlive the workgroup)
   const int64_t row0 = row_first + wm * TM;
@@ -886,9 +913,21 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
       }
     }
   };
+  // sums of at most 512 K (fp32: 128 MFMAs) in one chain, added up beside
+  constexpr int CHAIN = 512 / K;
+  floatx4_t beside[MB][NB] = {};
   load(k_begin, 0);
   load(k_begin + 1, 1);
   for (int s = k_begin; s < k_end; s += 2) {
+    if (s > k_begin && (s - k_begin) % CHAIN == 0) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          beside[mb][nb] += acc[mb][nb];
+          acc[mb][nb] = floatx4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
     store(s, 0, 0);
     __syncthreads();                                         // (a buffer's reads lie before the barrier of the step between)
     load(s + 2, 0);
@@ -900,6 +939,10 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
       multiply(1);
     }
   }
+#pragma unroll
+  for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) acc[mb][nb] += beside[mb][nb];
   const int64_t row0 = row_first + wm * TM;
   if constexpr (EPI::RANGES) {
     put_ranges<typename EPI::type>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);

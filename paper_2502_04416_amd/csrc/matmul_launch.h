@@ -6,11 +6,11 @@
 namespace cmoe {
 
 // The ring's tiles and those of the kernel for any operand: rows, columns, columns of waves (the columns of a wave are a range of PRODUCT_LSE).
-enum Tile { RING_256, RING_128, RING_64, ANY_128, ANY_64, ANY_32, TILES };
+enum Tile { RING_256, RING_128, RING_64, ANY_64, ANY_32, TILES };
 struct TileShape {
   int bm, bn, wgn;
 };
-constexpr TileShape kTiles[TILES] = {{256, 256, 2}, {128, 128, 2}, {64, 128, 2}, {128, 128, 2}, {64, 64, 2}, {32, 128, 4}};
+constexpr TileShape kTiles[TILES] = {{256, 256, 2}, {128, 128, 2}, {64, 128, 2}, {64, 64, 2}, {32, 128, 4}};
 
 template <class KERNEL>
 hipError_t launch_tiles(KERNEL kernel, LdsLimit& limit, size_t lds, const MatArgs& p, int bno, hipStream_t s) {
@@ -40,7 +40,6 @@ hipError_t launch_product(Tile tile, const MatArgs& p, hipStream_t s) {
   if constexpr (!ACOL) {
     if (tile == RING_64) e = launch_mat_ring<64, 128, 6, ACOL, BCOL, EPI>(p, s);
   }
-  if (tile == ANY_128) e = launch_mat_any<128, 128, 2, 2, ACOL, BCOL, EPI>(p, s);
   if (tile == ANY_64) e = launch_mat_any<64, 64, 2, 2, ACOL, BCOL, EPI>(p, s);
   if (tile == ANY_32) e = launch_mat_any<32, 128, 1, 4, ACOL, BCOL, EPI>(p, s);
   if (e != hipSuccess || p.k_split == 1) return e;

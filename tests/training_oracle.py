@@ -69,9 +69,24 @@ def head_loss(x, w, ids):
 def head_gradients(x, w, ids, lse, dloss, scale):
     """{name: (value, bound)} of dx and dw from a stored lse."""
     z, e = head_logits(x, w)
-    v = w.shape[0]
+    far = (z - lse.double()[:, None]).abs()
     p = torch.exp(z - lse.double()[:, None])
-    ep = p * torch.expm1(e + (8 + 4 * (z - lse.double()[:, None]).abs()) * U32)
+    return _head_gradients(x, w, ids, dloss, scale, p, p * torch.expm1(e + (8 + 4 * far) * U32))
+
+
+def head_gradients_of_one_pass(x, w, ids, dloss, scale):
+    """The same where the backward pass's logits have the bits of those that lse was taken of: an error d of the logits moves p by
+    p (d - sum p d), at most 2 p (1 - p) max |d|, and half as much again for what that moves in turn; the rest is the rounding of lse and
+    of the exponential."""
+    z, e = head_logits(x, w)
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    p = torch.exp(z - lse)
+    assert float(e.max()) < 0.1
+    return _head_gradients(x, w, ids, dloss, scale, p, 3 * p * (1 - p) * e.amax(1, keepdim=True) + p * (16 + 4 * (z - lse).abs() + 2 * lse.abs()) * U32)
+
+
+def _head_gradients(x, w, ids, dloss, scale, p, ep):
+    v = w.shape[0]
     rows = ((ids >= 0) & (ids < v)).nonzero()[:, 0]
     weight = torch.zeros(len(ids), 1, dtype=torch.float64, device=x.device)
     weight[rows, 0] = dloss.double()[rows] if dloss is not None else 1.0
