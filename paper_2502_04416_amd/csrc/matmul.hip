@@ -33,8 +33,8 @@ struct Cost {
   double alone, share, ends;
   int per_cu;
 };
-constexpr Cost kBf16[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {0.4, 0.25, 5, 4}, {0.4, 0.3, 5, 2}};
-constexpr Cost kFp32[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {1.2, 0.82, 6, 4}, {1.2, 0.9, 6, 2}};
+constexpr Cost kBf16[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {0.3, 0.2, 5, 4}, {0.35, 0.3, 5, 2}};
+constexpr Cost kFp32[TILES] = {{0, 0, 0, 1}, {0.85, 0.85, 10, 1}, {0.60, 0.60, 8, 1}, {0.82, 0.62, 6, 4}, {0.85, 0.7, 6, 2}};
 constexpr double kLaunch = 4, kBytesPerUs = 4.5e6;
 
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -65,8 +65,8 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
   double best_cost = 1e300;
   for (int t = RING_256; t <= (direct ? RING_64 : ANY_32); ++t) {
     const bool ring = t <= RING_64;
-    if (sh.a_columns && t == RING_64) continue;
-    if (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && (any || forced_tile <= RING_64) && !(sh.a_columns && forced_tile == RING_64) &&
+    if ((sh.a_columns && t == RING_64) || (planes == 3 && t == RING_256)) continue;
+    if (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && (any || forced_tile <= RING_64) && !(sh.a_columns && forced_tile == RING_64) && !(planes == 3 && forced_tile == RING_256) &&
         !(direct && forced_tile > RING_64))
       continue;
     if (!ring && !any) continue;
@@ -75,7 +75,7 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
     if ((kind == PRODUCT_LSE || kind == PRODUCT_DLOGITS) && t == RING_256 && m <= FEW_ROWS) continue;
     const size_t room = ring ? copies : 0;
     if (room > workspace) continue;
-    const int64_t steps = steps1 * (ring && planes == 3 ? PAIRS : 1);
+    const int64_t steps = steps1;
     const int64_t tiles = (m + kTiles[t].bm - 1) / kTiles[t].bm * ((cols + kTiles[t].bn - 1) / kTiles[t].bn) * pair;
     const Cost& c = (dtype == CMOE_F32 ? kFp32 : kBf16)[t];
     const int64_t slots = (int64_t)CUS * c.per_cu, full = sh.splits ? tiles / slots * slots : 0, rest = tiles - full;

@@ -13,14 +13,15 @@
 // bit 2 is the other read).
 //
 // fp32 on the ring: an operand is copied into three planes of bf16 that hold the first, the second and the last eight of its 24 bits
-// (matmul_prepare; cut, not rounded, so that their sum is the value), and the six products of planes above 2^-24 are summed as parts of K, the
-// smallest first: the sums and their errors are those of fp32 products.  Infinities become NaN.  One such product runs at a sixth
-// of the bf16 rate, 200 TFLOP/s, where the fp32 matrix instructions have 157 at most.  bf16 operands at odd addresses or of
-// odd widths are copied into one plane.
+// (matmul_prepare; cut, not rounded, so that their sum is the value).  A stage holds a step of all planes, and the six products of planes above
+// 2^-24 are summed: the sums and their errors are those of fp32 products.  Infinities become NaN.  Such a product runs at a sixth of
+// the bf16 rate, above 200 TFLOP/s, where the fp32 matrix instructions have 157 at most.  bf16 operands at odd addresses or of odd
+// widths are copied into one plane.
 //
 // matmul_any: both types, any alignment and size, operands through registers with every chunk's end checked: what is too small to be worth copying.
 #pragma once
 #include <type_traits>
+#include <utility>
 
 #include "device_utils.h"
 #include "dropout_device.h"
@@ -480,27 +481,40 @@ __device__ __forceinline__ bf16x8_t read_turned2(const bf16_t* at, int further) 
   return u.v;
 }
 
-constexpr int mat_ring_elems(int bm, int bn, int stages) { return stages * (bm + bn) * BK; }
-template <int BM, int BN, int STAGES, int WGM, int WGN>
+constexpr int mat_ring_elems(int bm, int bn, int stages, int planes) { return stages * planes * (bm + bn) * BK; }
+template <class EPI>
+constexpr int planes_of() { return sizeof(typename EPI::type) == 4 ? 3 : 1; }
+template <int BM, int BN, int STAGES, int WGM, int WGN, class EPI>
 constexpr size_t mat_ring_bytes() {
-  const int strips = WGM * WGN * strip_floats<BM / WGM / 16, BN / WGN / 16>() * 4, ring = mat_ring_elems(BM, BN, STAGES) * 2;
+  const int strips = WGM * WGN * strip_floats<BM / WGM / 16, BN / WGN / 16>() * 4, ring = mat_ring_elems(BM, BN, STAGES, planes_of<EPI>()) * 2;
   return ring > strips ? ring : strips;
 }
 
 constexpr int FEW_ROWS = 64;                                 // whose products are bound by the other operand's way out of memory
 
-// The pairs of planes of two fp32 operands whose products count, smallest first: plane of A and of B, two bits each.
-constexpr int PAIRS = 6, PAIRS_A = 0 | 1 << 2 | 2 << 4 | 0 << 6 | 1 << 8 | 0 << 10, PAIRS_B = 2 | 1 << 2 | 0 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
+// f(0), f(1) ... with indices that are constants: more of them than the compiler unrolls of a loop.
+template <int N, class F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each_index(F&& f) {
+  each_of<N>(f, std::make_integer_sequence<int, N>{});
+}
+
+// The pairs of planes of two fp32 operands whose products count; the last one's sums are by far the largest and are kept apart from the others'.
+constexpr int PAIRS = 6;
+constexpr int kPairA[PAIRS] = {0, 1, 2, 0, 1, 0}, kPairB[PAIRS] = {2, 1, 0, 1, 0, 0};
 
 template <int BM, int BN, int STAGES, int WGM, int WGN, bool ACOL, bool BCOL, class EPI>
 __global__ __launch_bounds__(WGM* WGN * 64)
-__attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 1024 ? 2 : 1))) void matmul_ring(MatArgs p) {
+__attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES, planes_of<EPI>()) * 2 <= 80 * 1024 ? 2 : 1))) void matmul_ring(MatArgs p) {
   constexpr int NW = WGM * WGN;
   constexpr int TM = BM / WGM, TN = BN / WGN, MB = TM / 16, NB = TN / 16;
-  constexpr int A_CH = BM / 16 / NW, B_CH = BN / 16 / NW, LPT = A_CH + B_CH;   // load instructions per wave and step
-  constexpr int A_ELEMS = BM * BK, STAGE_ELEMS = (BM + BN) * BK;
-  constexpr bool PLANES = sizeof(typename EPI::type) == 4;
-  constexpr int SEGS = (PLANES ? PAIRS : 1) * (EPI::SEGMENTS ? 2 : 1);         // parts of K one after the other
+  constexpr int PL = planes_of<EPI>();
+  constexpr int A_CH = BM / 16 / NW, B_CH = BN / 16 / NW, LPT = PL * (A_CH + B_CH);   // load instructions per wave and step
+  constexpr int A_ELEMS = PL * BM * BK, STAGE_ELEMS = PL * (BM + BN) * BK;
+  constexpr int SEGS = EPI::SEGMENTS ? 2 : 1;                                  // parts of K one after the other
   static_assert(NW == 4 && BM % 64 == 0 && BN % 64 == 0, "a wave loads whole blocks and panels");
   static_assert((!ACOL || TM % 64 == 0) && (!BCOL || EPI::DUAL || TN % 64 == 0), "panels belong to one wave column");
   static_assert(!EPI::DUAL || (BCOL && BN % 128 == 0 && (TN / 2) % 32 == 0), "gate and up panels alternate");
@@ -550,13 +564,10 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
   int f_left = KT, f_seg = SEGS > 1 && seg_steps > 0 ? k_begin / seg_steps : 0, f_step = k_begin - f_seg * seg_steps + turn;
   const bf16_t *f_a, *f_b, *f_b2 = nullptr;
   auto place_of = [&]() {
-    const int part = EPI::SEGMENTS ? f_seg / (SEGS / 2) : 0, pair = f_seg - part * (EPI::SEGMENTS ? SEGS / 2 : 0);
-    const bf16_t* a = static_cast<const bf16_t*>(EPI::SEGMENTS && part ? p.a2 : p.a);
-    const bf16_t* b = static_cast<const bf16_t*>((EPI::SEGMENTS && part) || (EPI::PAIRED && z) ? p.b2 : p.b);
-    const int64_t at_a = (ACOL ? row_first + f_step * BK * p.lda : row_first * p.lda + f_step * BK) + (PLANES ? (PAIRS_A >> (2 * pair) & 3) * p.a_plane : 0);
-    const int64_t at_b = (BCOL ? col_first + f_step * BK * p.ldb : col_first * p.ldb + f_step * BK) + (PLANES ? (PAIRS_B >> (2 * pair) & 3) * p.b_plane : 0);
-    f_a = uniform_ptr(a + at_a);
-    f_b = uniform_ptr(b + at_b);
+    const bool second = EPI::SEGMENTS && f_seg > 0;
+    f_a = uniform_ptr(static_cast<const bf16_t*>(second ? p.a2 : p.a) + (ACOL ? row_first + f_step * BK * p.lda : row_first * p.lda + f_step * BK));
+    const int64_t at_b = BCOL ? col_first + f_step * BK * p.ldb : col_first * p.ldb + f_step * BK;
+    f_b = uniform_ptr(static_cast<const bf16_t*>(second || (EPI::PAIRED && z) ? p.b2 : p.b) + at_b);
     if (EPI::DUAL) f_b2 = uniform_ptr(static_cast<const bf16_t*>(p.b2) + at_b);
   };
   place_of();
@@ -588,12 +599,16 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
     dma16_buffer(base, __builtin_amdgcn_readfirstlane(f_left > 0 ? size : 0), off, 0, dst);
   };
   auto issue = [&](int slot, int i) {                        // load i of the step fetched next
+    const int plane = i / (A_CH + B_CH), q = i % (A_CH + B_CH);
     bf16_t* st = smem + slot * STAGE_ELEMS;
-    if (i < A_CH) {
-      fetch(std::bool_constant<ACOL>{}, f_a, p.lda, p.k, a_off[i], st + (ACOL ? i * 2048 + wave * 512 : (wave + i * NW) * BLK));
+    if (q < A_CH) {
+      fetch(std::bool_constant<ACOL>{}, PL > 1 ? uniform_ptr(f_a + plane * p.a_plane) : f_a, p.lda, p.k, a_off[q],
+            st + plane * BM * BK + (ACOL ? q * 2048 + wave * 512 : (wave + q * NW) * BLK));
     } else {
-      const int j = i - A_CH;
-      fetch(std::bool_constant<BCOL>{}, EPI::DUAL && (j & 1) ? f_b2 : f_b, p.ldb, p.k_b, b_off[j], st + A_ELEMS + (BCOL ? j * 2048 + wave * 512 : (wave + j * NW) * BLK));
+      const int j = q - A_CH;
+      const bf16_t* base = EPI::DUAL && (j & 1) ? f_b2 : f_b;
+      fetch(std::bool_constant<BCOL>{}, PL > 1 ? uniform_ptr(base + plane * p.b_plane) : base, p.ldb, p.k_b, b_off[j],
+            st + A_ELEMS + plane * BN * BK + (BCOL ? j * 2048 + wave * 512 : (wave + j * NW) * BLK));
     }
   };
 
@@ -611,32 +626,39 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
 #pragma unroll
   for (int c = 0; c < 4; ++c) turned_a[c] = (kq * 8 + tj) * 64 + ((c ^ swz) << 4) + ((r16 & 3) << 2);
 
-  floatx4_t acc[MB][NB];
+  floatx4_t acc[MB][NB], low[PL > 1 ? MB : 1][PL > 1 ? NB : 1];               // low: of the pairs of planes but the last
 #pragma unroll
   for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[mb][nb][i] = 0.0f;
+      for (int i = 0; i < 4; ++i) {
+        acc[mb][nb][i] = 0.0f;
+        if (PL > 1) low[mb][nb][i] = 0.0f;
+      }
 
-  bf16x8_t af[2][MB], wf[2][NB];
-  auto load_frag = [&](int slot, int f, int set) {           // B fragments first, then A
+  bf16x8_t af[2][PL * MB], wf[2][PL * NB];
+  auto load_frag = [&](int slot, int f, int set) {           // of every plane B's fragments first, then A's
+    const int plane = f / (NB + MB), g = f % (NB + MB);
     const bf16_t* st = smem + slot * STAGE_ELEMS;
-    if (f < NB) {
-      if constexpr (!BCOL) wf[set][f] = *reinterpret_cast<const bf16x8_t*>(st + A_ELEMS + (wn * NB + f) * BLK + frag);
+    if (g < NB) {
+      const bf16_t* tb = st + A_ELEMS + plane * BN * BK;
+      bf16x8_t& to = wf[set][plane * NB + g];
+      if constexpr (!BCOL) to = *reinterpret_cast<const bf16x8_t*>(tb + (wn * NB + g) * BLK + frag);
       else if constexpr (EPI::DUAL) {
-        const int which = f / (NB / 2), c = f % (NB / 2);    // panel of the wave's column block, in gate / up pairs
-        wf[set][f] = read_turned2(st + A_ELEMS + ((wn * (NB / 2) / 4 + c / 4) * 2 + which) * 2048 + turned[c % 4], 4 * 64);
-      } else wf[set][f] = read_turned2(st + A_ELEMS + (wn * (NB / 4) + f / 4) * 2048 + turned[f % 4], 4 * 64);
+        const int which = g / (NB / 2), c = g % (NB / 2);    // panel of the wave's column block, in gate / up pairs
+        to = read_turned2(tb + ((wn * (NB / 2) / 4 + c / 4) * 2 + which) * 2048 + turned[c % 4], 4 * 64);
+      } else to = read_turned2(tb + (wn * (NB / 4) + g / 4) * 2048 + turned[g % 4], 4 * 64);
     } else {
-      const int q = f - NB;
-      if constexpr (!ACOL) af[set][q] = *reinterpret_cast<const bf16x8_t*>(st + (wm * MB + q) * BLK + frag);
-      else af[set][q] = read_turned2(st + (wm * (MB / 4) + q / 4) * 2048 + turned_a[q % 4], 4 * 64);
+      const bf16_t* ta = st + plane * BM * BK;
+      const int q = g - NB;
+      if constexpr (!ACOL) af[set][plane * MB + q] = *reinterpret_cast<const bf16x8_t*>(ta + (wm * MB + q) * BLK + frag);
+      else af[set][plane * MB + q] = read_turned2(ta + (wm * (MB / 4) + q / 4) * 2048 + turned_a[q % 4], 4 * 64);
     }
   };
   static_assert(!EPI::DUAL || NB / 2 == 2 || NB / 2 % 4 == 0, "a wave's gate columns are whole panels, or half of one");
 
-  constexpr int NM = MB * NB, NF = MB + NB, ND = LPT;
+  constexpr int NM = (PL > 1 ? PAIRS : 1) * MB * NB, NF = PL * (MB + NB), ND = LPT;
   static_assert(ND <= NM, "at most one load instruction after an MFMA");
 #pragma unroll
   for (int st = 0; st < STAGES; ++st) {
@@ -661,27 +683,27 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     const int next = slot + 1 == STAGES ? 0 : slot + 1;
-#pragma unroll
-    for (int m = 0; m < NM; ++m) {
-      const int mb = m / NB, nb = m % NB;
+    each_index<NM>([&](auto m_tag) {
+      constexpr int m = decltype(m_tag)::value, pair = m / (MB * NB), mb = m / NB % MB, nb = m % NB;
+      constexpr int pa = PL > 1 ? kPairA[pair] : 0, pb = PL > 1 ? kPairB[pair] : 0;
+      floatx4_t& sum = PL > 1 && pair < PAIRS - 1 ? low[PL > 1 ? mb : 0][PL > 1 ? nb : 0] : acc[mb][nb];
       __builtin_amdgcn_sched_barrier(0);
-      if (WAIT && m == NM - 1) mfma_acc<true>(acc[mb][nb], wf[SET][nb], af[SET][mb]);
-      else mfma_acc<false>(acc[mb][nb], wf[SET][nb], af[SET][mb]);
+      mfma_acc<WAIT && m == NM - 1>(sum, wf[SET][pb * NB + nb], af[SET][pa * MB + mb]);
       __builtin_amdgcn_sched_barrier(0);
       // the fragments of the next step in the first three quarters of the MFMAs, the load instructions spread over all
+      constexpr int f0 = (m * NF * 4 + NM * 3 - 1) / (NM * 3), f1 = ((m + 1) * NF * 4 + NM * 3 - 1) / (NM * 3);
 #pragma unroll
-      for (int f = 0; f < NF; ++f)
-        if (f * NM * 3 / (NF * 4) == m) load_frag(next, f, SET ^ 1);
-      const int i = ((m + 1) * ND + NM - 1) / NM - 1;
-      if (i < ND && (i + 1) * NM / ND - 1 == m) issue(slot, i);
-    }
+      for (int f = f0; f < (f1 < NF ? f1 : NF); ++f) load_frag(next, f, SET ^ 1);
+      constexpr int i = ((m + 1) * ND + NM - 1) / NM - 1;
+      if constexpr (i < ND && (i + 1) * NM / ND - 1 == m) issue(slot, i);
+    });
     advance();
     __builtin_amdgcn_sched_barrier(0);
     slot = next;
   };
   // Logits of few rows, which one token's loss hangs on: sums of 512 K each, added up beside, have a third of the rounding of one chain (4096 K:
   // 3e-6 of a logit of 16 or so before).  Smaller tiles have the registers for it, larger ones are not taken for few rows.
-  constexpr bool BESIDE = EPI::LOGITS && !PLANES && BM * BN <= 128 * 128;
+  constexpr bool BESIDE = EPI::LOGITS && PL == 1 && BM * BN <= 128 * 128;
   floatx4_t beside[BESIDE ? MB : 1][BESIDE ? NB : 1] = {};
   const bool few = BESIDE && p.m <= FEW_ROWS;
   int ks = 0;
@@ -708,6 +730,12 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES) * 2 <= 80 * 10
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) acc[mb][nb] += beside[mb][nb];
     }
+  }
+  if constexpr (PL > 1) {
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) acc[mb][nb] += low[mb][nb];
   }
   __builtin_amdgcn_sched_barrier(0);
   wait_vmcnt<0>();                                           // (no load into LDS may outlive the workgroup)

@@ -24,7 +24,7 @@ hipError_t launch_tiles(KERNEL kernel, LdsLimit& limit, size_t lds, const MatArg
 template <int BM, int BN, int STAGES, bool ACOL, bool BCOL, class EPI>
 hipError_t launch_mat_ring(const MatArgs& p, hipStream_t s) {
   static LdsLimit limit;
-  return launch_tiles(matmul_ring<BM, BN, STAGES, 2, 2, ACOL, BCOL, EPI>, limit, mat_ring_bytes<BM, BN, STAGES, 2, 2>(), p, EPI::DUAL ? BN / 2 : BN, s);
+  return launch_tiles(matmul_ring<BM, BN, STAGES, 2, 2, ACOL, BCOL, EPI>, limit, mat_ring_bytes<BM, BN, STAGES, 2, 2, EPI>(), p, EPI::DUAL ? BN / 2 : BN, s);
 }
 template <int BM, int BN, int WGM, int WGN, bool ACOL, bool BCOL, class EPI>
 hipError_t launch_mat_any(const MatArgs& p, hipStream_t s) {
@@ -35,10 +35,13 @@ hipError_t launch_mat_any(const MatArgs& p, hipStream_t s) {
 template <bool ACOL, bool BCOL, class EPI>
 hipError_t launch_product(Tile tile, const MatArgs& p, hipStream_t s) {
   hipError_t e = hipErrorInvalidValue;
-  if (tile == RING_256) e = launch_mat_ring<256, 256, 5, ACOL, BCOL, EPI>(p, s);
-  if (tile == RING_128) e = launch_mat_ring<128, 128, 5, ACOL, BCOL, EPI>(p, s);
+  constexpr bool PLANES = planes_of<EPI>() > 1;
+  if constexpr (!PLANES) {
+    if (tile == RING_256) e = launch_mat_ring<256, 256, 5, ACOL, BCOL, EPI>(p, s);
+  }
+  if (tile == RING_128) e = launch_mat_ring<128, 128, PLANES ? 3 : 5, ACOL, BCOL, EPI>(p, s);
   if constexpr (!ACOL) {
-    if (tile == RING_64) e = launch_mat_ring<64, 128, 6, ACOL, BCOL, EPI>(p, s);
+    if (tile == RING_64) e = launch_mat_ring<64, 128, PLANES ? 4 : 6, ACOL, BCOL, EPI>(p, s);
   }
   if (tile == ANY_64) e = launch_mat_any<64, 64, 2, 2, ACOL, BCOL, EPI>(p, s);
   if (tile == ANY_32) e = launch_mat_any<32, 128, 1, 4, ACOL, BCOL, EPI>(p, s);

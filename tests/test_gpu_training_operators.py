@@ -326,7 +326,7 @@ def test_head_gradients_of_nearly_certain_targets(B, dtype, shift, t, d, v):
     m.intact()
 
 
-@pytest.mark.parametrize("dtype,shift,tiles", [("bf16", 0, [*RING]), ("bf16", 1, [*RING]), ("bf16", 1, [*ANY]), ("fp32", 0, [*RING]), ("fp32", 0, [*ANY])])
+@pytest.mark.parametrize("dtype,shift,tiles", [("bf16", 0, [*RING]), ("bf16", 1, [*RING]), ("bf16", 1, [*ANY]), ("fp32", 0, ["ring 128", "ring 64"]), ("fp32", 0, [*ANY])])
 def test_logits_have_the_same_bits_on_every_tile(B, forced, dtype, shift, tiles):
     """One column of ranges and one token: lse and dweight are functions of the logits alone."""
     dt = TYPES[dtype]

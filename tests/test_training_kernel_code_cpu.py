@@ -32,7 +32,7 @@ def test_mfma_results_are_waited_for(kernels):
 
 def test_nothing_waits_for_the_loads_but_the_barrier(kernels):
     # loads per wave and step times the steps that stay under way
-    left = {"Li256ELi256ELi5E": 3 * 8, "Li128ELi128ELi5E": 3 * 4, "Li64ELi128ELi6E": 4 * 3}
+    left = {"Li256ELi256ELi5E": 3 * 8, "Li128ELi128ELi5E": 3 * 4, "Li64ELi128ELi6E": 4 * 3, "Li128ELi128ELi3E": 12, "Li64ELi128ELi4E": 2 * 9}
     for name, code in kernels.items():
         want = next(n for shape, n in left.items() if shape in name)
         mfmas = [i for i, ins in enumerate(code) if ins[1] == "v_mfma_f32_16x16x32_bf16"]
