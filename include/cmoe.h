@@ -426,7 +426,8 @@ int cmoe_adapters_backward(const cmoe_adapters_backward_args* args, void* hip_st
  * Conventions as above: contiguous [rows, cols] batches at any address an element may have (rows of multiples of 8 elements at 16-byte
  * addresses run on faster kernels), sums in fp32, enqueue only, no atomics, outputs that overlap nothing but, where it is said, the very
  * buffer of an input.  Workspaces are 16-byte aligned and may be shared by calls that one stream orders; the functions that say their size
- * return 0 where none is needed.  Tokens, widths and vocabularies are at most 2^20. */
+ * return 0 where none is needed.  Tokens, widths and vocabularies are at most 2^20.  Products of fp32 matrices are those of their 24
+ * bits, in the order and on the units that the sizes make fastest; an infinity in one may become NaN where it is multiplied. */
 
 /* The gated feed-forward block F(x) of Eq. 3 on matrices that are trained: gate = x w_gate, up = x w_up,
  * hidden = gate / (1 + exp(-gate)) * up, each rounded to dtype where it is stored; y = base + hidden w_down (of hidden as stored).
@@ -480,8 +481,8 @@ size_t cmoe_ffn_backward_workspace_bytes(int64_t tokens, int32_t d, int32_t d_ff
 int cmoe_ffn_backward(const cmoe_ffn_backward_args* args, void* hip_stream);
 
 /* Softmax cross entropy of a head over a vocabulary, whose logits z = x weight^T are never stored: lse[t] = log sum_v exp(z[t, v]),
- * loss[t] = lse[t] - z[t, ids[t]].  A token whose id is not in [0, vocab) has no target: its loss is 0.  A row whose logits
- * hold a NaN or +infinity has an lse that is NaN. */
+ * loss[t] = lse[t] - z[t, ids[t]].  A token whose id is not in [0, vocab) has no target: its loss is 0, and whatever its row of x holds reaches
+ * nothing but its own lse.  A row whose logits hold a NaN or +infinity has an lse that is NaN. */
 typedef struct {
   const void* x;             /* [tokens, d] */
   const void* weight;        /* [vocab, d] */

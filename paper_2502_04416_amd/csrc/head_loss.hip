@@ -5,6 +5,7 @@
 //              dX += dZ W (fp32 between the pieces) and dW = scale * dZ^T X, complete for the piece's rows
 // What a piece costs beside its products is dX's sums, read and written, so pieces are as wide as 128 MB of dZ allow:
 // it is read twice soon after it is written, and this part's last cache holds 256 MB.
+// dW takes x from a copy without the rows of tokens that have no target: what such a row holds (padding, NaN) would reach every row of dW as 0 times it.
 // `scale` is applied to the sums in fp32, and not to dZ: what all tokens share would round the entries of all targets, which are all
 // close to -scale, to the same side.
 #include <algorithm>
@@ -36,8 +37,9 @@ bool logits_in_place(int dtype, int64_t t, int64_t d, int64_t vocab) { return !m
 // How many vocabulary entries a piece may have for the copies of their rows, where operands may be copied, to stay below 256 MB (up to a width of
 // 8192); all of them otherwise.
 int64_t copied_piece(int dtype, int64_t t, int64_t d, int64_t vocab) {
-  if (logits_in_place(dtype, t, d, vocab)) return vocab;
-  return std::min(vocab, std::max<int64_t>(4096, ((int64_t)1 << (dtype == CMOE_F32 ? 25 : 27)) / d / 256 * 256));
+  const int64_t most = std::max<int64_t>(4096, ((int64_t)1 << 35) / t / 256 * 256);      // (a launch has fewer than 2^32 threads)
+  if (logits_in_place(dtype, t, d, vocab)) return std::min(vocab, most);
+  return std::min({vocab, most, std::max<int64_t>(4096, ((int64_t)1 << (dtype == CMOE_F32 ? 25 : 27)) / d / 256 * 256)});
 }
 
 struct ForwardSpace {
@@ -57,13 +59,14 @@ struct ForwardSpace {
 
 struct BackwardSpace {
   int64_t piece, ld;                       // vocabulary entries of a piece, elements of a row of dZ
-  size_t acc, product, total;              // offsets of dX's sums and of the products' workspace; dZ at 0
+  size_t acc, rows, product, total;        // offsets of dX's sums, of x's rows that count and of the products' workspace; dZ at 0
   BackwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
     piece = std::max(PIECE_LEAST, PIECE_BYTES / (int64_t)elem_size(dtype) / std::max<int64_t>(t, 1) / 256 * 256);
     piece = std::min(piece, copied_piece(dtype, t, d, vocab));
     ld = (piece + 7) / 8 * 8;
     acc = round16((size_t)t * ld * elem_size(dtype));
-    product = acc + (piece < vocab ? round16((size_t)t * d * 4) : 0);
+    rows = acc + (piece < vocab ? round16((size_t)t * d * 4) : 0);
+    product = rows + round16((size_t)t * d * elem_size(dtype));
     size_t most = 0;
     const int64_t last = vocab - (vocab - 1) / piece * piece;
     for (int64_t w : {piece, last}) {
@@ -99,6 +102,24 @@ __global__ __launch_bounds__(256) void head_finish(const float2* part, int range
     // (not lse - picked: a target that is nearly certain has a loss far below the rounding of lse)
     if (loss) loss[row] = (uint32_t)ids[row] < (uint32_t)vocab ? (mine.x - picked[row]) + rest : 0.0f;
   }
+}
+
+// x without the rows of tokens that have no target.  A thread per eight columns.
+template <typename T>
+__global__ __launch_bounds__(256) void head_rows(const T* x, const int32_t* ids, int vocab, int64_t tokens, int d, T* out) {
+  const uint32_t per_row = (uint32_t)(d + 7) >> 3;
+  const uint64_t first = (uint64_t)blockIdx.x * 256;
+  const uint64_t row0 = first / per_row;
+  const uint32_t c0 = (uint32_t)(first - row0 * per_row) + threadIdx.x;
+  const int64_t row = row0 + c0 / per_row;
+  if (row >= tokens) return;
+  const int col = (int)(c0 % per_row) * 8, n = d - col;
+  float v[8];
+  load8(x + row * d + col, n, v);
+  const bool has = (uint32_t)ids[row] < (uint32_t)vocab;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = has ? v[e] : 0.0f;
+  store8(out + row * d + col, n, v);
 }
 
 int check_workspace(const char* what, const void* ws, uint64_t have, size_t need) {
@@ -188,6 +209,14 @@ extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args,
                               {{"dx", a.dx, td, es}, {"dweight", a.dweight, vd, es}, {"the workspace", a.workspace, ws.total, 16}}))
     return rc;
   char* base = static_cast<char*>(a.workspace);
+  if (a.dweight) {
+    w.b = base + ws.rows;
+    const unsigned groups = (unsigned)((a.tokens * ((a.d + 7) / 8) + 255) / 256);
+    if (a.dtype == CMOE_BF16)
+      hipLaunchKernelGGL(head_rows<bf16_t>, dim3(groups), dim3(256), 0, s, (const bf16_t*)a.x, a.ids, a.vocab, a.tokens, a.d, (bf16_t*)(base + ws.rows));
+    else hipLaunchKernelGGL(head_rows<float>, dim3(groups), dim3(256), 0, s, (const float*)a.x, a.ids, a.vocab, a.tokens, a.d, (float*)(base + ws.rows));
+    if (hipError_t e = hipGetLastError()) return launched(what, e);
+  }
   void* const room = base + ws.product;
   const size_t room_bytes = ws.total - ws.product;
   for (int64_t first = 0; first < a.vocab; first += ws.piece) {

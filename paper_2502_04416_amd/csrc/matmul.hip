@@ -34,7 +34,7 @@ struct Cost {
   int per_cu;
 };
 constexpr Cost kBf16[TILES] = {{0.62, 0.69, 14, 1}, {0.265, 0.33, 6, 2}, {0.20, 0.21, 5, 2}, {0.3, 0.2, 5, 4}, {0.35, 0.3, 5, 2}};
-constexpr Cost kFp32[TILES] = {{0, 0, 0, 1}, {0.85, 0.85, 10, 1}, {0.60, 0.60, 8, 1}, {0.82, 0.62, 6, 4}, {0.85, 0.7, 6, 2}};
+constexpr Cost kFp32[TILES] = {{0, 0, 0, 1}, {0.82, 0.82, 8, 1}, {0.58, 0.58, 7, 1}, {0.82, 0.62, 6, 4}, {0.85, 0.7, 6, 2}};
 constexpr double kLaunch = 4, kBytesPerUs = 4.5e6;
 
 int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }

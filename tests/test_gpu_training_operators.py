@@ -263,7 +263,7 @@ def test_head_without_any_target(B):
 
 
 def test_head_ignores_what_a_token_without_a_target_holds(B):
-    """NaN and infinities in rows without a target reach no gradient of theirs; the weight's gradient sees them as 0 * their row."""
+    """NaN and infinities in rows without a target reach their own lse alone."""
     for dt, shift in ((torch.bfloat16, 0), (torch.float32, 1)):
         m = Arena(9, shift=shift)
         x, w = m.normal(40, 64, dtype=dt), m.normal(300, 64, dtype=dt, std=0.1)
@@ -274,9 +274,14 @@ def test_head_ignores_what_a_token_without_a_target_holds(B):
         B.head_loss_forward(x, w, ids, loss, lse)
         assert bool((loss[::4] == 0).all()) and bool(torch.isfinite(loss).all())
         assert bool(torch.isnan(lse[0])) and bool(torch.isfinite(lse[8:]).all())
-        dx = m.out(40, 64, dtype=dt)
-        B.head_loss_backward(x, w, ids, lse, dx=dx)
+        dx, dw = m.out(40, 64, dtype=dt), m.out(300, 64, dtype=dt)
+        B.head_loss_backward(x, w, ids, lse, dx=dx, dweight=dw)
         assert bool((dx[::4] == 0).all()) and bool(torch.isfinite(dx).all())
+        clean, other, also = x.clone(), torch.empty_like(lse), torch.empty_like(dw)
+        clean[::4] = 0
+        B.head_loss_forward(clean, w, ids, lse=other)
+        B.head_loss_backward(clean, w, ids, other, dweight=also)
+        assert torch.equal(dw, also)
         # and with a target the NaN is seen
         ids[0] = 5
         B.head_loss_forward(x, w, ids, loss, lse)
