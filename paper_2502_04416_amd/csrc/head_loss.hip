@@ -31,38 +31,38 @@ int check_sizes(const char* what, int32_t dtype, int64_t tokens, int32_t d, int3
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// Whether both passes take their logits from operands where they are: of the sizes alone, so that they agree (see MatArgs::no_copies).
-bool logits_in_place(int dtype, int64_t t, int64_t d, int64_t vocab) { return !matmul_copies(PRODUCT_LSE, dtype, t, vocab, d); }
-
 // How many vocabulary entries a piece may have for the copies of their rows, where operands may be copied, to stay below 256 MB (up to a width of
 // 8192); all of them otherwise.
-int64_t copied_piece(int dtype, int64_t t, int64_t d, int64_t vocab) {
+int64_t copied_piece(int dtype, int64_t t, int64_t d, int64_t vocab, const LogitsPlan& plan) {
   const int64_t most = std::max<int64_t>(4096, ((int64_t)1 << 35) / t / 256 * 256);      // (a launch has fewer than 2^32 threads)
-  if (logits_in_place(dtype, t, d, vocab)) return std::min(vocab, most);
+  if (plan.in_place) return std::min(vocab, most);
   return std::min({vocab, most, std::max<int64_t>(4096, ((int64_t)1 << (dtype == CMOE_F32 ? 25 : 27)) / d / 256 * 256)});
 }
 
 struct ForwardSpace {
+  LogitsPlan plan;
   int64_t piece, last;                     // entries of a piece, and of the last one
   size_t picked, product, total;           // offsets of the targets' logits and of the products' workspace; the ranges at 0
   ForwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
-    piece = copied_piece(dtype, t, d, vocab);
-    const bool in_place = logits_in_place(dtype, t, d, vocab);
+    plan = logits_plan(dtype, t, vocab, d);
+    piece = copied_piece(dtype, t, d, vocab, plan);
     const int64_t pieces = (vocab - 1) / piece;              // but the last
     last = vocab - pieces * piece;
-    const int64_t ranges = pieces * lse_ranges(dtype, t, piece, d, in_place) + lse_ranges(dtype, t, last, d, in_place);
+    const int64_t ranges = pieces * lse_ranges(dtype, t, piece, d, plan) + lse_ranges(dtype, t, last, d, plan);
     picked = round16((size_t)ranges * t * sizeof(float2));
     product = picked + round16((size_t)t * 4);
-    total = product + std::max(matmul_workspace_bytes(PRODUCT_LSE, dtype, t, piece, d, in_place), matmul_workspace_bytes(PRODUCT_LSE, dtype, t, last, d, in_place));
+    total = product + std::max(matmul_workspace_bytes(PRODUCT_LSE, dtype, t, piece, d, &plan), matmul_workspace_bytes(PRODUCT_LSE, dtype, t, last, d, &plan));
   }
 };
 
 struct BackwardSpace {
+  LogitsPlan plan;
   int64_t piece, ld;                       // vocabulary entries of a piece, elements of a row of dZ
   size_t acc, rows, product, total;        // offsets of dX's sums, of x's rows that count and of the products' workspace; dZ at 0
   BackwardSpace(int dtype, int64_t t, int64_t d, int64_t vocab) {
+    plan = logits_plan(dtype, t, vocab, d);
     piece = std::max(PIECE_LEAST, PIECE_BYTES / (int64_t)elem_size(dtype) / std::max<int64_t>(t, 1) / 256 * 256);
-    piece = std::min(piece, copied_piece(dtype, t, d, vocab));
+    piece = std::min(piece, copied_piece(dtype, t, d, vocab, plan));
     ld = (piece + 7) / 8 * 8;
     acc = round16((size_t)t * ld * elem_size(dtype));
     rows = acc + (piece < vocab ? round16((size_t)t * d * 4) : 0);
@@ -71,7 +71,7 @@ struct BackwardSpace {
     const int64_t last = vocab - (vocab - 1) / piece * piece;
     for (int64_t w : {piece, last}) {
       const int64_t padded = (w + 7) / 8 * 8;
-      most = std::max({most, matmul_workspace_bytes(PRODUCT_DLOGITS, dtype, t, padded, d, logits_in_place(dtype, t, d, vocab)), matmul_workspace_bytes(PRODUCT_DHEAD, dtype, t, d, padded),
+      most = std::max({most, matmul_workspace_bytes(PRODUCT_DLOGITS, dtype, t, padded, d, &plan), matmul_workspace_bytes(PRODUCT_DHEAD, dtype, t, d, padded),
                        matmul_workspace_bytes(PRODUCT_DW, dtype, w, d, t)});
     }
     total = product + most;
@@ -164,7 +164,7 @@ extern "C" int cmoe_head_loss_forward(const cmoe_head_loss_forward_args* args, v
     p.a = a.x, p.lda = a.d, p.b = static_cast<const char*>(a.weight) + (size_t)first * a.d * es, p.ldb = a.d;
     p.m = (int)a.tokens, p.n = (int)std::min(ws.piece, a.vocab - first), p.k = a.d;
     p.ids = a.ids, p.vocab = a.vocab, p.col0 = (int)first;
-    p.no_copies = logits_in_place(a.dtype, a.tokens, a.d, a.vocab);
+    p.logits = ws.plan;
     p.part = part + (size_t)ranges * a.tokens, p.picked = picked;
     int more = 0;
     if (hipError_t e = matmul(PRODUCT_LSE, a.dtype, p, base + ws.product, ws.total - ws.product, s, &more)) return launched(what, e);
@@ -227,7 +227,7 @@ extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args,
     p.m = (int)a.tokens, p.n = padded, p.n_b = n, p.k = a.d;
     p.c = base, p.ldc = ws.ld;
     p.ids = a.ids, p.vocab = a.vocab, p.col0 = (int)first, p.lse = a.lse, p.dloss = a.dloss;
-    p.no_copies = logits_in_place(a.dtype, a.tokens, a.d, a.vocab);
+    p.logits = ws.plan;
     if (hipError_t e = matmul(PRODUCT_DLOGITS, a.dtype, p, room, room_bytes, s)) return launched(what, e);
     if (a.dx) {
       MatArgs q = {};

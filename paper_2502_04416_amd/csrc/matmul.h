@@ -19,6 +19,13 @@ enum Product {
   PRODUCT_DHEAD,    // A by rows, B by columns: acc (+)= A B over the pieces of a vocabulary, c = alpha * acc with the last one
 };
 
+// PRODUCT_LSE and PRODUCT_DLOGITS have to agree to the bit: 1 - p of a likely target is a difference of both.  The ring's tiles sum in one
+// order, those for any operand in another, and so does every K split: both passes go by the same plan, which is a function of the sizes alone.
+struct LogitsPlan {
+  bool in_place;             // of operands that the ring cannot read where they are: no copies
+  int k_split;               // of all tiles
+};
+
 struct MatArgs {
   const void *a, *a2, *b, *b2;
   int64_t lda, ldb;          // elements from one row of memory to the next (of both parts)
@@ -39,9 +46,7 @@ struct MatArgs {
   const int32_t* ids;        // [m]
   const float* lse;          // [m]
   const float* dloss;        // [m] or null
-  // PRODUCT_LSE and PRODUCT_DLOGITS have to agree to the bit: 1 - p of a likely target is a difference of both.  The ring's tiles sum in one
-  // order, those for any operand in another: both passes say which, for operands that the ring cannot read where they are.
-  bool no_copies;
+  LogitsPlan logits;
   float2* part;              // [column ranges][m]
   float* picked;             // [m]
   // Tiles are numbered over both results (zs of them); from tile `full` on, each is split into k_split parts of K, whose sums go to slab
@@ -50,12 +55,12 @@ struct MatArgs {
   float* slab;
 };
 
+// The plan for the logits of m tokens of width k over n entries; for the two products of logits, below, of any piece of them.
+LogitsPlan logits_plan(int dtype, int64_t m, int64_t n, int64_t k);
 // Bytes of workspace, for copies of operands and slabs of a K split, that a product may ask for, whatever its operands' alignment.
-size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k, bool no_copies = false);
-// Whether the product of operands that the ring cannot read where they are copies them.
-bool matmul_copies(Product kind, int dtype, int64_t m, int64_t n, int64_t k);
+size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k, const LogitsPlan* plan = nullptr);
 // Column ranges that PRODUCT_LSE may write: rows of `part`, whatever its operands' alignment.
-int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k, bool no_copies);
+int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k, const LogitsPlan& plan);
 // Enqueues the product; m_a, n_b and k_b count as m, n and k where they are 0.  Workspace: 16-byte aligned.  *ranges, of PRODUCT_LSE: how many
 // ranges have been written.
 hipError_t matmul(Product kind, int dtype, MatArgs p, void* workspace, size_t workspace_bytes, hipStream_t s, int* ranges = nullptr);

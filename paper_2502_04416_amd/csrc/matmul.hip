@@ -13,11 +13,11 @@ namespace {
 constexpr int CUS = 256;
 
 struct Shape {
-  bool a_columns, b_columns, dual, segments, splits;
+  bool a_columns, b_columns, dual, segments, logits;
 };
 constexpr Shape shape_of(Product kind) {
   return {kind == PRODUCT_DW, kind == PRODUCT_GATED || kind == PRODUCT_DOWN || kind == PRODUCT_DW || kind == PRODUCT_DHEAD, kind == PRODUCT_GATED,
-          kind == PRODUCT_DX, kind != PRODUCT_LSE && kind != PRODUCT_DLOGITS};
+          kind == PRODUCT_DX, kind == PRODUCT_LSE || kind == PRODUCT_DLOGITS};
 }
 
 struct Choice {
@@ -46,10 +46,9 @@ size_t copy_bytes(const Shape& sh, int planes, int64_t m, int64_t n, int64_t k, 
   return ((size_t)(a + b) * planes * 2 + 255) / 256 * 256;
 }
 
-// direct: bf16 operands that the ring can read where they are.  second: there is a second B.  logits: of logits of other operands, 1 on the kernel for any,
-// 0 on the ring, where that is settled.
+// direct: bf16 operands that the ring can read where they are.  second: there is a second B.  plan: of logits, where it is settled.
 // The tiles that fill the chip a whole number of times are left whole; the rest, if that is shorter, is split.
-Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace, int logits = -1) {
+Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace, const LogitsPlan* plan = nullptr) {
   const Shape sh = shape_of(kind);
   const int pair = kind == PRODUCT_DW && second ? 2 : 1, planes = dtype == CMOE_F32 ? 3 : 1;
   const int64_t steps1 = ((k + 31) / 32) * (sh.segments ? 2 : 1);
@@ -63,27 +62,31 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
   const bool any = m * k >= 8 && std::max<int64_t>(n - 7, 1) * std::max<int64_t>(k - 7, 1) >= 8;
   Choice best{RING_128, 0, 1, !direct, 0};
   double best_cost = 1e300;
-  for (int t = RING_256; t <= (direct ? RING_64 : ANY_32); ++t) {
+  auto can = [&](int t) {
+    if (t > (direct ? RING_64 : ANY_32)) return false;
     const bool ring = t <= RING_64;
-    if ((sh.a_columns && t == RING_64) || (planes == 3 && t == RING_256)) continue;
-    if (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && (any || forced_tile <= RING_64) && !(sh.a_columns && forced_tile == RING_64) && !(planes == 3 && forced_tile == RING_256) &&
-        !(direct && forced_tile > RING_64))
-      continue;
-    if (!ring && !any) continue;
-    // logits have the bits of one order of sums in both passes: see MatArgs::no_copies
-    if (logits >= 0 && !direct && any && ring == (logits == 1)) continue;
-    if ((kind == PRODUCT_LSE || kind == PRODUCT_DLOGITS) && t == RING_256 && m <= FEW_ROWS) continue;
+    if ((sh.a_columns && t == RING_64) || (planes == 3 && t == RING_256) || (!ring && !any)) return false;
+    // logits have the bits of one order of sums in both passes (see LogitsPlan), and those of few rows are summed in two levels
+    if (plan && !direct && any && ring == plan->in_place) return false;
+    return !(sh.logits && t == RING_256 && m <= FEW_ROWS);
+  };
+  for (int t = RING_256; t < TILES; ++t) {
+    if (!can(t) || (forced_tile >= 0 && forced_tile < TILES && forced_tile != t && can(forced_tile))) continue;
+    const bool ring = t <= RING_64;
     const size_t room = ring ? copies : 0;
     if (room > workspace) continue;
     const int64_t steps = steps1;
     const int64_t tiles = (m + kTiles[t].bm - 1) / kTiles[t].bm * ((cols + kTiles[t].bn - 1) / kTiles[t].bn) * pair;
     const Cost& c = (dtype == CMOE_F32 ? kFp32 : kBf16)[t];
-    const int64_t slots = (int64_t)CUS * c.per_cu, full = sh.splits ? tiles / slots * slots : 0, rest = tiles - full;
+    const int64_t slots = (int64_t)CUS * c.per_cu, whole = tiles / slots * slots;
     for (int split = 1; split <= 32; ++split) {
+      // (of logits either all tiles are split or none: which are last differs between the passes)
+      const int64_t full = sh.logits && split > 1 ? 0 : whole, rest = tiles - full;
+      if (plan && split != plan->k_split) continue;
       const size_t slab = split > 1 ? (size_t)rest * split * kTiles[t].bm * kTiles[t].bn * 4 : 0;
-      if (split > 1 && (!sh.splits || rest == 0 || room + slab > workspace)) break;
-      if (split > 1 && forced_split < 1 && (steps / split < 6 || rest * (split - 1) >= slots)) break;
-      if (forced_split >= 1 && split != forced_split && sh.splits && rest > 0) continue;
+      if (split > 1 && (rest == 0 || room + slab > workspace)) break;
+      if (split > 1 && !plan && forced_split < 1 && (steps / split < 6 || rest * (split - 1) >= slots)) break;
+      if (!plan && forced_split >= 1 && split != forced_split && rest > 0) continue;
       const double part = (double)((steps + split - 1) / split);
       auto round = [&](double steps_of, int64_t on_a_cu) { return steps_of * std::max(c.alone, c.share * on_a_cu) + c.ends; };
       double cost = kLaunch + (double)(full / slots) * round((double)steps, c.per_cu);
@@ -112,24 +115,24 @@ hipError_t prepare(const CopyArgs& args, uint32_t groups, hipStream_t s) {
 
 }  // namespace
 
-int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k, bool no_copies) {
+LogitsPlan logits_plan(int dtype, int64_t m, int64_t n, int64_t k) {
+  const Choice other = choose(PRODUCT_LSE, dtype, false, false, m, n, k, EVERYTHING);
+  return {!other.copies, dtype == CMOE_BF16 && k % 8 == 0 ? choose(PRODUCT_LSE, dtype, true, false, m, n, k, EVERYTHING).k_split : other.k_split};
+}
+
+int64_t lse_ranges(int dtype, int64_t m, int64_t n, int64_t k, const LogitsPlan& plan) {
   int64_t most = 0;
-  for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct) most = std::max(most, ranges_of(choose(PRODUCT_LSE, dtype, direct, false, m, n, k, EVERYTHING, no_copies), n));
+  for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct) most = std::max(most, ranges_of(choose(PRODUCT_LSE, dtype, direct, false, m, n, k, EVERYTHING, &plan), n));
   return most;
 }
 
-bool matmul_copies(Product kind, int dtype, int64_t m, int64_t n, int64_t k) {
-  return choose(kind, dtype, false, has_second(kind), m, n, k, EVERYTHING).copies;
-}
-
-size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k, bool no_copies) {
-  const int logits = kind == PRODUCT_LSE || kind == PRODUCT_DLOGITS ? no_copies : -1;
+size_t matmul_workspace_bytes(Product kind, int dtype, int64_t m, int64_t n, int64_t k, const LogitsPlan* plan) {
   if (m <= 0 || n <= 0) return 0;
   const Shape sh = shape_of(kind);
   size_t most = 0;
   for (int direct = 0; direct <= (dtype == CMOE_BF16); ++direct)
     for (int second = has_second(kind); second <= (has_second(kind) || kind == PRODUCT_DW); ++second) {
-      const Choice c = choose(kind, dtype, direct, second, m, n, k, EVERYTHING, logits);
+      const Choice c = choose(kind, dtype, direct, second, m, n, k, EVERYTHING, plan);
       most = std::max(most, (c.copies ? copy_bytes(sh, dtype == CMOE_F32 ? 3 : 1, m, n, k, second) : 0) + c.slab);
     }
   return (most + 15) / 16 * 16;
@@ -146,7 +149,7 @@ hipError_t matmul(Product kind, int dtype, MatArgs p, void* workspace, size_t wo
   const bool direct = dtype == CMOE_BF16 && wide(p.a) && wide(p.a2) && wide(p.b) && wide(p.b2) && p.lda % 8 == 0 && p.ldb % 8 == 0 &&
                       (sh.a_columns ? p.m_a : p.k) % 8 == 0 && (sh.b_columns ? p.n_b : p.k) % 8 == 0;
   const Choice c = choose(kind, dtype, direct, second, p.m, p.n, p.k, workspace ? workspace_bytes : 0,
-                          kind == PRODUCT_LSE || kind == PRODUCT_DLOGITS ? p.no_copies : -1);
+                          sh.logits ? &p.logits : nullptr);
   p.zs = kind == PRODUCT_DW && second ? 2 : 1;
   p.full = c.full, p.k_split = c.k_split, p.bm = kTiles[c.tile].bm, p.bn = kTiles[c.tile].bn;
   char* room = static_cast<char*>(workspace);

@@ -200,6 +200,9 @@ template <typename T>
 struct EpiLse {
   static constexpr bool LOGITS = true, DUAL = false, SEGMENTS = false, PAIRED = false, RANGES = true;
   typedef T type;
+  typedef HeldNothing Held;
+  static __device__ __forceinline__ void hold(const MatArgs&, int64_t, int, int, Held&) {}
+  static __device__ __forceinline__ void put(const MatArgs&, int, int64_t, int, int, float (&)[8], float (&)[8], const Held&) {}
 };
 
 // The largest of two, and the exponentials summed below it.  An empty range is (-inf, 0).
@@ -317,6 +320,7 @@ __device__ __forceinline__ void put_tile(const MatArgs& p, const floatx4_t (&acc
       }
     return;
   }
+  if constexpr (EPI::RANGES) return;                         // (whole tiles of logits are reduced where they are)
   auto stage = [&](int mb) {
 #pragma unroll
     for (int r = 0; r < RB; ++r)
@@ -406,6 +410,33 @@ __global__ __launch_bounds__(256) void matmul_finish(MatArgs p) {
     }
   }
   EPI::put(p, at.z, row, col, n, v, w, held);
+}
+
+// The same of logits: a wave per row of a tile, its columns' largest and sum as the first of the ranges that the tile has, the others empty.
+template <typename T>
+__global__ __launch_bounds__(256) void matmul_finish_ranges(MatArgs p, int ranges) {
+  const int lane = threadIdx.x & 63, rr = blockIdx.y * 4 + (threadIdx.x >> 6);
+  TileAt at;
+  tile_of(p, p.full + blockIdx.x, (p.m + p.bm - 1) / p.bm, (p.n + p.bn - 1) / p.bn, &at);
+  const int64_t row = (int64_t)at.mt * p.bm + rr;
+  if (rr >= p.bm || row >= p.m) return;
+  const int64_t each = (int64_t)p.bm * p.bn;
+  const float* from = p.slab + (int64_t)blockIdx.x * p.k_split * each + rr * p.bn;
+  const int want = (int)((uint32_t)p.ids[row] - (uint32_t)(p.col0 + at.nt * p.bn));
+  float2 mine = {-INFINITY, 0.0f};
+  for (int c = lane; c < p.bn; c += 64) {
+    float v = from[c];
+    for (int s = 1; s < p.k_split; ++s) v += from[s * each + c];
+    if (at.nt * p.bn + c >= p.n) break;
+    if (want == c) p.picked[row] = v;
+    // (a NaN is passed over by the maximum and makes the sum one)
+    const float top = fmaxf(mine.x, v);
+    mine.y = (mine.y > 0.0f ? mine.y * exp_from<T>(mine.x, top) : mine.y) + (top == -INFINITY && v == v ? 0.0f : exp_from<T>(v, top));
+    mine.x = top;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) mine = join_ranges(mine, float2{__shfl_xor(mine.x, d), __shfl_xor(mine.y, d)});
+  if (lane < ranges) p.part[((int64_t)at.nt * ranges + lane) * p.m + row] = lane == 0 ? mine : float2{-INFINITY, 0.0f};
 }
 
 // ---- operands copied for the ring ---------------------------------------------------------------------------------------
@@ -740,7 +771,7 @@ __attribute__((amdgpu_waves_per_eu(mat_ring_elems(BM, BN, STAGES, planes_of<EPI>
   __builtin_amdgcn_sched_barrier(0);
   wait_vmcnt<0>();                                           // (no load into LDS may outlive the workgroup)
   const int64_t row0 = row_first + wm * TM;
-  if constexpr (EPI::RANGES) {
+  if (EPI::RANGES && at.slot < 0) {
     put_ranges<typename EPI::type>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
   } else {
     __syncthreads();                                         // every wave has left the ring
@@ -972,7 +1003,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void matmul_any(MatArgs p) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) acc[mb][nb] += beside[mb][nb];
   const int64_t row0 = row_first + wm * TM;
-  if constexpr (EPI::RANGES) {
+  if (EPI::RANGES && at.slot < 0) {
     put_ranges<typename EPI::type>(p, acc, row0, col_first + wn * TN, at.nt * WGN + wn);
   } else {
     __syncthreads();

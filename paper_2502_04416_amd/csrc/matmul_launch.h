@@ -46,13 +46,14 @@ hipError_t launch_product(Tile tile, const MatArgs& p, hipStream_t s) {
   if (tile == ANY_64) e = launch_mat_any<64, 64, 2, 2, ACOL, BCOL, EPI>(p, s);
   if (tile == ANY_32) e = launch_mat_any<32, 128, 1, 4, ACOL, BCOL, EPI>(p, s);
   if (e != hipSuccess || p.k_split == 1) return e;
-  if constexpr (!EPI::RANGES) {
-    const int bno = EPI::DUAL ? p.bn / 2 : p.bn;
-    const int64_t tiles = ((int64_t)p.m + p.bm - 1) / p.bm * (((int64_t)p.n + bno - 1) / bno) * p.zs;
-    hipLaunchKernelGGL(matmul_finish<EPI>, dim3((unsigned)(tiles - p.full), (p.bm * bno / 8 + 255) / 256), dim3(256), 0, s, p);
-    e = hipGetLastError();
-  }
-  return e;
+  const int bno = EPI::DUAL ? p.bn / 2 : p.bn;
+  const int64_t tiles = ((int64_t)p.m + p.bm - 1) / p.bm * (((int64_t)p.n + bno - 1) / bno) * p.zs;
+  const unsigned split = (unsigned)(tiles - p.full);
+  if constexpr (EPI::RANGES)
+    hipLaunchKernelGGL(matmul_finish_ranges<typename EPI::type>, dim3(split, p.bm / 4), dim3(256), 0, s, p, kTiles[tile].wgn);
+  else
+    hipLaunchKernelGGL(matmul_finish<EPI>, dim3(split, (p.bm * bno / 8 + 255) / 256), dim3(256), 0, s, p);
+  return hipGetLastError();
 }
 
 // By product and type; each in the translation unit of its group.

@@ -331,15 +331,16 @@ def test_head_gradients_of_nearly_certain_targets(B, dtype, shift, t, d, v):
     m.intact()
 
 
+@pytest.mark.parametrize("split", [1, 3])
 @pytest.mark.parametrize("dtype,shift,tiles", [("bf16", 0, [*RING]), ("bf16", 1, [*RING]), ("bf16", 1, [*ANY]), ("fp32", 0, ["ring 128", "ring 64"]), ("fp32", 0, [*ANY])])
-def test_logits_have_the_same_bits_on_every_tile(B, forced, dtype, shift, tiles):
+def test_logits_have_the_same_bits_on_every_tile(B, forced, dtype, shift, tiles, split):
     """One column of ranges and one token: lse and dweight are functions of the logits alone."""
     dt = TYPES[dtype]
     m = Arena(6, shift=shift)
     x, w, ids = m.normal(1, 1496, dtype=dt), m.normal(20, 1496, dtype=dt, std=0.1), torch.tensor([7], dtype=torch.int32, device="cuda")
     seen = []
     for tile in tiles:
-        forced(tile)
+        forced(tile, split)
         lse, dw = m.out(1), m.out(20, 1496, dtype=dt)
         B.head_loss_forward(x, w, ids, lse=lse)
         B.head_loss_backward(x, w, ids, lse, dweight=dw)
