@@ -124,9 +124,11 @@ __global__ __launch_bounds__(256) void clip_scale(List list, const double* place
   const double ratio = (double)max_norm / (n + (double)eps);
   // a norm that is no number makes every gradient none; without a limit nothing is looked at
   const float c = max_norm == INFINITY || ratio >= 1.0 ? 1.0f : (float)ratio;
-  const Listed& t = list.t[listed_of(list, blockIdx.x)];
+  // (from the list's end on: what the first launch read last may still be in a cache)
+  const uint32_t group = list.groups - 1 - blockIdx.x;
+  const Listed& t = list.t[listed_of(list, group)];
   if (c == 1.0f && t.out == t.g) return;
-  const int64_t count = t.n < 0 ? ~t.n : t.n, from = (int64_t)(blockIdx.x - t.first) * list.run;
+  const int64_t count = t.n < 0 ? ~t.n : t.n, from = (int64_t)(group - t.first) * list.run;
   const int64_t mine = min(list.run, count - from);
   if (t.n < 0) scale_run(static_cast<const float*>(t.g) + from, static_cast<float*>(t.out) + from, mine, c);
   else scale_run(static_cast<const bf16_t*>(t.g) + from, static_cast<bf16_t*>(t.out) + from, mine, c);
