@@ -5,7 +5,9 @@
 //              dWg = X^T dG, dWu = X^T dU, dWd = H^T dY
 // Two launches forward and four backward (and one before each product whose operands are copied, one behind each that splits K): both projections, the activation and the product in one,
 // its gradient behind the product that makes dH, dX one product over twice the width, and the two gradients that share X
-// one launch.
+// one launch.  Bound by the matrix cores (4096 tokens of 4096 x 14336 in bf16: 780 + 365 us forward, 460 + 775 + 735 + 380 backward, 1.24 to 1.36
+// PFLOP/s but for dH's product, whose results are four times as large as its operands' shares) and by the weights' way out of memory with few
+// tokens (one token of 4096 x 11008: 32 + 19 us, 5.6 and 4.8 TB/s).
 #include <algorithm>
 
 #include "../../include/cmoe.h"

@@ -31,12 +31,15 @@ def test_mfma_results_are_waited_for(kernels):
 
 
 def test_nothing_waits_for_the_loads_but_the_barrier(kernels):
-    # loads per wave and step times the steps that stay under way
-    left = {"Li256ELi256ELi5E": 3 * 8, "Li128ELi128ELi5E": 3 * 4, "Li64ELi128ELi6E": 4 * 3, "Li128ELi128ELi3E": 12, "Li64ELi128ELi4E": 2 * 9}
+    # loads per wave and step, and the steps that stay under way
+    rings = {"Li256ELi256ELi5E": (8, 3), "Li128ELi128ELi5E": (4, 3), "Li64ELi128ELi6E": (3, 4), "Li128ELi128ELi3E": (12, 1), "Li64ELi128ELi4E": (9, 2)}
     for name, code in kernels.items():
-        want = next(n for shape, n in left.items() if shape in name)
+        loads, steps = next(n for shape, n in rings.items() if shape in name)
+        want = loads * steps
         mfmas = [i for i, ins in enumerate(code) if ins[1] == "v_mfma_f32_16x16x32_bf16"]
         loop = code[mfmas[0]:mfmas[-1]]
         waits = {ins[2] for ins in loop if ins[1] == "s_waitcnt" and "vmcnt" in ins[2]}
         assert waits == {"vmcnt(%d)" % want}, (name, waits)
+        # three copies of a step are in the code: the two of the loop and the odd last one
+        assert sum(ins[1] == "buffer_load_dwordx4" and "lds" in ins[2].split() for ins in loop) == 3 * loads, name
         assert not [ins for ins in loop if ins[1].startswith(("scratch_", "global_", "flat_", "buffer_store"))], name
