@@ -48,7 +48,7 @@ size_t copy_bytes(const Shape& sh, int planes, int64_t m, int64_t n, int64_t k, 
 
 // direct: bf16 operands that the ring can read where they are.  second: there is a second B.  plan: of logits, where it is settled.
 // The tiles that fill the chip a whole number of times are left whole; the rest, if that is shorter, is split.
-Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace, const LogitsPlan* plan = nullptr) {
+Choice weigh(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace, const LogitsPlan* plan) {
   const Shape sh = shape_of(kind);
   const int pair = kind == PRODUCT_DW && second ? 2 : 1, planes = dtype == CMOE_F32 ? 3 : 1;
   const int64_t steps1 = ((k + 31) / 32) * (sh.segments ? 2 : 1);
@@ -99,6 +99,32 @@ Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int6
     }
   }
   return best;
+}
+
+// The same, remembered by a thread for the questions it has asked lately: a call asks each product's two or three times, for sizes and then to
+// run it, and programs make the same calls over and over (1 us each to weigh, 5 in a backward pass of a few tokens).
+Choice choose(Product kind, int dtype, bool direct, bool second, int64_t m, int64_t n, int64_t k, size_t workspace, const LogitsPlan* plan = nullptr) {
+  struct Asked {
+    int64_t m, n, k;
+    size_t workspace;
+    int how, tile, split, plan;
+    bool operator==(const Asked& o) const {
+      return m == o.m && n == o.n && k == o.k && workspace == o.workspace && how == o.how && tile == o.tile && split == o.split && plan == o.plan;
+    }
+  };
+  constexpr int KEPT = 64;
+  thread_local Asked asked[KEPT] = {};       // (m = 0 is never asked)
+  thread_local Choice said[KEPT];
+  const Asked q = {m, n, k, workspace, (kind << 3) | (dtype << 2) | (direct << 1) | (int)second, tuning().mat_tile, tuning().mat_split,
+                   plan ? plan->k_split * 2 + plan->in_place : -1};
+  uint64_t h = (uint64_t)m * 0x9E3779B97F4A7C15u + (uint64_t)n * 0xC2B2AE3D27D4EB4Fu + (uint64_t)k * 0x165667B19E3779F9u + (uint64_t)workspace * 0x27D4EB2F165667C5u +
+               (uint64_t)(q.how * 64 + q.plan) * 0x85EBCA77C2B2AE63u;
+  const int at = (int)((h ^ h >> 29) >> 20 & (KEPT - 1));
+  if (!(asked[at] == q)) {
+    said[at] = weigh(kind, dtype, direct, second, m, n, k, workspace, plan);
+    asked[at] = q;
+  }
+  return said[at];
 }
 
 int64_t ranges_of(const Choice& c, int64_t n) { return (n + kTiles[c.tile].bn - 1) / kTiles[c.tile].bn * kTiles[c.tile].wgn; }
