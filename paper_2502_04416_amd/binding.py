@@ -706,15 +706,19 @@ def clip_gradients(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6)
     dev, stream = _place("norm", norm)
     to, n, tensor = _operand("norm", norm, torch.float32, (1,), dev), len(grads), torch.Tensor
     # a call's time is the host's where tensors are many and small: columns of the list at once, not tensor by tensor
-    sizes = [*map(tensor.numel, grads)]
-    dtypes = [g.dtype for g in grads]
+    try:
+        sizes = [*map(tensor.numel, grads)]
+        dtypes = [g.dtype for g in grads]
+        out_sizes = sizes if out is grads else [*map(tensor.numel, out)]
+    except TypeError:
+        raise CmoeError("grads and out must be lists of tensors") from None
     lists = (("grads", grads),) if out is grads else (("grads", grads), ("out", out))
     for name, ts in lists:
         if not all(map(tensor.is_contiguous, ts)):
             raise CmoeError("%s must be contiguous tensors" % name)
         if {*map(tensor.get_device, ts)} - {dev}:
             raise CmoeError("%s must be on the current HIP device" % name)
-    if out is not grads and ([*map(tensor.numel, out)] != sizes or [o.dtype for o in out] != dtypes):
+    if out is not grads and (out_sizes != sizes or [o.dtype for o in out] != dtypes):
         raise CmoeError("out must have the sizes and types of grads")
     code = {torch.bfloat16: CMOE_BF16, torch.float32: CMOE_F32}
     if not code.keys() >= {*dtypes}:

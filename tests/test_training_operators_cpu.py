@@ -179,6 +179,14 @@ def test_binding_refuses_what_does_not_fit():
     refused("out must have", binding.clip_gradients, [x], torch.zeros(1), 1.0, out=[])
 
 
+def test_clip_refuses_lists_of_other_things(monkeypatch):
+    """A list with the gradient of a parameter that has none."""
+    monkeypatch.setattr(binding, "_place", lambda name, t: (-1, 0))
+    for grads, kw in (([torch.zeros(3), None], {}), ([torch.zeros(3)], dict(out=[None])), ([1.0], {})):
+        with pytest.raises(binding.CmoeError, match="tensors"):
+            binding.clip_gradients(grads, torch.zeros(1), 1.0, **kw)
+
+
 def test_oracle_against_autograd():
     g = torch.Generator().manual_seed(0)
     n = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64).requires_grad_()  # noqa: E731
