@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void clip_squares(List list, double* places) {
 }
 
 template <typename T>
-__device__ __forceinline__ void scale_run(const T* g, T* out, int64_t n, float c) {
+__device__ __forceinline__ void scale_run(const T* g, T* out, int64_t n, float pre, float c) {
   constexpr int AHEAD = 4;
   int64_t at = (int64_t)threadIdx.x * 8;
   for (; at + (AHEAD - 1) * 2048 + 8 <= n; at += AHEAD * 2048) {
@@ -102,7 +102,7 @@ __device__ __forceinline__ void scale_run(const T* g, T* out, int64_t n, float c
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[a][e] *= c;
+      for (int e = 0; e < 8; ++e) v[a][e] = v[a][e] * pre * c;
       store8(out + at + a * 2048, 8, v[a]);
     }
   }
@@ -111,7 +111,7 @@ __device__ __forceinline__ void scale_run(const T* g, T* out, int64_t n, float c
     const int left = (int)(n - at < 8 ? n - at : 8);
     load8(g + at, left, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= c;
+    for (int e = 0; e < 8; ++e) v[e] = v[e] * pre * c;
     store8(out + at, left, v);
   }
 }
@@ -124,15 +124,18 @@ __global__ __launch_bounds__(256) void clip_scale(List list, const double* place
   if (list.place == 0 && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = (float)n;
   const double ratio = (double)max_norm / (n + (double)eps);
   // a norm that is no number makes every gradient none; without a limit nothing is looked at
-  const float c = max_norm == INFINITY || ratio >= 1.0 ? 1.0f : (float)ratio;
+  // A factor near fp32's smallest numbers or below them would have few bits left: 2^-64 of it goes to the gradient first, exactly (what falls
+  // below the normal numbers there, under 2^-62, would come to less than 2^-162, and that is zero).
+  const float pre = ratio < 0x1p-100 ? 0x1p-64f : 1.0f;
+  const float c = max_norm == INFINITY || ratio >= 1.0 ? 1.0f : (float)(ratio / (double)pre);
   // (from the list's end on: what the first launch read last may still be in a cache)
   const uint32_t group = list.groups - 1 - blockIdx.x;
   const Listed& t = list.t[listed_of(list, group)];
   if (c == 1.0f && t.out == t.g) return;
   const int64_t count = t.n < 0 ? ~t.n : t.n, from = (int64_t)(group - t.first) * list.run;
   const int64_t mine = min(list.run, count - from);
-  if (t.n < 0) scale_run(static_cast<const float*>(t.g) + from, static_cast<float*>(t.out) + from, mine, c);
-  else scale_run(static_cast<const bf16_t*>(t.g) + from, static_cast<bf16_t*>(t.out) + from, mine, c);
+  if (t.n < 0) scale_run(static_cast<const float*>(t.g) + from, static_cast<float*>(t.out) + from, mine, pre, c);
+  else scale_run(static_cast<const bf16_t*>(t.g) + from, static_cast<bf16_t*>(t.out) + from, mine, pre, c);
 }
 
 __global__ void clip_nothing(float* norm) { norm[0] = 0.0f; }

@@ -456,6 +456,27 @@ def test_clip_at_the_ends_of_the_range(B, dtype, std):
     check_clip(B, m, grads, 1.0, eps=0.0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("std,max_norm", [(1e30, 1e-12), (1e37, 1e-8), (1e36, 1e-38), (1e20, 1e-30)])
+def test_clip_by_a_factor_below_normal_numbers(B, dtype, std, max_norm):
+    """The factor alone would be a subnormal number of a few bits; what it scales to is an ordinary one, or nothing."""
+    m = Arena(5)
+    grads, norm = [m.normal(5000, dtype=TYPES[dtype], std=std), m.normal(70, 9, std=std)], m.out(1)
+    out = [m.out(*g.shape, dtype=g.dtype) for g in grads]
+    B.clip_gradients(grads, norm, max_norm, eps=0.0, out=out)
+    want, c = R.clip(grads, max_norm, 0.0)
+    # 5630 normal numbers of 1e37: their norm is 7.4e38, beyond the largest fp32 of 3.4e38, and the factor is none the less 1e-8 of its inverse
+    if want > torch.finfo(torch.float32).max:
+        assert float(norm) == float("inf")
+    else:
+        assert abs(float(norm) - want) <= 2 * O.U32 * want
+    for o, g in zip(out, grads):
+        # half a step of the type, of the factor and of the product, and half of the smallest numbers' step (1.4e-45, in bf16 9.2e-41)
+        size = (g.double() * c).abs()
+        O.check(o, g.double() * c, O.half_step(o.dtype) * size + 4 * O.U32 * size + (5e-41 if o.dtype == torch.bfloat16 else 1e-45), "out")
+    m.intact()
+
+
 def test_clip_of_infinities_and_nan(B):
     inf = float("inf")
     m = Arena(6)
