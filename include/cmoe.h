@@ -426,8 +426,10 @@ int cmoe_adapters_backward(const cmoe_adapters_backward_args* args, void* hip_st
  * Conventions as above: contiguous [rows, cols] batches at any address an element may have (rows of multiples of 8 elements at 16-byte
  * addresses run on faster kernels), sums in fp32, enqueue only, no atomics, outputs that overlap nothing but, where it is said, the very
  * buffer of an input.  Workspaces are 16-byte aligned and may be shared by calls that one stream orders; the functions that say their size
- * return 0 where none is needed.  Tokens, widths and vocabularies are at most 2^20.  Products of fp32 matrices are those of their 24
- * bits, in the order and on the units that the sizes make fastest; an infinity in one may become NaN where it is multiplied. */
+ * return 0 where none is needed.  Tokens, widths and vocabularies are at most 2^20.  Products of fp32 matrices have all
+ * 24 bits of their factors, on the units and in the order that the sizes make fastest: each is within 2.2 x 2^-24 of its value, to either side, if its
+ * factors are zeros or at least 2^-110 and neither it nor a sum is within a hundredth of fp32's largest number.  An infinity may become NaN where
+ * it is multiplied. */
 
 /* The gated feed-forward block F(x) of Eq. 3 on matrices that are trained: gate = x w_gate, up = x w_up,
  * hidden = gate / (1 + exp(-gate)) * up, each rounded to dtype where it is stored; y = base + hidden w_down (of hidden as stored).

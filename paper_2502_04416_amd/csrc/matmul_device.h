@@ -14,9 +14,11 @@
 // with (row >> 2) & 3; 32-byte chunks of a panel's row k with bits 1 and 3 of k (bit 0 chooses the half of the 256-byte bank line,
 // bit 2 is the other read).
 //
-// fp32 on the ring: an operand is copied into three planes of bf16 that hold the first, the second and the last eight of its 24 bits
-// (matmul_prepare; cut, not rounded, so that their sum is the value).  A stage holds a step of all planes, and the six products of planes above
-// 2^-24 are summed: the sums and their errors are those of fp32 products.  Infinities become NaN.  Such a product runs at a sixth of
+// fp32 on the ring: an operand is copied into three planes of bf16 that hold its 24 bits (matmul_prepare; each plane is what is left, rounded to
+// nearest, so that the rests have either sign and the planes' sum is the value).  A stage holds a step of all planes, and six products of planes are
+// summed; the three that are left out, of the smaller planes, come to less than 2^-24 of the product, to either side: a product is as exact as an
+// fp32 one (2^-24 at most for the last sum; planes that are cut have left-out products of the product's own sign: 0.65 x 2^-24 short on average, up to
+// 7.8).  That holds from 2^-110 on (below it the last plane falls under bf16's smallest number).  Infinities become NaN.  Such a product runs at a sixth of
 // the bf16 rate, above 200 TFLOP/s, where the fp32 matrix instructions have 157 at most.  bf16 operands at odd addresses or of odd
 // widths are copied into one plane.
 //
@@ -480,10 +482,12 @@ __global__ __launch_bounds__(256) void matmul_prepare(CopyArgs args) {
     float top[8], mid[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      top[e] = __uint_as_float(__float_as_uint(v[e]) & 0xffff0000u);
+      top[e] = as_stored<bf16_t>(v[e]);
+      // (above bf16's largest number fp32 has some that would be rounded to infinity: their first plane is cut)
+      if (isinf(top[e]) && !isinf(v[e])) top[e] = __uint_as_float(__float_as_uint(v[e]) & 0xffff0000u);
       // (an infinity or NaN is passed on as NaN: its rest is NaN)
       const float rest = v[e] - top[e];
-      mid[e] = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+      mid[e] = as_stored<bf16_t>(rest);
       v[e] = rest - mid[e];
     }
     const int64_t plane = op.rows * op.pitch;

@@ -1,0 +1,93 @@
+"""How exact the operators of a training step are where a sum's bound over many roundings would not show it: single products of fp32 matrices
+on the matrix cores, logits that both passes of the head have to share, factors of the head's gradients, joins of its ranges."""
+import pytest
+import torch
+
+import operator_oracle as O
+from test_gpu_operators import Arena
+
+pytestmark = pytest.mark.gpu
+
+TILES = {"ring 128": 1, "ring 64": 2}
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2502_04416_amd import binding as b
+    b.load()
+    return b
+
+
+@pytest.fixture
+def forced(B):
+    def force(tile=None):
+        B.cmoe_set_tuning("CMOE_MAT_TILE", TILES.get(tile, -1))
+    yield force
+    force()
+
+
+# ---- products of fp32 matrices from planes of bf16 --------------------------------------------------------------------
+
+
+def outer_as_gradient(B, h, d):
+    """The gradient of w_down of a single token: h[i] d[j], a product over one K."""
+    f, n = len(h), len(d)
+    z = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    out = torch.empty(f, n, device="cuda")
+    B.ffn_backward(d[None], z(1, n), z(1, f), z(1, f), h[None], z(n, f), z(n, f), z(f, n), z(1, f), z(1, f), dw_down=out)
+    return out
+
+
+def outer_as_output(B, h, d):
+    """y of a hidden state that is one wide, h[i] d[j]: hidden = gate / (1 + exp(-gate)) * up with a gate that is its own silu."""
+    t, n = len(h), len(d)
+    hidden, y = torch.empty(t, 1, device="cuda"), torch.empty(t, n, device="cuda")
+    x = torch.zeros(t, n, device="cuda")
+    x[:, 0], x[:, 1] = 128.0, h                              # exp(-128) is below half a step of 1
+    wg, wu = torch.zeros(n, 1, device="cuda"), torch.zeros(n, 1, device="cuda")
+    wg[0], wu[1] = 1.0, 2.0 ** -7
+    B.ffn_forward(x, y, wg, wu, d[None], hidden)
+    assert torch.equal(hidden[:, 0], h)
+    return y
+
+
+def spread(n, seed, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    sign = torch.where(torch.rand(n, generator=g) < 0.5, -1.0, 1.0)
+    return (sign * (1 + torch.rand(n, generator=g)) * scale).cuda()
+
+
+# Three planes of eight bits, each rounded to nearest: the second is at most 2^-8 of the value's power of two, the third 2^-17.  The pairs that
+# are left out, second times third twice and third times third, come to less than 2^-24 (1 + 2^-9) of the product; the small pairs' sum is 2^-7 of it at most and
+# rounded five times, the last sum once: 2^-24 (1 + 10 * 2^-7).
+ONE_PRODUCT = 2.15 * O.U32
+
+
+def check_products(out, h, d):
+    want = h.double()[:, None] * d.double()[None]
+    off = (out.double() - want) / want.abs()
+    assert float(off.abs().max()) <= ONE_PRODUCT, float(off.abs().max()) / O.U32
+    return off * want.sign()
+
+
+@pytest.mark.parametrize("tile,outer", [("ring 128", outer_as_gradient), ("ring 128", outer_as_output), ("ring 64", outer_as_output)])
+def test_products_of_fp32_have_24_bits_and_no_side(B, forced, tile, outer):
+    forced(tile)
+    h, d = spread(1024, 1), spread(1000, 2)
+    h[:4] = torch.tensor([0x3f80ffff, 0x3fffffff, 0x3f800001, 0x3f7f7fff], dtype=torch.int32).view(torch.float32).cuda()
+    d[:4] = h[:4]
+    short = check_products(outer(B, h, d), h, d)
+    # errors of either sign: independent from row to row, each at most the bound, so that their mean is within 5 deviations of 2.15 / sqrt(1000)
+    assert abs(float(short.mean())) <= 5 * ONE_PRODUCT / 1000 ** 0.5, float(short.mean()) / O.U32
+
+
+@pytest.mark.parametrize("power", [-110, -100, -60, 60, 127])
+def test_products_of_fp32_over_the_range(B, forced, power):
+    """From 2^-110, whose last bit is bf16's smallest number, to the largest, which no plane may round to infinity."""
+    forced("ring 128")
+    h, d = spread(128, 3, 2.0 ** power), spread(128, 4, 2.0 ** (-power // 2 - 2))
+    most = torch.finfo(torch.float32).max
+    if power == 127:
+        h[0], h[1] = most, -most
+        h[2:5] = torch.tensor([0x7f7f7fff, 0x7f7f8000, 0x7f7f8001], dtype=torch.int32).view(torch.float32).cuda()
+    check_products(outer_as_gradient(B, h, d), h, d)
