@@ -20,7 +20,9 @@ enum Product {
 };
 
 // PRODUCT_LSE and PRODUCT_DLOGITS have to agree to the bit: 1 - p of a likely target is a difference of both.  The ring's tiles sum in one
-// order, those for any operand in another, and so does every K split: both passes go by the same plan, which is a function of the sizes alone.
+// order, those for any operand in another, and so does every K split: both passes go by the same plan, for every piece of a vocabulary, which is a
+// function of the sizes alone.  (bf16 operands that the ring can read where they are need no copies and take the ring in any case: x and the weight have to
+// be at the same alignment in both passes, as the same tensors are.)
 struct LogitsPlan {
   bool in_place;             // of operands that the ring cannot read where they are: no copies
   int k_split;               // of all tiles

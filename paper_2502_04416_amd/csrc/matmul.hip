@@ -58,8 +58,9 @@ Choice weigh(Product kind, int dtype, bool direct, bool second, int64_t m, int64
   const double copy_time = direct ? 0 : kLaunch + (double)copies * (planes == 3 ? 10.0 / 6 : 2) / kBytesPerUs;
   // the operands once, at the rate at which they arrive
   const double arrive = (double)(m * steps1 * 32 + cols * steps1 * 32) * (planes == 3 ? 4 : 2) / kBytesPerUs;
-  // (the kernel for any operand loads 16 bytes at a time: operands that have not so many are copied too.  B may be up to 7 rows or K short of n and k)
-  const bool any = m * k >= 8 && std::max<int64_t>(n - 7, 1) * std::max<int64_t>(k - 7, 1) >= 8;
+  // (the kernel for any operand loads 16 bytes at a time: operands that have not so many are copied too.  B may be up to 7 rows or K short of n and k.
+  // Of logits one row of B has to be enough, so that the last piece of a vocabulary goes the way of all others, however narrow it is)
+  const bool any = sh.logits ? k >= 8 : m * k >= 8 && std::max<int64_t>(n - 7, 1) * std::max<int64_t>(k - 7, 1) >= 8;
   Choice best{RING_128, 0, 1, !direct, 0};
   double best_cost = 1e300;
   auto can = [&](int t) {

@@ -91,3 +91,31 @@ def test_products_of_fp32_over_the_range(B, forced, power):
         h[0], h[1] = most, -most
         h[2:5] = torch.tensor([0x7f7f7fff, 0x7f7f8000, 0x7f7f8001], dtype=torch.int32).view(torch.float32).cuda()
     check_products(outer_as_gradient(B, h, d), h, d)
+
+
+# ---- the logits of both passes -----------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype,shift,t,d,v", [
+    (torch.float32, 0, 65600, 8, 2051), (torch.float32, 0, 65600, 5, 2051), (torch.float32, 1, 2048, 14, 131075), (torch.bfloat16, 1, 65600, 8, 2051),
+    (torch.bfloat16, 1, 65600, 7, 2051), (torch.bfloat16, 0, 65600, 8, 2051), (torch.float32, 0, 300, 3, 7), (torch.float32, 0, 40, 1, 2051),
+])
+def test_a_certain_target_has_no_gradient(B, dtype, shift, t, d, v):
+    """A target that has all of the softmax, in a last piece of the vocabulary that is a few entries wide: every other logit lies more than 104 below
+    (exp is 0 in fp32), so lse is the target's logit, loss 0, and its entry exp(z - lse) - 1 is 0 as long as both passes have the same bits of z."""
+    m = Arena(t + d, shift=shift)
+    # positive factors of many sizes, so that the order of a sum shows in its last bits
+    size = lambda n: torch.exp2(-9 * torch.rand(n, d, generator=m.rng)) * torch.tensor([16.0] + [4.0] * (d - 1))  # noqa: E731
+    x, w = size(t), -size(v)
+    x[:, 0] = 16 + torch.rand(t, generator=m.rng)
+    w[v - 1] = size(1)[0]
+    w[:, 0] = -16 - torch.rand(v, generator=m.rng)
+    w[v - 1, 0] *= -1
+    x, w = m.put(x.to(dtype)), m.put(w.to(dtype))
+    ids = torch.full((t,), v - 1, dtype=torch.int32, device="cuda")
+    loss, lse, dx, dw = m.out(t), m.out(t), m.out(t, d, dtype=dtype), m.out(v, d, dtype=dtype)
+    B.head_loss_forward(x, w, ids, loss, lse)
+    assert bool((loss == 0).all())
+    B.head_loss_backward(x, w, ids, lse, dx=dx, dweight=dw)
+    assert int((dx != 0).sum()) == 0 and int((dw != 0).sum()) == 0
+    m.intact()
