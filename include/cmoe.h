@@ -523,7 +523,7 @@ size_t cmoe_head_loss_backward_workspace_bytes(int64_t tokens, int32_t d, int32_
 int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args, void* hip_stream);
 
 /* The norm n of all tensors of a list together and, with c = min(1, max_norm / (n + eps)), out = c * g of each, rounded to its dtype.
- * Squares and sums are fp64.  out may be g itself (and then nothing is written where c = 1); the same tensor may be listed twice only with
+ * c = 1 where n + eps is 0.  Squares and sums are fp64.  out may be g itself (and then nothing is written where c = 1); the same tensor may be listed twice only with
  * outputs of their own.  max_norm = infinity: c = 1, whatever the norm.  A norm that is infinite or NaN shows in every gradient:
  * c is 0 or NaN.  (One beyond fp32 is written as infinity; c goes by its value.)  The list is host memory, read during the call. */
 typedef struct {

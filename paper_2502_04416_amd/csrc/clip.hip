@@ -1,5 +1,5 @@
 // The norm of a list of tensors together, and the tensors scaled so that it is at most a given one:
-//   n = sqrt(sum over all tensors of v^2),  c = min(1, max_norm / (n + eps)),  out = c v
+//   n = sqrt(sum over all tensors of v^2),  c = min(1, max_norm / (n + eps)), 1 where n + eps is 0,  out = c v
 // Squares and sums are fp64: a bf16 or fp32 gradient's square neither overflows nor vanishes there, and the vector units do a
 // conversion and an fp64 multiply-add per element in a fraction of the time that memory takes for it.  Every workgroup sums one run of one
 // tensor and leaves the sum at its own place; in the second launch every workgroup adds all places in the same order.  No
@@ -122,7 +122,8 @@ __global__ __launch_bounds__(256) void clip_scale(List list, const double* place
   for (uint32_t i = threadIdx.x; i < list.places; i += 256) sum += places[i];
   const double n = sqrt(add_all(sum, shared));
   if (list.place == 0 && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = (float)n;
-  const double ratio = (double)max_norm / (n + (double)eps);
+  const double over = n + (double)eps;
+  const double ratio = over == 0.0 ? 1.0 : (double)max_norm / over;        // (zeros stay zeros, whatever the limit)
   // a norm that is no number makes every gradient none; without a limit nothing is looked at
   // A factor near fp32's smallest numbers or below them would have few bits left: 2^-64 of it goes to the gradient first, exactly (what falls
   // below the normal numbers there, under 2^-62, would come to less than 2^-162, and that is zero).
