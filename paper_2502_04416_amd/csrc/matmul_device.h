@@ -210,11 +210,12 @@ struct EpiLse {
   static __device__ __forceinline__ void put(const MatArgs&, int, int64_t, int, int, float (&)[8], float (&)[8], const Held&) {}
 };
 
-// The largest of two, and the exponentials summed below it.  An empty range is (-inf, 0).
+// The largest of two, and the exponentials summed below it.  An empty range is (-inf, 0).  (expf, of bf16 logits too: a range's factor is an error
+// of its whole sum, and a power of two of (x - from) log2 e would be off by |x - from| roundings, 14 at -13.)
 __device__ __forceinline__ float2 join_ranges(float2 a, float2 b) {
   const float top = fmaxf(a.x, b.x);
   if (top == -INFINITY) return float2{top, a.y + b.y};
-  return float2{top, a.y * __expf(a.x - top) + b.y * __expf(b.x - top)};
+  return float2{top, a.y * expf(a.x - top) + b.y * expf(b.x - top)};
 }
 
 // Rows of a wave's tile, reduced over its columns where they are: a lane holds columns kq * 4 .. + 3 of every block of 16 in row r16.

@@ -119,3 +119,28 @@ def test_a_certain_target_has_no_gradient(B, dtype, shift, t, d, v):
     B.head_loss_backward(x, w, ids, lse, dx=dx, dweight=dw)
     assert int((dx != 0).sum()) == 0 and int((dw != 0).sum()) == 0
     m.intact()
+
+
+# ---- the join of the ranges --------------------------------------------------------------------------------------------
+
+
+def test_ranges_are_joined_with_fp32_exponentials(B):
+    """One logit of 0 behind 2^20 - 1 equal ones of -12.2 to -13.8, where an exponential as 2^(x log2 e) is off by up to 14 roundings.  Every range
+    but the last sums to a whole number, exactly; what is left to be rounded lies where the last range meets the others."""
+    t, v = 64, 1 << 20
+    m = Arena(3, shift=0)
+    x, w = torch.zeros(t, 8), torch.zeros(v, 8)
+    x[:, 0], w[:v - 1, 0] = 12.2 + 1.6 * torch.rand(t, generator=m.rng), -1.0
+    x, w, ids = m.put(x), m.put(w), torch.full((t,), v - 1, dtype=torch.int32, device="cuda")
+    loss, lse = m.out(t), m.out(t)
+    B.head_loss_forward(x, w, ids, loss, lse)
+    want = torch.log1p((v - 1) * torch.exp(-x[:, 0].double()))
+    # Roundings of 2^-24, spread evenly over what each may be off by (a third of its square is the variance).  The sum S = 1 + (2 to 6.3) has twelve
+    # additions below 2 and two beyond: (12 + 2 * 4) / 3 / S^2, at S = 2.06 1.57; the others' exponential within one unit of the last place, two roundings:
+    # 4/3, and its product 1/3, of at most (1 - 1 / S)^2 = 0.71; the logarithm within one unit of its last place, two roundings from 1 on: 4/3.
+    # Of 64 tokens' mean square five standard deviations, each sqrt(2 / 64), more.
+    variance = 1.57 + (4 / 3 + 1 / 3) * 0.71 + 4 / 3
+    for got in (loss, lse):
+        off = (got.double() - want) / O.U32
+        assert float(off.square().mean()) <= variance * (1 + 5 * (2 / t) ** 0.5), float(off.square().mean()) ** 0.5
+    m.intact()
