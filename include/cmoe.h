@@ -521,6 +521,9 @@ typedef struct {
 } cmoe_head_loss_backward_args;
 size_t cmoe_head_loss_backward_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab, int32_t dtype);
 int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args, void* hip_stream);
+/* The same with scale * factor[0], which is device memory and read by the kernels: 1 / the number of targets, where only the device knows it.
+ * NULL: 1. */
+int cmoe_head_loss_backward_scaled(const cmoe_head_loss_backward_args* args, const float* factor, void* hip_stream);
 
 /* The norm n of all tensors of a list together and, with c = min(1, max_norm / (n + eps)), out = c * g of each, rounded to its dtype.
  * c = 1 where n + eps is 0.  Squares and sums are fp64.  out may be g itself (and then nothing is written where c = 1); the same tensor may be listed twice only with

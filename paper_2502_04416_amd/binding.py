@@ -48,6 +48,7 @@ EXPORTS = [
     "cmoe_adapters_forward", "cmoe_adapters_backward", "cmoe_adapters_backward_workspace_bytes",
     "cmoe_ffn_forward", "cmoe_ffn_forward_workspace_bytes", "cmoe_ffn_backward", "cmoe_ffn_backward_workspace_bytes",
     "cmoe_head_loss_forward", "cmoe_head_loss_forward_workspace_bytes", "cmoe_head_loss_backward", "cmoe_head_loss_backward_workspace_bytes",
+    "cmoe_head_loss_backward_scaled",
     "cmoe_clip_gradients", "cmoe_clip_gradients_workspace_bytes",
 ]
 
@@ -119,6 +120,7 @@ def load():
     for name in ("cmoe_norm_forward", "cmoe_norm_backward", "cmoe_adapters_forward", "cmoe_adapters_backward", "cmoe_ffn_forward", "cmoe_ffn_backward",
                  "cmoe_head_loss_forward", "cmoe_head_loss_backward"):
         getattr(lib, name).argtypes = [C.c_char_p, vp]                   # the packed bytes of an argument struct
+    lib.cmoe_head_loss_backward_scaled.argtypes = [C.c_char_p, vp, vp]
     lib.cmoe_norm_backward_workspace_bytes.argtypes = [i64, C.c_int32]
     lib.cmoe_norm_backward_workspace_bytes.restype = sz
     lib.cmoe_adapters_backward_workspace_bytes.argtypes = [i64] + [C.c_int32] * 5
@@ -668,16 +670,19 @@ def head_loss_forward(x, weight, ids, loss=None, lse=None) -> None:
            "cmoe_head_loss_forward")
 
 
-def head_loss_backward(x, weight, ids, lse, *, dx=None, dweight=None, dloss=None, scale: float = 1.0) -> None:
+def head_loss_backward(x, weight, ids, lse, *, dx=None, dweight=None, dloss=None, scale=1.0) -> None:
     """Gradients of scale * sum(dloss * loss) from the forward pass's lse: dx and dweight, of x's type; one of them at least.
 
     dloss: [tokens] fp32, None: 1 for every token.  A factor that all tokens share, 1 / their number for instance, belongs into scale,
-    which is not rounded to the type on the way."""
+    which is not rounded to the type on the way: a finite number, or one fp32 value on the device, which the kernels read there."""
+    import torch
     dtype, code, t, d, v = _head_shapes(x, weight)
-    if not -3.4e38 <= scale <= 3.4e38:
+    factor = 0
+    if isinstance(scale, torch.Tensor) and scale.dtype is torch.float32 and scale.numel() == 1 and scale.is_cuda and scale.get_device() == x.get_device():
+        factor, scale = scale.data_ptr(), 1.0
+    elif not -3.4e38 <= scale <= 3.4e38:
         raise CmoeError("scale must be finite")
     dev, stream = _place("x", x)
-    import torch
     operands = (
         _operand("x", x, dtype, (t, d), dev), _operand("weight", weight, dtype, (v, d), dev), _operand("ids", ids, torch.int32, (t,), dev),
         _operand("lse", lse, torch.float32, (t,), dev), _operand("dloss", dloss, torch.float32, (t,), dev), _operand("dx", dx, dtype, (t, d), dev),
@@ -686,7 +691,7 @@ def head_loss_backward(x, weight, ids, lse, *, dx=None, dweight=None, dloss=None
     nbytes = lib.cmoe_head_loss_backward_workspace_bytes(t, d, v, code)
     ws = _workspace(nbytes) if nbytes else None
     args = _HEAD_LOSS_BACKWARD.pack(*operands, ws.data_ptr() if nbytes else 0, nbytes, t, _HEAD_LOSS_BACKWARD.size, code, d, v, scale, 0)
-    _check(lib.cmoe_head_loss_backward(args, stream), "cmoe_head_loss_backward")
+    _check(lib.cmoe_head_loss_backward_scaled(args, factor, stream), "cmoe_head_loss_backward")
 
 
 def clip_gradients(grads, norm, max_norm: float, *, out=None, eps: float = 1e-6) -> None:

@@ -8,8 +8,8 @@
 // dW takes x from a copy without the rows of tokens that have no target: what such a row holds (padding, NaN) would reach every row of dW as 0 times it.
 // Bound by the matrix cores (8192 tokens of 4096 over 131072 in bf16: forward 6.5 ms, 1.35 PFLOP/s; per piece of 8192 entries 440 us of logits, 420 of dX,
 // 370 of dW) and by the vocabulary's way out of memory with few tokens (one token over 32768: 45 us, 5.9 TB/s).
-// `scale` is applied to the sums in fp32, and not to dZ: what all tokens share would round the entries of all targets, which are all
-// close to -scale, to the same side.
+// `scale` and the factor on the device are applied to the sums in fp32, and not to dZ: what all tokens share would round the entries of all targets,
+// which are all close to -scale, to the same side.
 #include <algorithm>
 
 #include "../../include/cmoe.h"
@@ -186,7 +186,9 @@ extern "C" size_t cmoe_head_loss_backward_workspace_bytes(int64_t tokens, int32_
   return check_sizes("cmoe_head_loss_backward", dtype, tokens, d, vocab) || tokens == 0 ? 0 : BackwardSpace(dtype, tokens, d, vocab).total;
 }
 
-extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args, void* hip_stream) {
+extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args, void* hip_stream) { return cmoe_head_loss_backward_scaled(args, nullptr, hip_stream); }
+
+extern "C" int cmoe_head_loss_backward_scaled(const cmoe_head_loss_backward_args* args, const float* factor, void* hip_stream) {
   using namespace cmoe;
   const char* what = "cmoe_head_loss_backward";
   if (!args || args->struct_bytes != (int32_t)sizeof(*args)) return fail(CMOE_EINVAL, "%s: the arguments are null or a struct of another version", what);
@@ -207,10 +209,12 @@ extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args,
   const BackwardSpace ws(a.dtype, a.tokens, a.d, a.vocab);
   if (int rc = check_workspace(what, a.workspace, a.workspace_bytes, ws.total)) return rc;
   const uint64_t rows = (uint64_t)a.tokens * 4, td = (uint64_t)a.tokens * a.d * es, vd = (uint64_t)a.vocab * a.d * es;
-  if (int rc = check_operands(what, {{"x", a.x, td, es}, {"weight", a.weight, vd, es}, {"ids", a.ids, rows, 4}, {"lse", a.lse, rows, 4}, {"dloss", a.dloss, rows, 4}},
+  if (int rc = check_operands(what, {{"x", a.x, td, es}, {"weight", a.weight, vd, es}, {"ids", a.ids, rows, 4}, {"lse", a.lse, rows, 4}, {"dloss", a.dloss, rows, 4},
+                                     {"factor", factor, 4, 4}},
                               {{"dx", a.dx, td, es}, {"dweight", a.dweight, vd, es}, {"the workspace", a.workspace, ws.total, 16}}))
     return rc;
   char* base = static_cast<char*>(a.workspace);
+  w.factor = factor;                       // (not without tokens: the zeros above are zeros whatever it is)
   if (a.dweight) {
     w.b = base + ws.rows;
     const unsigned groups = (unsigned)((a.tokens * ((a.d + 7) / 8) + 255) / 256);
@@ -236,7 +240,7 @@ extern "C" int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args,
       q.a = base, q.lda = ws.ld, q.b = rows_of_w, q.ldb = a.d;
       q.m = (int)a.tokens, q.n = a.d, q.k = padded, q.k_b = n;
       q.acc = reinterpret_cast<float*>(base + ws.acc), q.first = first == 0, q.last = first + n == a.vocab;
-      q.c = a.dx, q.ldc = a.d, q.alpha = a.scale;
+      q.c = a.dx, q.ldc = a.d, q.alpha = a.scale, q.factor = factor;
       if (hipError_t e = matmul(PRODUCT_DHEAD, a.dtype, q, room, room_bytes, s)) return launched(what, e);
     }
     if (a.dweight) {

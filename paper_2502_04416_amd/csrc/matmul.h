@@ -13,10 +13,10 @@ enum Product {
   PRODUCT_DOWN,     // A by rows, B by columns: c = e1 + A B (e1 may be null)
   PRODUCT_DGATED,   // A, B by rows: from dH = A B^T, G = e1, U = e2: c = dG, c2 = dU
   PRODUCT_DX,       // A, B by rows, K in two parts: c = e1 + A B^T + A2 B2^T (e1 may be null)
-  PRODUCT_DW,       // A, B by columns: c = alpha A^T B, and c2 = alpha A^T B2 where c2 is given
+  PRODUCT_DW,       // A, B by columns: c = alpha A^T B, and c2 = alpha A^T B2 where c2 is given (alpha times factor[0], where that is given)
   PRODUCT_LSE,      // A, B by rows: per row and column range the largest logit and the sum of exponentials; the target's logit
   PRODUCT_DLOGITS,  // A, B by rows: c = row weight * (exp(A B^T - lse) - [target])
-  PRODUCT_DHEAD,    // A by rows, B by columns: acc (+)= A B over the pieces of a vocabulary, c = alpha * acc with the last one
+  PRODUCT_DHEAD,    // A by rows, B by columns: acc (+)= A B over the pieces of a vocabulary, c = alpha * acc with the last one (factor as above)
 };
 
 // PRODUCT_LSE and PRODUCT_DLOGITS have to agree to the bit: 1 - p of a likely target is a difference of both.  The ring's tiles sum in one
@@ -40,6 +40,7 @@ struct MatArgs {
   const void *e1, *e2;
   int64_t ldc;               // of c, c2, c3, e1 and e2
   float alpha;
+  const float* factor;       // of alpha, on the device, or null: 1
   // head
   float* acc;                // [m, n]
   int first, last;           // pieces of the vocabulary

@@ -76,20 +76,24 @@ __device__ __forceinline__ float held(const Raw8<T>& r, int e) {
   return __uint_as_float(e & 1 ? r.w[e >> 1] & 0xffff0000u : r.w[e >> 1] << 16);
 }
 
+__device__ __forceinline__ float alpha_of(const MatArgs& p) { return p.factor ? p.alpha * *p.factor : p.alpha; }
+
 template <typename T, bool SEGS, bool PAIR>
 struct EpiStore {                                             // PRODUCT_DOWN, PRODUCT_DX, PRODUCT_DW
   static constexpr bool LOGITS = false, DUAL = false, SEGMENTS = SEGS, PAIRED = PAIR, RANGES = false;
   typedef T type;
   struct Held {
     Raw8<T> base;
+    float alpha;
   };
   static __device__ __forceinline__ void hold(const MatArgs& p, int64_t row, int col, int n, Held& h) {
-    if (!PAIR && p.e1) hold8(static_cast<const T*>(p.e1) + row * p.ldc + col, n, h.base);
+    if (PAIR) h.alpha = alpha_of(p);
+    else if (p.e1) hold8(static_cast<const T*>(p.e1) + row * p.ldc + col, n, h.base);
   }
   static __device__ __forceinline__ void put(const MatArgs& p, int z, int64_t row, int col, int n, float (&v)[8], float (&)[8], const Held& h) {
     if (PAIR) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= p.alpha;
+      for (int e = 0; e < 8; ++e) v[e] *= h.alpha;
     } else if (p.e1) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += held(h.base, e);
@@ -182,9 +186,11 @@ struct EpiDHead {
   typedef T type;
   struct Held {
     Raw8<float> before;
+    float alpha;
   };
   static __device__ __forceinline__ void hold(const MatArgs& p, int64_t row, int col, int n, Held& h) {
     if (!p.first) hold8(p.acc + row * p.n + col, n, h.before);
+    if (p.last) h.alpha = alpha_of(p);
   }
   static __device__ __forceinline__ void put(const MatArgs& p, int, int64_t row, int col, int n, float (&v)[8], float (&)[8], const Held& h) {
     if (!p.first) {
@@ -193,7 +199,7 @@ struct EpiDHead {
     }
     if (p.last) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= p.alpha;
+      for (int e = 0; e < 8; ++e) v[e] *= h.alpha;
       store8(static_cast<T*>(p.c) + row * p.ldc + col, n, v);
     } else {
       store8(p.acc + row * p.n + col, n, v);

@@ -31,12 +31,9 @@ class Head:
         loss, lse, dout = torch.empty(len(out), device="cuda"), torch.empty(len(out), device="cuda"), torch.empty_like(out)
         dweight = torch.empty_like(self.weight) if train else None
         binding.head_loss_forward(out, self.weight, targets, loss, lse)
-        each = (((targets >= 0) & (targets < len(self.weight))).sum().clamp(min=1)).reciprocal()
-        # (the mean's factor is on the device: gradients of the sum, scaled when all are there)
-        binding.head_loss_backward(out, self.weight, targets, lse, dx=dout, dweight=dweight)
-        dout *= each
-        if train:
-            dweight *= each
+        # the mean's factor, on the device and in fp32: the gradients' sums are scaled by it before they are rounded
+        each = ((targets >= 0) & (targets < len(self.weight))).sum().clamp(min=1).float().reciprocal()
+        binding.head_loss_backward(out, self.weight, targets, lse, dx=dout, dweight=dweight, scale=each)
         return loss.sum() * each, dout, dweight
 
 
