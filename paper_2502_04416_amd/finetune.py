@@ -15,11 +15,17 @@ from typing import Optional
 from . import binding, recovery, synth
 
 
+def _trained(v):
+    """A copy of a tensor or array, in fp32 on the device: what is trained is not the caller's."""
+    import torch
+    return torch.as_tensor(v).detach().to(device="cuda", dtype=torch.float32, copy=True, memory_format=torch.contiguous_format)
+
+
 class Head:
-    """Rows of a vocabulary, [vocab, d] in fp32 as trained; the operators read them in `dtype`."""
+    """Rows of a vocabulary, [vocab, d] in fp32 as trained, a copy of those given; the operators read them in `dtype`."""
 
     def __init__(self, weight, dtype):
-        self.params, self.dtype = {"head": weight.float().contiguous().cuda()}, dtype
+        self.params, self.dtype = {"head": _trained(weight)}, dtype
         self.cast()
 
     def cast(self):
@@ -38,12 +44,12 @@ class Head:
 
 
 class Dense:
-    """The trained dense block.  Matrices in the paper's orientation: w_gate, w_up [d, d_ff], w_down [d_ff, d]."""
+    """The trained dense block.  Matrices in the paper's orientation: w_gate, w_up [d, d_ff], w_down [d_ff, d]; copies of them are trained."""
 
     def __init__(self, w_gate, w_up, w_down, head: Head, form: str = "rms", eps: float = 1e-5):
         import torch
         self.head, self.form, self.eps, self.steps = head, form, eps, 0
-        self.params = {k: torch.as_tensor(v, dtype=torch.float32).contiguous().cuda() for k, v in (("gate", w_gate), ("up", w_up), ("down", w_down))}
+        self.params = {k: _trained(v) for k, v in (("gate", w_gate), ("up", w_up), ("down", w_down))}
         self.params["weight"] = torch.ones(self.params["gate"].shape[0], device="cuda")
         self.params.update(head.params)
         self.moments = {k: (torch.zeros_like(v), torch.zeros_like(v)) for k, v in self.params.items()}
