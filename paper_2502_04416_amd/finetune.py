@@ -34,7 +34,8 @@ class Head:
     def loss(self, out, targets, train: bool = True):
         """(mean loss of the targets in the vocabulary, gradient of out, gradient of the rows or None)."""
         import torch
-        loss, lse, dout = torch.empty(len(out), device="cuda"), torch.empty(len(out), device="cuda"), torch.empty_like(out)
+        loss, lse = (torch.empty(len(out), dtype=torch.float32, device="cuda") for _ in range(2))
+        dout = torch.empty_like(out)
         dweight = torch.empty_like(self.weight) if train else None
         binding.head_loss_forward(out, self.weight, targets, loss, lse)
         # the mean's factor, on the device and in fp32: the gradients' sums are scaled by it before they are rounded
@@ -50,7 +51,7 @@ class Dense:
         import torch
         self.head, self.form, self.eps, self.steps = head, form, eps, 0
         self.params = {k: _trained(v) for k, v in (("gate", w_gate), ("up", w_up), ("down", w_down))}
-        self.params["weight"] = torch.ones(self.params["gate"].shape[0], device="cuda")
+        self.params["weight"] = torch.ones(self.params["gate"].shape[0], dtype=torch.float32, device="cuda")
         self.params.update(head.params)
         self.moments = {k: (torch.zeros_like(v), torch.zeros_like(v)) for k, v in self.params.items()}
         self._cast()
@@ -87,7 +88,7 @@ class Dense:
         """One step of Adam on gradients clipped together; (loss, their norm) before it, on the device."""
         import torch
         loss, grads = self.gradients(x, residual, targets)
-        norm = torch.empty(1, device="cuda")
+        norm = torch.empty(1, dtype=torch.float32, device="cuda")
         binding.clip_gradients(list(grads.values()), norm, max_norm)
         self.steps += 1
         for k, g in grads.items():
@@ -119,7 +120,7 @@ def main(steps: int = 200, tokens: int = 1024, vocab: int = 4000):
         return x, torch.zeros_like(x), (x.float() @ says).argmax(1).to(torch.int32)
 
     def loss_of(out, targets):
-        loss = torch.empty(len(out), device="cuda")
+        loss = torch.empty(len(out), dtype=torch.float32, device="cuda")
         binding.head_loss_forward(out, head.weight, targets, loss)
         return float(loss.mean())
 

@@ -34,11 +34,11 @@ class Block:
         self.layer, self.form, self.eps, self.p, self.seed, self.steps = layer, form, eps, p, seed, 0
         d = layer.cfg.d_model
         self.dtype = torch.bfloat16 if layer.bf16 else torch.float32
-        rng = torch.Generator().manual_seed(seed)
+        rng, f32 = torch.Generator().manual_seed(seed), dict(dtype=torch.float32, device="cuda")
         # trained in fp32; the operators read them in the layer's type
-        self.params = {"a": (torch.randn(n_adapters, rank, d, generator=rng) * d ** -0.5).cuda(), "b": torch.zeros(n_adapters, d, rank, device="cuda"),
-                       "weight": torch.ones(d, device="cuda")}
-        self.scale = torch.full((n_adapters,), alpha / rank, device="cuda")
+        self.params = {"a": (torch.randn(n_adapters, rank, d, generator=rng, dtype=torch.float32) * d ** -0.5).cuda(), "b": torch.zeros(n_adapters, d, rank, **f32),
+                       "weight": torch.ones(d, **f32)}
+        self.scale = torch.full((n_adapters,), alpha / rank, **f32)
         self.moments = {k: (torch.zeros_like(v), torch.zeros_like(v)) for k, v in self.params.items()}
         self._cast()
 
