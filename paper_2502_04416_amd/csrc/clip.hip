@@ -4,7 +4,7 @@
 // conversion and an fp64 multiply-add per element in a fraction of the time that memory takes for it.  Every workgroup sums one run of one
 // tensor and leaves the sum at its own place; in the second launch every workgroup adds all places in the same order.  No
 // atomics, so the same tensors give the same bits.  Bound by memory: 1.08 G elements in bf16, 2.2 GB, are read in 415 us (5.2 TB/s) and read and written
-// in 845 (5.1); small lists by the host, 0.55 to 0.7 us a tensor, with kernels of 3 and 5 us.
+// in 845 (5.1); small lists by the host, 0.45 to 0.7 us a tensor, with kernels of 3 and 5 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

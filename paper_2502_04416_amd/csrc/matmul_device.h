@@ -39,7 +39,8 @@ constexpr float LOG2E = 1.44269504088896341f;
 // exp(x - from), 1 where they are equal: the difference is taken first, or the product's rounding would be an error of every exponential of a row.
 template <typename T> __device__ __forceinline__ float exp_from(float x, float from);
 template <> __device__ __forceinline__ float exp_from<float>(float x, float from) { return expf(x - from); }
-// (the hardware's power of two: 2^-24 |x - from| relative)
+// (the hardware's power of two: 1.3 x 2^-24 |x - from| relative, of logits that are sums in fp32 of thousands of products and
+// no more exact.  expf: head-sized steps 2 to 2.5 per cent longer, 8192 tokens over 131072 entries 27.0 -> 27.7 ms)
 template <> __device__ __forceinline__ float exp_from<bf16_t>(float x, float from) { return __builtin_amdgcn_exp2f((x - from) * LOG2E); }
 template <typename T> __device__ __forceinline__ float sigmoid_of(float x);
 template <> __device__ __forceinline__ float sigmoid_of<float>(float x) { return 1.0f / (1.0f + expf(-x)); }

@@ -10,8 +10,6 @@ cmoe_build; recovery.Block then trains adapters beside the restructured layer on
 """
 from __future__ import annotations
 
-from typing import Optional
-
 from . import binding, recovery, synth
 
 
