@@ -4,11 +4,12 @@ import pytest
 import torch
 
 import operator_oracle as O
-from test_gpu_operators import Arena
+from test_gpu_operators import Arena, TYPES
+from test_gpu_training_operators import run_head
 
 pytestmark = pytest.mark.gpu
 
-TILES = {"ring 128": 1, "ring 64": 2}
+RINGS = {"ring 128": 1, "ring 64": 2}
 
 
 @pytest.fixture(scope="module")
@@ -21,7 +22,7 @@ def B():
 @pytest.fixture
 def forced(B):
     def force(tile=None):
-        B.cmoe_set_tuning("CMOE_MAT_TILE", TILES.get(tile, -1))
+        B.cmoe_set_tuning("CMOE_MAT_TILE", RINGS.get(tile, -1))
     yield force
     force()
 
@@ -144,3 +145,10 @@ def test_ranges_are_joined_with_fp32_exponentials(B):
         off = (got.double() - want) / O.U32
         assert float(off.square().mean()) <= variance * (1 + 5 * (2 / t) ** 0.5), float(off.square().mean()) ** 0.5
     m.intact()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("t,d,v", [(1, 8, 1), (1, 9, 1), (3, 8, 2), (1, 15, 7), (2, 7, 1), (5, 14, 9), (1, 4, 2)])
+def test_heads_of_a_few_values(B, dtype, t, d, v):
+    """Operands that have just the 16 bytes that a load takes, and fewer."""
+    run_head(B, Arena(t + d + v, shift=1), TYPES[dtype], t, d, v, weighted=v == 1)
