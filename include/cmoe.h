@@ -426,10 +426,9 @@ int cmoe_adapters_backward(const cmoe_adapters_backward_args* args, void* hip_st
  * Conventions as above: contiguous [rows, cols] batches at any address an element may have (rows of multiples of 8 elements at 16-byte
  * addresses run on faster kernels), sums in fp32, enqueue only, no atomics, outputs that overlap nothing but, where it is said, the very
  * buffer of an input.  Workspaces are 16-byte aligned and may be shared by calls that one stream orders; the functions that say their size
- * return 0 where none is needed.  Tokens, widths and vocabularies are at most 2^20.  Products of fp32 matrices have all
- * 24 bits of their factors, on the units and in the order that the sizes make fastest: each is within 2.2 x 2^-24 of its value, to either side, if its
- * factors are zeros or at least 2^-110 and neither it nor a sum is within a hundredth of fp32's largest number.  An infinity may become NaN where
- * it is multiplied. */
+ * return 0 where none is needed.  Tokens, widths and vocabularies are at most 2^20.  Products of fp32 matrices take all 24 bits of their factors,
+ * on the units and in the order that the sizes make fastest: each is within 2.2 x 2^-24 of its value, to either side, if its factors are zeros
+ * or at least 2^-110 and neither it nor a sum is within a hundredth of fp32's largest number.  An infinity may become NaN where it is multiplied. */
 
 /* The gated feed-forward block F(x) of Eq. 3 on matrices that are trained: gate = x w_gate, up = x w_up,
  * hidden = gate / (1 + exp(-gate)) * up, each rounded to dtype where it is stored; y = base + hidden w_down (of hidden as stored).
@@ -525,9 +524,9 @@ int cmoe_head_loss_backward(const cmoe_head_loss_backward_args* args, void* hip_
  * NULL: 1. */
 int cmoe_head_loss_backward_scaled(const cmoe_head_loss_backward_args* args, const float* factor, void* hip_stream);
 
-/* The norm n of all tensors of a list together and, with c = min(1, max_norm / (n + eps)), out = c * g of each, rounded to its dtype.
- * c = 1 where n + eps is 0.  Squares and sums are fp64.  out may be g itself (and then nothing is written where c = 1); the same tensor may be listed twice only with
- * outputs of their own.  max_norm = infinity: c = 1, whatever the norm.  A norm that is infinite or NaN shows in every gradient:
+/* The norm n of all tensors of a list together and, with c = min(1, max_norm / (n + eps)), 1 where n + eps is 0, out = c * g of each, rounded to
+ * its dtype.  Squares and sums are fp64.  out may be g itself (and then nothing is written where c = 1); the same tensor may be listed twice
+ * only with outputs of their own.  max_norm = infinity: c = 1, whatever the norm.  A norm that is infinite or NaN shows in every gradient:
  * c is 0 or NaN.  (One beyond fp32 is written as infinity; c goes by its value.)  The list is host memory, read during the call. */
 typedef struct {
   const void* g;
